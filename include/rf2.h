@@ -13,6 +13,9 @@
  *   rf2_unpermute         inverse of the Sec. 3.3 permutation
  *   (rf2_block_sparse_attn_unpermuted does the last two in one kernel.)
  *
+ * Beside it, for models that generate chunk after chunk (new frames, or tokens, that attend to everything generated
+ * before): a paged cache of keys and values and the attention of new tokens over it, rf2_paged_* below.
+ *
  * Conventions
  *   - Every function returns an int: RF2_OK (0) or a negative RF2_ERR_* code.
  *     Nothing throws, aborts or synchronises the device behind the caller's back.
@@ -239,6 +242,134 @@ int rf2_block_sparse_attn_unpermuted(const rf2_plan* plan, const void* qp, const
 
 /* o[perm[p]] = op[p] for p < N.  op: [B, Hh, N_pad, d] bf16; o: [B, Hh, N, d] (or [B, N, Hh, d]) bf16. */
 int rf2_unpermute(const rf2_plan* plan, const void* op, void* o, void* stream);
+
+/* ---- Paged cache ------------------------------------------------------------------------------------------------
+ *
+ * The keys and values of many sequences in one pool of pages, each page holding `page` tokens of one sequence, all K/V
+ * heads.  Row s of a block table lists the pages of sequence s in order; token j of it lies at slot
+ *     block_table[s][j / page] * page + j % page.
+ * A step of a program:  rf2_paged_append (pages and slots for the new tokens), then for every layer rf2_paged_store (its
+ * K and V rows into its cache) and rf2_paged_attn; rf2_paged_release when sequences are finished.  All four read lengths,
+ * tables and counts from device memory, so a step can be captured in a graph and replayed for other lengths.
+ *
+ * Conventions as above (codes, streams, devices, ownership); nothing is allocated and no work is put off.  Pointers to
+ * device memory are aligned to 16 bytes, those to int32 to 4.  What device memory holds cannot be checked on the host:
+ * lengths, page numbers and slots out of range never lead to an access out of bounds; what becomes of them is said below.
+ */
+enum {
+  RF2_DTYPE_BF16 = 0,
+  RF2_DTYPE_F16 = 1 /* IEEE binary16 */
+};
+
+/* What rf2_paged_append and rf2_paged_release leave in `status` (sums of): 0, done, or nothing has been changed. */
+enum {
+  RF2_PAGED_BAD_LENGTH = 1, /* a new length below 0, a cached length outside [0, max_pages * page], n_free outside [0, n_pages] */
+  RF2_PAGED_SEQ_FULL = 2,   /* a sequence longer than max_pages * page */
+  RF2_PAGED_TOKENS_FULL = 4, /* more new tokens than n_tokens */
+  RF2_PAGED_POOL_FULL = 8   /* more pages than are free; on release: more than n_pages would be */
+};
+
+typedef struct {
+  int32_t heads, kv_heads; /* query heads, K/V heads: heads a multiple of kv_heads (query head i reads K/V head
+                              i / (heads / kv_heads)), at most 512 */
+  int32_t head_dim;        /* in {64, 128} */
+  int32_t page;            /* tokens of a page, in {32, 64, 128, 256} */
+  int32_t n_pages;         /* pages of the pool; n_pages * page <= 2^30 */
+  int32_t max_seqs;        /* sequences of a call at most, <= 4096 */
+  int32_t max_pages;       /* pages of a sequence at most = row length of the block table; max_pages * page <= 2^24 */
+  int32_t max_tokens;      /* new tokens of a call at most, all sequences together, <= 2^20 */
+  int32_t dtype;           /* RF2_DTYPE_*: q, k, v, o and both caches */
+  int32_t causal;          /* 1: a token sees the tokens of its sequence up to itself; 0: all that are cached, its whole
+                              chunk among them (new frames of a video) */
+  float scale;             /* factor of q.k; 0 = 1/sqrt(head_dim); finite, >= 0 */
+} rf2_paged_config;
+
+typedef struct {
+  int64_t cache_elements;  /* of k_cache, and of v_cache: n_pages * kv_heads * page * head_dim */
+  int64_t workspace_bytes; /* what rf2_paged_attn needs at `workspace` */
+} rf2_paged_info;
+
+typedef struct rf2_paged_plan rf2_paged_plan; /* opaque */
+
+/* Host only; the plan belongs to the device that is current (without any: host-only, like rf2_plan_create). */
+int rf2_paged_plan_create(const rf2_paged_config* cfg, rf2_paged_plan** out);
+int rf2_paged_plan_destroy(rf2_paged_plan* plan);
+int rf2_paged_plan_info(const rf2_paged_plan* plan, rf2_paged_info* out);
+
+/*
+ * Pages and slots for the new tokens of sequences 0..n_seqs-1.  All or nothing: if status is not 0, lengths and n_free
+ * come out as they went in, the table stays as it is, cu_new is all 0 and slots all -1 (store and attention then do nothing).
+ *   seq_len    : [n_seqs] int32, tokens cached                                             (in)
+ *   new_len    : [n_seqs] int32, tokens to come, 0 or more                                 (in)
+ *   free_pages : [n_pages] int32, a stack of the pages that are free: the first n_free      (in)
+ *   n_free     : [1] int32                                                                 (in)
+ *   block_table: [n_seqs, max_pages] int32; the entries of new pages are written: sequence by sequence and, within one,
+ *                in order, pages are taken from the top of the stack down                  (in, out)
+ *   seq_len_out: [n_seqs] int32, seq_len + new_len; may be seq_len                         (out)
+ *   n_free_out : [1] int32, pages still free; may be n_free                                (out)
+ *   cu_new     : [n_seqs + 1] int32: the new tokens of sequence s are rows cu_new[s] to cu_new[s+1] - 1 of q, k, v, o (out)
+ *   slots      : [n_tokens] int32, slot of each new token; -1 behind the last, and where the table holds no page (out)
+ *   status     : [1] int32                                                                 (out)
+ * A call with other outputs than inputs can be taken back by dropping its outputs: the stack itself is not written.
+ * n_seqs = 0 and n_tokens = 0 are allowed; at most max_seqs and max_tokens.  No two of the arrays may overlap, apart from the
+ * two pairs named.
+ */
+int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens, const int32_t* seq_len,
+                     const int32_t* new_len, const int32_t* free_pages, const int32_t* n_free, int32_t* block_table,
+                     int32_t* seq_len_out, int32_t* n_free_out, int32_t* cu_new, int32_t* slots, int32_t* status,
+                     void* stream);
+
+/*
+ * Gives back the pages of the sequences s with done[s] != 0: the entries of the first ceil(seq_len[s] / page) columns of
+ * their rows that are pages (others are holes) go on top of the stack, in order of s and column.  All or nothing.
+ *   done       : [n_seqs] uint8                                                            (in)
+ *   seq_len, block_table, n_free : as above                                                (in)
+ *   free_pages : [n_pages] int32, written behind its first n_free entries                  (in, out)
+ *   seq_len_out: [n_seqs] int32, 0 where done, else seq_len; may be seq_len                (out)
+ *   n_free_out : [1] int32; may be n_free                                                  (out)
+ *   status     : [1] int32                                                                 (out)
+ */
+int rf2_paged_release(const rf2_paged_plan* plan, int32_t n_seqs, const uint8_t* done, const int32_t* seq_len,
+                      const int32_t* block_table, int32_t* free_pages, const int32_t* n_free, int32_t* seq_len_out,
+                      int32_t* n_free_out, int32_t* status, void* stream);
+
+/*
+ * Rows of K and V into the cache.
+ *   k, v    : [n_tokens, kv_heads, head_dim], rows k_stride and v_stride elements apart (multiples of 8, at least
+ *             kv_heads * head_dim): parts of a joint projection's output need no copy      (in)
+ *   slots   : [n_tokens] int32; a token whose slot is outside [0, n_pages * page) is left out (in)
+ *   k_cache : [n_pages, kv_heads, page/32, head_dim/8, 32, 8]: channel c of the key at slot P*page + r is element
+ *             (P, head, r / 32, c / 8, r % 32, c % 8)                                      (out)
+ *   v_cache : [n_pages, kv_heads, page/32, 4, head_dim, 8]: channel c of it is element
+ *             (P, head, r / 32, r % 32 / 16 * 2 + r % 8 / 4, c, r % 16 / 8 * 4 + r % 4): the operand order of
+ *             rf2_permute's vp, each group of 16 keys in the order 0-3, 8-11, 4-7, 12-15   (out)
+ *             Both are read by rf2_paged_attn as matrix-core operands, 1 KiB at a time.  What no slot names stays.
+ * If two tokens have the same slot, each element of it is one of theirs.
+ */
+int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k, int64_t k_stride, const void* v,
+                    int64_t v_stride, const int32_t* slots, void* k_cache, void* v_cache, void* stream);
+
+/*
+ * softmax(scale q K^T) V of the new tokens over the cache of their sequences, which holds their own rows already.
+ * fp32 accumulation; probabilities are rounded to dtype for the second product, as in rf2_block_sparse_attn.
+ *   q           : [n_tokens, heads, head_dim], rows q_stride elements apart (a multiple of 8, at least heads * head_dim) (in)
+ *   k_cache, v_cache : as written by rf2_paged_store                                       (in)
+ *   block_table, seq_len, cu_new : as left by rf2_paged_append (seq_len is its seq_len_out), or a program's own.  Token
+ *                 t of the n new ones of sequence s sees the keys j < seq_len[s] - n + t + 1 (causal) or j < seq_len[s].
+ *                 An entry of the table outside [0, n_pages) is a hole: its keys are left out (pages that were evicted).
+ *                 Lengths are clamped to [0, max_pages * page], rows to [0, n_tokens).     (in)
+ *   workspace   : rf2_paged_info.workspace_bytes, written and read by this call alone: calls that may run at the same time
+ *                 need one each                                                            (scratch)
+ *   o           : [n_tokens, heads, head_dim]; a token that sees no key gets zeros         (out)
+ *   lse         : optional [n_tokens, heads] fp32, natural-log sum-exp of the scaled logits, -inf where there is no key;
+ *                 may be NULL                                                              (out)
+ * Rows from cu_new[n_seqs] on are neither read nor written.  Memory of the cache behind a sequence's last token may
+ * hold anything, infinities and NaN included.  The same call gives the same bits each time; in a batch of other
+ * sequences a token's result may differ by fp32 rounding.
+ */
+int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens, const void* q, int64_t q_stride,
+                   const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* seq_len,
+                   const int32_t* cu_new, void* workspace, void* o, float* lse, void* stream);
 
 /*
  * Measurement aid, not part of the layer: the ceilings of the device the calling thread is on, so

@@ -1,0 +1,37 @@
+// Internal declarations of the paged cache (not installed).
+#pragma once
+#include <algorithm>
+
+#include "rf2_internal.h"
+
+struct rf2_paged_plan {
+  rf2_paged_config cfg;
+  rf2_paged_info info;
+  int device;
+  float scale_log2;  // scale * log2(e)
+};
+
+constexpr int RF2_PAGED_MAX_SEQS = 4096;
+
+// Attention launches are cut into parts (rf2_paged_attn.hip): as many as this are aimed at, in all K/V heads together.
+constexpr int RF2_PAGED_PARTS = 1024;
+// Query rows of a workgroup: few rows to a sequence, and many.
+constexpr int RF2_PAGED_ROWS_FEW = 32, RF2_PAGED_ROWS_MANY = 128;
+
+inline int rf2_paged_parts_per_head(int kv_heads) { return std::max(1, RF2_PAGED_PARTS / kv_heads); }
+
+// Bytes of the partial results of a launch: a sequence that is cut has fewer than twice as many parts as are aimed at
+// (rf2_paged_attn.hip), each of `rows` rows of head_dim sums and two numbers more.
+inline int64_t rf2_paged_workspace(const rf2_paged_config& c) {
+  return 2ll * rf2_paged_parts_per_head(c.kv_heads) * c.kv_heads * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4;
+}
+
+inline bool rf2_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+inline int rf2_check_paged_device(const rf2_paged_plan* plan) {
+  if (plan->device < 0) return rf2_note_hip_error(hipErrorNoDevice);
+  int current = -1;
+  const hipError_t e = hipGetDevice(&current);
+  if (e != hipSuccess) return rf2_note_hip_error(e);
+  return current == plan->device ? RF2_OK : RF2_ERR_INVALID_ARG;
+}

@@ -18,6 +18,8 @@ RF2_ERR_INVALID_ARG, RF2_ERR_UNSUPPORTED, RF2_ERR_ALLOC, RF2_ERR_HIP, RF2_ERR_TO
 RF2_BUDGET_GLOBAL, RF2_BUDGET_ROW_INCL_SINK, RF2_BUDGET_ROW_PLUS_SINK = 0, 1, 2
 RF2_LAYOUT_BHND, RF2_LAYOUT_BNHD = 0, 1
 RF2_SELECT_TOPN, RF2_SELECT_CDF = 0, 1
+RF2_DTYPE_BF16, RF2_DTYPE_F16 = 0, 1
+RF2_PAGED_BAD_LENGTH, RF2_PAGED_SEQ_FULL, RF2_PAGED_TOKENS_FULL, RF2_PAGED_POOL_FULL = 1, 2, 4, 8
 
 
 class rf2_config(C.Structure):
@@ -37,6 +39,15 @@ class rf2_info(C.Structure):
                 ("N_pad_k", C.c_int64)]
 
 
+class rf2_paged_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "kv_heads", "head_dim", "page", "n_pages", "max_seqs", "max_pages",
+                                         "max_tokens", "dtype", "causal")] + [("scale", C.c_float)]
+
+
+class rf2_paged_info(C.Structure):
+    _fields_ = [("cache_elements", C.c_int64), ("workspace_bytes", C.c_int64)]
+
+
 # symbol -> (restype, argtypes); also the list of exports the tests check
 SIGNATURES = {
     "rf2_plan_create": (C.c_int, [C.POINTER(rf2_config), C.POINTER(C.c_void_p)]),
@@ -48,6 +59,13 @@ SIGNATURES = {
     "rf2_block_sparse_attn": (C.c_int, [C.c_void_p] * 9),
     "rf2_block_sparse_attn_unpermuted": (C.c_int, [C.c_void_p] * 9),
     "rf2_unpermute": (C.c_int, [C.c_void_p] * 4),
+    "rf2_paged_plan_create": (C.c_int, [C.POINTER(rf2_paged_config), C.POINTER(C.c_void_p)]),
+    "rf2_paged_plan_destroy": (C.c_int, [C.c_void_p]),
+    "rf2_paged_plan_info": (C.c_int, [C.c_void_p, C.POINTER(rf2_paged_info)]),
+    "rf2_paged_append": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 11),
+    "rf2_paged_release": (C.c_int, [C.c_void_p, C.c_int32] + [C.c_void_p] * 9),
+    "rf2_paged_store": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 4),
+    "rf2_paged_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64] + [C.c_void_p] * 9),
     "rf2_measure_peaks": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_void_p]),
     "rf2_measure_sustained_mfma": (C.c_int, [C.c_double, C.POINTER(C.c_double), C.c_void_p]),
     "rf2_probe_xcd_mapping": (C.c_int, [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_void_p]),
@@ -228,3 +246,133 @@ class Plan:
                                    buf.get("lse"), stream)
         self.rf2_unpermute(buf["op"], buf["o"], stream)
         return buf["o"]
+
+
+def _arg(t, what, dtype, numel, device):
+    """Address of a contiguous tensor of `numel` elements of `dtype` on the plan's device."""
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: expected {numel} contiguous elements of {dtype} on device {device}, got "
+                         f"{tuple(t.shape)} of {t.dtype} on {t.device}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _rows(t, what, dtype, shape, device):
+    """Address of a [tokens, heads, head_dim] tensor whose rows may be further apart than they are long, and how far."""
+    tokens, heads, dim = t.shape if t.dim() == 3 else (0, 0, 0)
+    stride = t.stride()
+    if (t.dim() != 3 or (tokens, heads, dim) != shape or t.dtype is not dtype or t.get_device() != device
+            or (tokens > 0 and (stride[2] != 1 or (heads > 1 and stride[1] != dim)))):
+        raise ValueError(f"{what}: expected {shape} of {dtype} on device {device}, heads and channels dense, got "
+                         f"{tuple(t.shape)} of {t.dtype} on {t.device}, strides {stride}")
+    return t.data_ptr(), stride[0] if tokens > 1 else heads * dim
+
+
+class PagedPlan:
+    """Owner of an rf2_paged_plan*: a paged cache of keys and values and the attention of new tokens over it.
+
+    The caller owns every tensor; `alloc` makes those that live as long as the cache, `alloc_step` those of a step.  A step:
+
+        plan.rf2_paged_append(seq_len, new_len, free_pages, n_free, block_table, seq_len, n_free, cu_new, slots, status)
+        for every layer:
+            plan.rf2_paged_store(k, v, slots, k_cache, v_cache)
+            plan.rf2_paged_attn(q, k_cache, v_cache, block_table, seq_len, cu_new, workspace, o)
+
+    n_seqs is the length of new_len (or done, or seq_len), n_tokens that of slots (or q): both may change from call to
+    call up to max_seqs and max_tokens, and rows behind the last new token are padding.
+    """
+
+    def __init__(self, *, heads, kv_heads, head_dim, page, n_pages, max_seqs, max_pages, max_tokens, dtype=torch.bfloat16,
+                 causal=True, scale=None):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"dtype: expected torch.bfloat16 or torch.float16, got {dtype}")
+        self.dtype = dtype
+        self.cfg = rf2_paged_config(heads, kv_heads, head_dim, page, n_pages, max_seqs, max_pages, max_tokens,
+                                    RF2_DTYPE_F16 if dtype is torch.float16 else RF2_DTYPE_BF16, int(causal),
+                                    0.0 if scale is None else float(scale))
+        self._h = C.c_void_p(0)
+        _check(lib().rf2_paged_plan_create(C.byref(self.cfg), C.byref(self._h)), "rf2_paged_plan_create")
+        self.info = rf2_paged_info()
+        _check(lib().rf2_paged_plan_info(self._h, C.byref(self.info)), "rf2_paged_plan_info")
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+
+    def close(self):
+        if self._h:
+            lib().rf2_paged_plan_destroy(self._h)
+            self._h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- buffers (allocation and the state of an empty cache) ---------------------------------
+    def alloc(self, device="cuda"):
+        """The cache of one layer and the tables, empty: every page on the stack, page 0 on top.  (Further layers need
+        a k_cache and a v_cache each; tables, lengths and the stack are shared by all.)"""
+        c = self.cfg
+        ints = dict(dtype=torch.int32, device=device)
+        tiles = (c.n_pages, c.kv_heads, c.page // 32)
+        return dict(
+            k_cache=torch.empty(*tiles, c.head_dim // 8, 32, 8, dtype=self.dtype, device=device),
+            v_cache=torch.empty(*tiles, 4, c.head_dim, 8, dtype=self.dtype, device=device),
+            block_table=torch.full((c.max_seqs, c.max_pages), -1, **ints),
+            seq_len=torch.zeros(c.max_seqs, **ints),
+            free_pages=torch.arange(c.n_pages - 1, -1, -1, **ints),
+            n_free=torch.full((1,), c.n_pages, **ints),
+            status=torch.zeros(1, **ints),
+            workspace=self.alloc_workspace(device))
+
+    def alloc_workspace(self, device="cuda"):
+        return torch.empty(self.info.workspace_bytes, dtype=torch.uint8, device=device)
+
+    def alloc_step(self, n_seqs, n_tokens, device="cuda"):
+        c = self.cfg
+        return dict(cu_new=torch.empty(n_seqs + 1, dtype=torch.int32, device=device),
+                    slots=torch.empty(n_tokens, dtype=torch.int32, device=device),
+                    o=torch.empty(n_tokens, c.heads, c.head_dim, dtype=self.dtype, device=device))
+
+    # -- the calls -----------------------------------------------------------------------------
+    def rf2_paged_append(self, seq_len, new_len, free_pages, n_free, block_table, seq_len_out, n_free_out, cu_new, slots, status,
+                         stream=None):
+        c, dev, i32 = self.cfg, self.device, torch.int32
+        n_seqs, n_tokens = new_len.numel(), slots.numel()
+        _check(lib().rf2_paged_append(
+            self._h, n_seqs, n_tokens, _arg(seq_len, "seq_len", i32, n_seqs, dev), _arg(new_len, "new_len", i32, n_seqs, dev),
+            _arg(free_pages, "free_pages", i32, c.n_pages, dev), _arg(n_free, "n_free", i32, 1, dev),
+            _arg(block_table, "block_table", i32, n_seqs * c.max_pages, dev),
+            _arg(seq_len_out, "seq_len_out", i32, n_seqs, dev), _arg(n_free_out, "n_free_out", i32, 1, dev),
+            _arg(cu_new, "cu_new", i32, n_seqs + 1, dev), _arg(slots, "slots", i32, n_tokens, dev),
+            _arg(status, "status", i32, 1, dev), _stream(stream)), "rf2_paged_append")
+
+    def rf2_paged_release(self, done, seq_len, block_table, free_pages, n_free, seq_len_out, n_free_out, status, stream=None):
+        c, dev, i32 = self.cfg, self.device, torch.int32
+        n_seqs = done.numel()
+        _check(lib().rf2_paged_release(
+            self._h, n_seqs, _arg(done, "done", torch.bool if done.dtype is torch.bool else torch.uint8, n_seqs, dev),
+            _arg(seq_len, "seq_len", i32, n_seqs, dev), _arg(block_table, "block_table", i32, n_seqs * c.max_pages, dev),
+            _arg(free_pages, "free_pages", i32, c.n_pages, dev), _arg(n_free, "n_free", i32, 1, dev),
+            _arg(seq_len_out, "seq_len_out", i32, n_seqs, dev), _arg(n_free_out, "n_free_out", i32, 1, dev),
+            _arg(status, "status", i32, 1, dev), _stream(stream)), "rf2_paged_release")
+
+    def rf2_paged_store(self, k, v, slots, k_cache, v_cache, stream=None):
+        c, dev, size = self.cfg, self.device, self.info.cache_elements
+        n_tokens = slots.numel()
+        shape = (n_tokens, c.kv_heads, c.head_dim)
+        _check(lib().rf2_paged_store(
+            self._h, n_tokens, *_rows(k, "k", self.dtype, shape, dev), *_rows(v, "v", self.dtype, shape, dev),
+            _arg(slots, "slots", torch.int32, n_tokens, dev), _arg(k_cache, "k_cache", self.dtype, size, dev),
+            _arg(v_cache, "v_cache", self.dtype, size, dev), _stream(stream)), "rf2_paged_store")
+
+    def rf2_paged_attn(self, q, k_cache, v_cache, block_table, seq_len, cu_new, workspace, o, lse=None, stream=None):
+        c, dev, size, i32 = self.cfg, self.device, self.info.cache_elements, torch.int32
+        n_seqs, n_tokens = seq_len.numel(), q.shape[0]
+        _check(lib().rf2_paged_attn(
+            self._h, n_seqs, n_tokens, *_rows(q, "q", self.dtype, (n_tokens, c.heads, c.head_dim), dev),
+            _arg(k_cache, "k_cache", self.dtype, size, dev), _arg(v_cache, "v_cache", self.dtype, size, dev),
+            _arg(block_table, "block_table", i32, n_seqs * c.max_pages, dev), _arg(seq_len, "seq_len", i32, n_seqs, dev),
+            _arg(cu_new, "cu_new", i32, n_seqs + 1, dev),
+            _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, dev),
+            _arg(o, "o", self.dtype, n_tokens * c.heads * c.head_dim, dev),
+            None if lse is None else _arg(lse, "lse", torch.float32, n_tokens * c.heads, dev), _stream(stream)),
+            "rf2_paged_attn")
