@@ -40,6 +40,8 @@ struct Bf16 {
   // P = exp2(x - m): bf16 and fp32 carry 2^40 as well as 1
   static constexpr float RANGE = 1.0995e12f, HEAD = 0.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
+  static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
 };
 struct F16 {
   typedef f16x8 x8;
@@ -50,6 +52,8 @@ struct F16 {
   // 2^15, and what is rounded away below 2^-25 is 2^-33 of it
   static constexpr float RANGE = 32768.f, HEAD = 8.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
+  static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
 };
 
 struct Args {
@@ -71,6 +75,8 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int s) {
   const int first = min(max(a.cu_new[s], 0), a.n_tokens), end = min(max(a.cu_new[s + 1], first), a.n_tokens);
   return {first, end - first, min(max(a.seq_len[s], 0), a.max_pages << (a.unit_shift + 5))};
 }
+// A value that is the same in every lane, which the compiler cannot always see (it then lives in a scalar register).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int units_of(int keys) { return max((keys + 31) >> 5, 1); }
 
 // What a workgroup works on: a part of a tile of rows.
@@ -127,8 +133,8 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum <= at);
     if (past != ~0ull) {                             // (a lane's sum only grows: the first lane that is beyond)
       const int l = __builtin_ctzll(~past);
-      const auto pick = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-      const auto pick64 = [&](int64_t x) { return (int64_t)((uint64_t)(uint32_t)pick((int)(x >> 32)) << 32 | (uint32_t)pick((int)x)); };
+      const auto pick = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, l); };
+      const auto pick64 = [&](int64_t x) __attribute__((always_inline)) { return (int64_t)((uint64_t)(uint32_t)pick((int)(x >> 32)) << 32 | (uint32_t)pick((int)x)); };
       w.seq = s0 + l;
       w.s = {pick(s.first), pick(s.n_new), pick(s.len)};
       w.tiles = pick(tiles);
@@ -165,44 +171,13 @@ __device__ __forceinline__ const unsigned char* uniform_ptr(const void* p) {
   return (const unsigned char*)(((uint64_t)hi << 32) | lo);
 }
 
-// The units of a wavefront that lie in pages, in order.  64 entries of the table are held, one to a lane, and 64 more are on
-// their way.
-struct Pages {
-  const int32_t* row;
-  int end, shift, n_pages, last;      // last: of the row
-  int base, ids, next_ids;
-  uint64_t there;
-  __device__ __forceinline__ int load(int from) const { return row[min(from + ((int)threadIdx.x & 63), last)]; }
-  __device__ __forceinline__ void begin(int u) {
-    base = u >> shift;
-    ids = load(base);
-    next_ids = load(base + 64);
-    there = __builtin_amdgcn_ballot_w64((unsigned)ids < (unsigned)n_pages);
-  }
-  // The first unit at or after u that lies in a page, or `end`.
-  __device__ __forceinline__ int seek(int u) {
-    while (u < end) {
-      const int at = (u >> shift) - base;
-      if (at >= 64) {
-        base += 64;
-        ids = next_ids;
-        next_ids = load(base + 64);
-        there = __builtin_amdgcn_ballot_w64((unsigned)ids < (unsigned)n_pages);
-        continue;
-      }
-      const uint64_t rest = there >> at;
-      if (rest & 1) return u;
-      u = (base + (rest == 0 ? 64 : at + __builtin_ctzll(rest))) << shift;
-    }
-    return end;
-  }
-  __device__ __forceinline__ int page(int u) const { return __builtin_amdgcn_readlane(ids, (u >> shift) - base); }
-};
+__device__ __attribute__((aligned(16))) const unsigned char zeros[8192] = {};      // a tile
 
 // QT: tiles of 32 rows to a wavefront; RW wavefronts with rows of their own, times KW that share a part's keys.
 template <class T, int D, int QT, int RW, int KW>
 __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kernel(Args a) {
   constexpr int DS = D / 16, DT = D / 32, ROWS = 32 * QT * RW;
+  constexpr int WINDOW = KW > 1 ? 256 : 512;      // columns of the table that a wavefront has listed at a time
   typedef typename T::x8 x8;
   Part w;
   if (!find_part<ROWS, false>(a, blockIdx.x, w)) return;
@@ -217,19 +192,16 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
   const int last_row = min(row0 + 32 * QT, n_rows) - 1;
   const int most = (limit_of(a, w.s, last_row) + 31) >> 5;    // units that a row of this wavefront sees
   const int share = (min(u0 + w.units, all) - u0 + KW - 1) / KW;
-  const int begin = u0 + kw * share, end = min(min(begin + share, most), min(u0 + w.units, all));
-  const int free_units = limit_of(a, w.s, row0) >> 5;         // units that every row sees whole
+  const int begin = uniform(u0 + kw * share), end = uniform(min(min(begin + share, most), min(u0 + w.units, all)));
+  const int free_units = uniform(limit_of(a, w.s, row0) >> 5);         // units that every row sees whole
+  const int kv_head = uniform(w.head);
 
   // this lane's rows: query column l32 of each tile (rows past the last stand for the last and are not written)
-  int row[QT], limit[QT];
-  int64_t out_row[QT];
+  auto row_of = [&](int q) __attribute__((always_inline)) { return row0 + 32 * q + l32; };
   x8 qf[QT][DS];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    row[q] = row0 + 32 * q + l32;
-    const int r = min(row[q], n_rows - 1), t = r / a.group, head = w.head * a.group + r % a.group;
-    limit[q] = limit_of(a, w.s, r);
-    out_row[q] = (int64_t)(w.s.first + t) * a.heads + head;
+    const int r = min(row_of(q), n_rows - 1), t = r / a.group, head = kv_head * a.group + r % a.group;
     const typename T::x1* const from = (const typename T::x1*)a.q + (w.s.first + t) * a.q_stride + head * D + 8 * lh;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) qf[q][ds] = *reinterpret_cast<const x8*>(from + 16 * ds);
@@ -247,115 +219,341 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
       for (int i = 0; i < 16; ++i) o[q][dt][i] = 0.f;
   }
 
-  Pages pages{a.table + (int64_t)w.seq * a.max_pages, end, a.unit_shift, a.n_pages, a.max_pages - 1};
+  // Rows of a unit that a row does not see.
+  auto mask = [&](f32x16& S, int q, int u) __attribute__((always_inline)) {
+    const int left = limit_of(a, w.s, min(row_of(q), n_rows - 1)) - 32 * u - 4 * lh;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (8 * (i / 4) + i % 4 >= left) S[i] = -INFINITY;
+  };
+  // V behind the last token: 0 times whatever is there has to be 0.  (The last unit of a sequence alone can have such keys.)
+  auto clear_v = [&](x8 (&v)[2 * DT], int u) __attribute__((always_inline)) {
+    if (32 * u + 32 <= w.s.len) return;
+#pragma unroll
+    for (int j = 0; j < 2 * DT; ++j) {
+      const int left = w.s.len - 32 * u - 16 * (j % 2) - 4 * lh;
+      u32x4 x = __builtin_bit_cast(u32x4, v[j]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = e / 2 * 8 + e % 2 * 2;
+        x[e] &= (key < left ? 0xffffu : 0u) | (key + 1 < left ? 0xffff0000u : 0u);
+      }
+      v[j] = __builtin_bit_cast(x8, x);
+    }
+  };
+  auto tile_at = [&](int u, int page) __attribute__((always_inline)) {      // byte offset of a unit's tile in either cache
+    return (((int64_t)page * a.kv_heads + kv_head) * (1 << a.unit_shift) + (u & ((1 << a.unit_shift) - 1))) * (32 * D * 2);
+  };
+  // Operands of a tile: buffer loads, the tile's address in scalar registers, a constant offset of the lane, and nothing past the tile.
+  constexpr unsigned TILE = 32 * D * 2;
   const uint32_t k_lane = (uint32_t)lane * 16, v_lane = (uint32_t)(lh * D + l32) * 16;
-  x8 kr[2][DS], vr[2 * DT];
-  auto tile_at = [&](const void* cache, int u, int page) {
-    const int64_t tile = ((int64_t)page * a.kv_heads + w.head) * (1 << a.unit_shift) + (u & ((1 << a.unit_shift) - 1));
-    return uniform_ptr((const unsigned char*)cache + tile * (32 * D * 2));
+  auto buffer = [](const unsigned char* tile) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)uniform_ptr(tile), 0, TILE, 0x00020000);
   };
-  auto load = [&](auto odd, int u, int page) {
-    const unsigned char* const kb = tile_at(a.k_cache, u, page);
-#pragma unroll
-    for (int c = 0; c < DS; ++c) kr[decltype(odd)::value][c] = *reinterpret_cast<const x8*>(kb + c * 1024 + k_lane);
+  auto k_load = [&](auto tile, int c) __attribute__((always_inline)) {
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + c % 4 * 1024, c / 4 * 4096, 0));
   };
-  auto load_v = [&](int u, int page) {
-    const unsigned char* const vb = tile_at(a.v_cache, u, page);
-#pragma unroll
-    for (int j = 0; j < 2 * DT; ++j) vr[j] = *reinterpret_cast<const x8*>(vb + j % 2 * (2 * D * 16) + j / 2 * 512 + v_lane);
+  auto v_load = [&](auto tile, int j) __attribute__((always_inline)) {
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + j / 2 * 512, j % 2 * (2 * D * 16), 0));
   };
-  // Unit u, whose operands are in registers B.
-  auto unit = [&](auto odd, int u) {
-    constexpr int B = decltype(odd)::value;
-    f32x16 S[QT];
+  auto operand_p = [](const uint32_t (&P)[8], int ks) __attribute__((always_inline)) {
+    const u32x4 x = {P[4 * ks], P[4 * ks + 1], P[4 * ks + 2], P[4 * ks + 3]};
+    return __builtin_bit_cast(x8, x);
+  };
+  // The reference of tile q moves to the largest exponent of S, if that is larger; what has been summed is rescaled.
+  auto move_reference = [&](int q, const f32x16& S) __attribute__((always_inline)) {
+    float top = S[0];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, S[i]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2 - T::HEAD, -FLT_MAX);
+    const float to = fmaxf(m[q], top), alpha = __builtin_amdgcn_exp2f(m[q] - to);
+    m[q] = to;
+    return alpha;
+  };
+  auto probabilities = [&](int q, const f32x16& S, uint32_t (&P)[8]) __attribute__((always_inline)) {
+    float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[q][i] = 0.f;
-#pragma unroll
-      for (int ds = 0; ds < DS; ++ds) S[q] = T::mfma(kr[B][ds], qf[q][ds], S[q]);
+    for (int i = 0; i < 16; i += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, -m[q])), p1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], a.scale_log2, -m[q]));
+      const typename T::x2 pk = {(typename T::x1)p0, (typename T::x1)p1};
+      sum += p0 + p1;
+      P[i / 2] = __builtin_bit_cast(uint32_t, pk);
     }
-    if (u >= free_units) {                                   // keys that a row does not see
+    return sum;
+  };
+  // Pages of the columns p to p1 - 1 of the table that exist, in order, with their columns; a wavefront's own list.  Unit x of the
+  // list is unit x % 2^unit_shift of page x / 2^unit_shift; units x0 to x1 - 1 are those from `begin` on and before `stop`.
+  const int32_t* const table = a.table + (int64_t)uniform(w.seq) * a.max_pages;
+  __shared__ int2 page_lists[RW * KW][WINDOW];
+  int2* const pages = page_lists[wave];
+  auto list_pages = [&](int p, int p1, int from, int stop, int& x0, int& x1) __attribute__((always_inline)) {
+    int ids[WINDOW / 64], n = 0;
 #pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        const int left = limit[q] - 32 * u - 4 * lh;
+    for (int i = 0; i < WINDOW / 64; ++i) ids[i] = table[min(p + 64 * i + lane, a.max_pages - 1)];
+    wave_fence();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (8 * (i / 4) + i % 4 >= left) S[q][i] = -INFINITY;
-      }
+    for (int i = 0; i < WINDOW / 64; ++i) {
+      const bool there = p + 64 * i + lane < p1 && (unsigned)ids[i] < (unsigned)a.n_pages;
+      const uint64_t some = __builtin_amdgcn_ballot_w64(there);
+      if (there) pages[n + __popcll(some & ((1ull << lane) - 1))] = make_int2(ids[i], p + 64 * i + lane);
+      n += __popcll(some);
     }
-    if (32 * u + 32 > w.s.len) {                             // V behind the last token: 0 times whatever is there has to be 0
+    wave_fence();
+    const int per = 1 << a.unit_shift;
+    x0 = n > 0 && uniform(pages[0].y) == from >> a.unit_shift ? from & (per - 1) : 0;
+    x1 = n * per;
+    if (n > 0 && uniform(pages[n - 1].y) == (stop - 1) >> a.unit_shift) x1 -= per - 1 - ((stop - 1) & (per - 1));
+  };
+  if constexpr (QT == 2) {
+    constexpr int NQ = DS, NP = 2 * DT, PAIRS = 16 / (NQ + NP);
+    x8 kr[2][NQ], vr[2][NP];
+    float last[2] = {};                      // sums of the latest unit, still to be added to l
+    // O of tile q times alpha.  In accumulation registers it is scaled where it is, through one vector register (left to the
+    // compiler, the copies cost the registers of the loop); the wait states cover a product in flight and one that follows.
+    auto rescale = [&](int q, float alpha) __attribute__((always_inline)) {
+      asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < 2 * DT; ++j) {
-        const int left = w.s.len - 32 * u - 16 * (j % 2) - 4 * lh;
-        u32x4 x = __builtin_bit_cast(u32x4, vr[j]);
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = e / 2 * 8 + e % 2 * 2;
-          x[e] &= (key < left ? 0xffffu : 0u) | (key + 1 < left ? 0xffff0000u : 0u);
+        for (int i = 0; i < 16; ++i) {
+          float x = o[q][dt][i], t;
+          asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                       : "+a"(x), "=&v"(t) : "v"(alpha));
+          o[q][dt][i] = x;
         }
-        vr[j] = __builtin_bit_cast(x8, x);
-      }
-    }
+      asm volatile("s_nop 7" ::: "memory");
+    };
+    // Step: S of the next unit, O += V P of the one before, the softmax arithmetic of the present one, operand by operand.  The
+    // operands' registers are loaded again as soon as both MFMAs that read them are issued: K at k_at, V at v_at.
+    auto step = [&](auto odd, f32x16 (&Scur)[2], f32x16 (&Snext)[2], uint32_t (&Pprev)[2][8], uint32_t (&Pcur)[2][8], const unsigned char* k_at, const unsigned char* v_at,
+                    int u_next) __attribute__((always_inline)) {
+      constexpr int B = decltype(odd)::value;
+      const auto kb = buffer(k_at), vb = buffer(v_at);
+      __builtin_amdgcn_sched_barrier(0);
+      float rs[2] = {}, e0[PAIRS], e1[PAIRS];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-      uint32_t P[8];
-      float sum;
-      auto probabilities = [&] {
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(S[q][i], a.scale_log2, -m[q]));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(S[q][i + 1], a.scale_log2, -m[q]));
-          const typename T::x2 pk = {(typename T::x1)p0, (typename T::x1)p1};
-          sum += p0 + p1;
-          P[i / 2] = __builtin_bit_cast(uint32_t, pk);
+      for (int g = 0; g < NQ + NP; ++g) {
+        const int j = g - NQ;
+        if (g % 2 == 0) {                    // (one wait for two operands)
+          if (g < NQ) asm volatile("" ::"v"(kr[B][g + 1]));
+          else asm volatile("" ::"v"(vr[B][j + 1]));
         }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (g < NQ) {
+            if (g == 0) T::first(Snext[q], kr[B][g], qf[q][g]);
+            else T::more(Snext[q], kr[B][g], qf[q][g]);
+          } else {
+            o[q][j / 2] = T::mfma(vr[B][j], operand_p(Pprev[q], j % 2), o[q][j / 2]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          if (q == 0) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) {
+              const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
+              e0[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i], a.scale_log2, -m[tile]));
+              e1[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i + 1], a.scale_log2, -m[tile]));
+              asm volatile("" : "+v"(e0[p]), "+v"(e1[p]));
+            }
+          } else {
+            if (g < NQ) kr[B][g] = k_load(kb, g);
+            else vr[B][j] = v_load(vb, j);
+            asm volatile("" ::: "memory");   // (the load stays here)
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) {
+              const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
+              const typename T::x2 pk = {(typename T::x1)e0[p], (typename T::x1)e1[p]};
+              uint32_t word = __builtin_bit_cast(uint32_t, pk);
+              rs[tile] = i == 0 ? e0[p] + e1[p] : rs[tile] + (e0[p] + e1[p]);
+              asm volatile("" : "+v"(word), "+v"(rs[tile]));
+              Pcur[tile][i / 2] = word;
+              if (i == 0) {
+                l[tile] += last[tile];
+                asm volatile("" : "+v"(l[tile]));
+              }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      last[0] = rs[0];
+      last[1] = rs[1];
+      // One branch, hardly ever taken: the present unit is out of range, or rows do not see all of the next one.
+      // (the limit is an integer select: as a float one it would be two branches, and the step twice)
+      int bound = u_next >= free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
+      asm volatile("" : "+s"(bound));
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
+        if (__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= T::RANGE)) != 0ull)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float alpha = move_reference(q, Scur[q]);
+            l[q] *= alpha;
+            rescale(q, alpha);
+            last[q] = probabilities(q, Scur[q], Pcur[q]);
+          }
+        if (u_next >= free_units) mask(Snext[0], 0, u_next), mask(Snext[1], 1, u_next);
+      }
+    };
+    // Units x0 to x1 - 1 of the list (behind unit `lead` of page `lead_page`, where there is one).
+    auto walk = [&](int x0, int x1, int lead, int lead_page, bool begins) __attribute__((always_inline)) {
+      // units s to s + 3 and their tiles; past the last one: none, in a tile of zeros
+      constexpr int NONE = 1 << 25;
+      int us[4], x = x0;
+      const unsigned char *k_at[4], *v_at[4];
+      auto fetch = [&](int i, int u, int page) __attribute__((always_inline)) {
+        const int64_t at = tile_at(u, page);
+        us[i] = u;
+        k_at[i] = (const unsigned char*)a.k_cache + at;
+        v_at[i] = (const unsigned char*)a.v_cache + at;
       };
-      probabilities();
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= T::RANGE)) != 0ull, 0)) {
-        // Out of range, or the first unit with a key: the reference moves to the largest exponent, what is there is rescaled.
-        float top = S[q][0];
+      int2 entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];       // of unit x, read a step before it is turned into addresses
+      auto following = [&](int i) __attribute__((always_inline)) {
+        const int page = uniform(entry.x), u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
+        const int64_t at = tile_at(u, page);
+        const bool there = x < x1;
+        us[i] = there ? u : NONE;
+        k_at[i] = there ? (const unsigned char*)a.k_cache + at : zeros;
+        v_at[i] = there ? (const unsigned char*)a.v_cache + at : zeros;
+        ++x;
+        entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];
+      };
+      auto shift = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, S[q][i]);
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2 - T::HEAD, -FLT_MAX);
-        const float to = fmaxf(m[q], top), alpha = __builtin_amdgcn_exp2f(m[q] - to);
-        m[q] = to;
-        l[q] *= alpha;
+        for (int i = 0; i < 3; ++i) us[i] = us[i + 1], k_at[i] = k_at[i + 1], v_at[i] = v_at[i + 1];
+      };
+      if (lead >= 0) fetch(0, lead, lead_page);
+      else following(0);
+      following(1);
+      following(2);
+      x8 k0[NQ];
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) k0[c] = k_load(buffer(k_at[0]), c);
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) kr[0][c] = k_load(buffer(k_at[1]), c);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) kr[1][c] = k_load(buffer(k_at[2]), c);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        vr[1][j] = v_load(buffer(v_at[0]), j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vr[0][j][e] = (typename T::x1)0.f;     // step 0 has no unit before it: it adds 0 x 0
+      }
+      f32x16 Sa[2], Sb[2];
+      uint32_t Pa[2][8], Pb[2][8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) {
+          if (ds == 0) T::first(Sa[q], k0[ds], qf[q][ds]);
+          else T::more(Sa[q], k0[ds], qf[q][ds]);
+        }
+        asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(Sa[q]));
+        if (us[0] >= free_units) mask(Sa[q], q, us[0]);
+        if (begins) (void)move_reference(q, Sa[q]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) Pb[q][e] = 0u;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) Sb[q][i] = 0.f;
+      }
+      if (lead >= 0) clear_v(vr[1], lead);
+      // (arrived before the loop, whose waits would else be those of its first round)
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) asm volatile("" : "+v"(kr[0][c]));
+      // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
+      do {
+        following(3);
+        step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_at[3], v_at[1], us[1]);
+        shift();
+        following(3);
+        step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_at[3], v_at[1], us[1]);
+        shift();
+      } while (us[0] != NONE);
+      // last product
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        l[q] += last[q];
+        last[q] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NP; ++j) o[q][j / 2] = T::mfma(vr[0][j], operand_p(Pb[q], j % 2), o[q][j / 2]);
+      }
+    };
+    // The last unit of a sequence can have keys behind its last token, whose V has to be cleared: it goes first, so that no step
+    // has to look for it.
+    int stop = end, lead = -1, lead_page = 0;
+    if (begin < end && 32 * end > w.s.len) {
+      stop = end - 1;
+      lead_page = uniform(table[stop >> a.unit_shift]);
+      lead = (unsigned)lead_page < (unsigned)a.n_pages ? stop : -1;
+    }
+    bool begins = true;
+    for (int p = begin >> a.unit_shift, p1 = (stop + (1 << a.unit_shift) - 1) >> a.unit_shift; p < p1 || lead >= 0; p += WINDOW) {
+      int x0, x1;
+      list_pages(p, min(p + WINDOW, p1), begin, stop, x0, x1);
+      if (x0 < x1 || lead >= 0) {
+        walk(x0, x1, lead, lead_page, begins);
+        begins = false;
+        lead = -1;
+      }
+    }
+  } else {
+    x8 kr[2][DS], vr[2 * DT];
+    auto load = [&](auto odd, int x, int& u) __attribute__((always_inline)) {
+      const int2 entry = pages[x >> a.unit_shift];
+      u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
+      const int64_t at = tile_at(u, uniform(entry.x));
+      const auto kb = buffer((const unsigned char*)a.k_cache + at);
+#pragma unroll
+      for (int c = 0; c < DS; ++c) kr[decltype(odd)::value][c] = k_load(kb, c);
+      return (const unsigned char*)a.v_cache + at;
+    };
+    auto load_v = [&](const unsigned char* at) __attribute__((always_inline)) {
+      const auto vb = buffer(at);
+#pragma unroll
+      for (int j = 0; j < 2 * DT; ++j) vr[j] = v_load(vb, j);
+    };
+    // Unit u, whose K is in registers B.
+    auto unit = [&](auto odd, int u) __attribute__((always_inline)) {
+      constexpr int B = decltype(odd)::value;
+      f32x16 S;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) S = T::mfma(kr[B][ds], qf[0][ds], S);
+      if (u >= free_units) mask(S, 0, u);
+      clear_v(vr, u);
+      uint32_t P[8];
+      float sum = probabilities(0, S, P);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= T::RANGE)) != 0ull, 0)) {
+        const float alpha = move_reference(0, S);
+        l[0] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[q][dt][i] *= alpha;
-        probabilities();
+          for (int i = 0; i < 16; ++i) o[0][dt][i] *= alpha;
+        sum = probabilities(0, S, P);
       }
-      l[q] += sum;
+      l[0] += sum;
 #pragma unroll
-      for (int j = 0; j < 2 * DT; ++j) {
-        const u32x4 p = {P[4 * (j % 2)], P[4 * (j % 2) + 1], P[4 * (j % 2) + 2], P[4 * (j % 2) + 3]};
-        o[q][j / 2] = T::mfma(vr[j], __builtin_bit_cast(x8, p), o[q][j / 2]);
-      }
-    }
-  };
-  if (begin < end) {
-    pages.begin(begin);
-    int u = pages.seek(begin);
-    if (u < end) {
-      int page = pages.page(u);
-      load(std::integral_constant<int, 0>{}, u, page);
+      for (int j = 0; j < 2 * DT; ++j) o[0][j / 2] = T::mfma(vr[j], operand_p(P, j % 2), o[0][j / 2]);
+    };
+    for (int p = begin >> a.unit_shift, p1 = (end + (1 << a.unit_shift) - 1) >> a.unit_shift; begin < end && p < p1; p += WINDOW) {
+      int x, x1, ua, ub;
+      list_pages(p, min(p + WINDOW, p1), begin, end, x, x1);
+      if (x >= x1) continue;
+      const unsigned char* va = load(std::integral_constant<int, 0>{}, x, ua);
+      // (past the last unit it is fetched again: no branch stands between a load and its use)
       while (true) {
-        // (past the last unit it is fetched again: no branch stands between a load and its use)
-        const int u1 = pages.seek(u + 1), page1 = u1 < end ? pages.page(u1) : page;
-        load_v(u, page);
-        load(std::integral_constant<int, 1>{}, u1 < end ? u1 : u, page1);
-        unit(std::integral_constant<int, 0>{}, u);
-        if (u1 >= end) break;
-        u = pages.seek(u1 + 1);
-        page = u < end ? pages.page(u) : page1;
-        load_v(u1, page1);
-        load(std::integral_constant<int, 0>{}, u < end ? u : u1, page);
-        unit(std::integral_constant<int, 1>{}, u1);
-        if (u >= end) break;
+        load_v(va);
+        const unsigned char* const vb = load(std::integral_constant<int, 1>{}, min(x + 1, x1 - 1), ub);
+        unit(std::integral_constant<int, 0>{}, ua);
+        if (++x >= x1) break;
+        load_v(vb);
+        va = load(std::integral_constant<int, 0>{}, min(x + 1, x1 - 1), ua);
+        unit(std::integral_constant<int, 1>{}, ub);
+        if (++x >= x1) break;
       }
     }
   }
@@ -411,9 +609,10 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
   const int64_t place = w.place + ((int64_t)w.head * w.chunks + w.chunk) * w.tiles + w.tile;
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    if (row[q] >= n_rows) continue;
+    const int r = row_of(q) - w.tile * ROWS;
+    if (row_of(q) >= n_rows) continue;
+    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + kv_head * a.group + row_of(q) % a.group;
     const float f = whole ? (l[q] > 0.f ? 1.0f / l[q] : (l[q] == 0.f ? 0.f : l[q])) : 1.0f;     // a row that sees no key yields zeros
-    const int r = row[q] - w.tile * ROWS;
     float* const part = a.parts + place * (ROWS * (D + 2));
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -425,7 +624,7 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
           typename T::x4 pk;
 #pragma unroll
           for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(o[q][dt][4 * g + e] * f);
-          *reinterpret_cast<typename T::x4*>((typename T::x1*)a.o + out_row[q] * D + ch) = pk;
+          *reinterpret_cast<typename T::x4*>((typename T::x1*)a.o + out_row * D + ch) = pk;
         } else {
           *reinterpret_cast<float4*>(part + r * D + ch) = make_float4(o[q][dt][4 * g], o[q][dt][4 * g + 1], o[q][dt][4 * g + 2], o[q][dt][4 * g + 3]);
         }
@@ -433,7 +632,7 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
     }
     if (lh == 0 && kw == 0) {
       if (!whole) *reinterpret_cast<float2*>(part + ROWS * D + 2 * r) = make_float2(m[q], l[q]);
-      else if (a.lse != nullptr) a.lse[out_row[q]] = (m[q] + __log2f(l[q])) * 0.6931471805599453f;
+      else if (a.lse != nullptr) a.lse[out_row] = (m[q] + __log2f(l[q])) * 0.6931471805599453f;
     }
   }
 }
