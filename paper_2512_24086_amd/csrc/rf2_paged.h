@@ -20,10 +20,12 @@ constexpr int RF2_PAGED_ROWS_FEW = 32, RF2_PAGED_ROWS_MANY = 128;
 
 inline int rf2_paged_parts_per_head(int kv_heads) { return std::max(1, RF2_PAGED_PARTS / kv_heads); }
 
-// Bytes of the partial results of a launch: a sequence that is cut has fewer than twice as many parts as are aimed at
-// (rf2_paged_attn.hip), each of `rows` rows of head_dim sums and two numbers more.
+// Bytes of the partial results of a launch: sequences that are cut have fewer than twice as many parts as are aimed at, each of
+// `rows` rows of head_dim sums and two numbers more, and at most as many tiles, with 32 bytes for every 8 rows
+// (rf2_paged_attn.hip).
 inline int64_t rf2_paged_workspace(const rf2_paged_config& c) {
-  return 2ll * rf2_paged_parts_per_head(c.kv_heads) * c.kv_heads * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4;
+  const int64_t aimed = (int64_t)rf2_paged_parts_per_head(c.kv_heads) * c.kv_heads;
+  return 2 * aimed * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4 + 32 * (aimed * (RF2_PAGED_ROWS_MANY / 8) + 1);
 }
 
 inline bool rf2_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }

@@ -63,7 +63,7 @@ struct Args {
   void* o;
   float* lse;
   int64_t q_stride;
-  int n_seqs, n_tokens, heads, kv_heads, group, unit_shift, n_pages, max_pages, causal, aimed, least;
+  int n_seqs, n_tokens, heads, kv_heads, group, unit_shift, n_pages, max_pages, causal, aimed, least, places, most_joints;
   float scale_log2;
 };
 
@@ -82,77 +82,95 @@ __device__ __forceinline__ int units_of(int keys) { return max((keys + 31) >> 5,
 // What a workgroup works on: a part of a tile of rows.
 struct Part {
   int seq, head, tile, chunk;     // chunk: number of the part
-  int tiles, chunks, units;       // of the sequence; units of a part
+  int tiles, units;               // of the sequence; units of a part of it
   Seq s;
-  int64_t place;                  // of the sequence's first part of K/V head 0 among those of the sequences that are cut
+  int place, joint;               // of the part among those of the sequences that are cut, of the tile's first 8 rows; -1: it is not cut
 };
 
-__device__ __forceinline__ int64_t wave_sum_before(int64_t& x) {      // inclusive sum in x, returns the exclusive one
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t mine = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t other = __shfl_up(x, d);
-    x += lane >= d ? other : 0;
-  }
-  return x - mine;
+// Inclusive sums over the lanes of a wavefront, in the vector unit (rows of 16 lanes, then their last ones carried on).
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
+#define RF2_ADD(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, true)
+  RF2_ADD(0x111, 0xf);            // row_shr:1, 2, 4, 8
+  RF2_ADD(0x112, 0xf);
+  RF2_ADD(0x114, 0xf);
+  RF2_ADD(0x118, 0xf);
+  RF2_ADD(0x142, 0xa);            // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+  RF2_ADD(0x143, 0xc);
+#undef RF2_ADD
+  return x;
 }
 
-// Finds part number `block` of the launch (CUT: tile number `block` of the sequences that are cut).  ROWS: of a tile.
-// Every wavefront does it for itself, 64 sequences at a time.
-template <int ROWS, bool CUT>
+// What is to be added up, 8 rows of a tile that is cut at a time: written by the workgroup of the tile's first part, in the
+// workspace behind their number.
+struct Joint {
+  int parts, place, step;         // parts of the tile (0: the tile has one and is done); place of the first, places to the next
+  int row, n_rows;                // first row of the sequence's, how many
+  int first, head;                // the sequence's first token, K/V head
+  int pad;
+};
+__device__ __forceinline__ int* joints_count(const Args& a) { return (int*)a.parts; }
+__device__ __forceinline__ Joint* joints(const Args& a) { return (Joint*)a.parts + 1; }
+template <int ROWS, int D>
+__device__ __forceinline__ float* part_sums(const Args& a, int place) { return a.parts + 8 * (a.most_joints + 1) + (int64_t)place * (ROWS * D); }
+template <int ROWS, int D>
+__device__ __forceinline__ float2* part_stats(const Args& a, int place) {
+  return (float2*)(a.parts + 8 * (a.most_joints + 1) + (int64_t)a.places * (ROWS * D)) + (int64_t)place * ROWS;
+}
+
+// Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.
+// (Sums are of 32 bits: of rows there are at most 2^20 tokens.  Rows that overlap, which no table of this library has, may be left out.)
+template <int ROWS>
 __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w) {
   const int lane = (int)threadIdx.x & 63;
-  int64_t work = 0;
   Seq s{0, 0, 0};
+  int tiles = 0;
+  const auto look = [&](int at) __attribute__((always_inline)) {
+    s = at < a.n_seqs ? seq_of(a, at) : Seq{0, 0, 0};
+    tiles = (int)((unsigned)(s.n_new * a.group + ROWS - 1) / (unsigned)ROWS);
+  };
+  float work = 0.f;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    if (s0 + lane < a.n_seqs) {
-      s = seq_of(a, s0 + lane);
-      work += (int64_t)((s.n_new * a.group + ROWS - 1) / ROWS) * units_of(s.len);
-    }
+    look(s0 + lane);
+    work += (float)tiles * (float)units_of(s.len);
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
-  // (no sequence has more than 2^19 units)
-  const int units = (int)min(max((work + a.aimed - 1) / a.aimed, (int64_t)a.least), (int64_t)1 << 20);
+  // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
+  const int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
   // Workgroups with equal number % 8 share an XCD and its L2.  Where the K/V heads can be dealt to the XCDs evenly, they are.
   const bool dealt = a.kv_heads % 8 == 0;
-  const int heads = dealt ? a.kv_heads / 8 : a.kv_heads;
-  int64_t at = dealt ? block >> 3 : block;
-  at /= heads;                                       // parts before this one, one head's counted
-  int64_t items_before = 0, place = 0;
+  const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
+  unsigned before = 0, places = 0, eights = 0;       // of the sequences before, one head's
+  bool found = false;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const bool there = s0 + lane < a.n_seqs;
-    if (a.n_seqs > 64) s = there ? seq_of(a, s0 + lane) : Seq{0, 0, 0};
-    const int tiles = there ? (s.n_new * a.group + ROWS - 1) / ROWS : 0;
-    const int chunks = (units_of(s.len) + units - 1) / units;
-    const int64_t cut = chunks > 1 ? (int64_t)tiles * chunks : 0;
-    int64_t sum = CUT ? (chunks > 1 ? tiles : 0) : (int64_t)tiles * chunks, cut_sum = cut;
-    const int64_t before = items_before + wave_sum_before(sum), cut_before = place + wave_sum_before(cut_sum);
-    sum += items_before;
+    if (a.n_seqs > 64) look(s0 + lane);
+    const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units;
+    const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, eight = chunks > 1 ? (unsigned)(s.n_new * a.group + 7) / 8 : 0;
+    const unsigned sum = before + wave_sums(items), cut_sum = places + wave_sums(cut), eight_sum = eights + wave_sums(eight);
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum <= at);
-    if (past != ~0ull) {                             // (a lane's sum only grows: the first lane that is beyond)
+    if (!found && past != ~0ull) {                   // (a lane's sum only grows: the first lane that is beyond)
       const int l = __builtin_ctzll(~past);
       const auto pick = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, l); };
-      const auto pick64 = [&](int64_t x) __attribute__((always_inline)) { return (int64_t)((uint64_t)(uint32_t)pick((int)(x >> 32)) << 32 | (uint32_t)pick((int)x)); };
       w.seq = s0 + l;
       w.s = {pick(s.first), pick(s.n_new), pick(s.len)};
       w.tiles = pick(tiles);
-      w.chunks = pick(chunks);
-      w.units = units;
-      w.place = pick64(cut_before) * a.kv_heads;
-      const int64_t each = CUT ? w.tiles : (int64_t)w.tiles * w.chunks;
-      const int64_t rest = (dealt ? (int64_t)(block >> 3) : (int64_t)block) - pick64(before) * heads;
-      const int hh = (int)(rest / each), x = (int)(rest % each);
-      w.head = dealt ? hh * 8 + (int)(block & 7) : hh;
-      w.chunk = CUT ? 0 : x / w.tiles;
-      w.tile = w.tiles - 1 - (CUT ? x : x % w.tiles);      // (under a causal mask the last tile is the longest: it goes first)
-      return true;
+      const unsigned n = (unsigned)pick((int)chunks), each = w.tiles * n;
+      w.units = (int)((unsigned)(units_of(w.s.len) + n - 1) / n);          // (all parts alike, but for the last)
+      const unsigned rest = mine - (unsigned)pick((int)(sum - items)) * heads, hh = rest / each, x = rest % each;
+      w.head = (int)(dealt ? hh * 8 + (block & 7) : hh);
+      w.chunk = (int)(x / (unsigned)w.tiles);
+      w.tile = w.tiles - 1 - (int)(x % (unsigned)w.tiles);                 // (under a causal mask the last tile is the longest: it goes first)
+      w.place = n > 1 ? (int)(((unsigned)pick((int)(cut_sum - cut)) * a.kv_heads + w.head * each) + x) : -1;
+      w.joint = (int)((unsigned)pick((int)(eight_sum - eight)) * a.kv_heads + w.head * (unsigned)pick((int)eight)) + w.tile * (ROWS / 8);
+      found = w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / 8 <= a.most_joints;
+      if (block != 0) return found;
     }
-    items_before = __shfl(sum, 63);
-    place += __shfl(cut_sum, 63);
+    before = (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
+    places = (unsigned)__builtin_amdgcn_readlane((int)cut_sum, 63);
+    eights = (unsigned)__builtin_amdgcn_readlane((int)eight_sum, 63);
   }
-  return false;
+  if (block == 0 && threadIdx.x == 0) *joints_count(a) = (int)min(eights * (unsigned)a.kv_heads, (unsigned)a.most_joints);
+  return found;
 }
 
 // Keys that row r of a sequence sees.
@@ -180,13 +198,19 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
   constexpr int WINDOW = KW > 1 ? 256 : 512;      // columns of the table that a wavefront has listed at a time
   typedef typename T::x8 x8;
   Part w;
-  if (!find_part<ROWS, false>(a, blockIdx.x, w)) return;
+  if (!find_part<ROWS>(a, blockIdx.x, w)) return;
   const int lane = (int)threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
   const int wave = RW * KW > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, rw = wave / KW, kw = wave % KW;
   const int n_rows = w.s.n_new * a.group, row0 = w.tile * ROWS + rw * 32 * QT;
   static_assert(RW == 1 || KW == 1, "a wavefront without rows leaves here");
   if (row0 >= n_rows) return;
   const int all = tile_units<ROWS>(a, w), u0 = w.chunk * w.units;
+  if (w.place >= 0 && w.chunk == 0 && threadIdx.x < ROWS / 8) {
+    const int row = w.tile * ROWS + 8 * (int)threadIdx.x;
+    if (row < n_rows)
+      joints(a)[w.joint + threadIdx.x] = {all > w.units ? (all + w.units - 1) / w.units : 0, w.place, w.tiles, row, min(n_rows - row, 8),
+                                          w.s.first, w.head, 0};
+  }
   if (w.chunk > 0 && u0 >= all) return;                      // this tile ends before
   const bool whole = all <= w.units;                         // its only part: no other has to be added
   const int last_row = min(row0 + 32 * QT, n_rows) - 1;
@@ -606,14 +630,13 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
     m[0] = top;
     l[0] = sum;
   }
-  const int64_t place = w.place + ((int64_t)w.head * w.chunks + w.chunk) * w.tiles + w.tile;
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     const int r = row_of(q) - w.tile * ROWS;
     if (row_of(q) >= n_rows) continue;
     const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + kv_head * a.group + row_of(q) % a.group;
     const float f = whole ? (l[q] > 0.f ? 1.0f / l[q] : (l[q] == 0.f ? 0.f : l[q])) : 1.0f;     // a row that sees no key yields zeros
-    float* const part = a.parts + place * (ROWS * (D + 2));
+    float* const part = part_sums<ROWS, D>(a, w.place) + r * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       if (KW > 1 && dt != kw) continue;
@@ -626,52 +649,85 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
           for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(o[q][dt][4 * g + e] * f);
           *reinterpret_cast<typename T::x4*>((typename T::x1*)a.o + out_row * D + ch) = pk;
         } else {
-          *reinterpret_cast<float4*>(part + r * D + ch) = make_float4(o[q][dt][4 * g], o[q][dt][4 * g + 1], o[q][dt][4 * g + 2], o[q][dt][4 * g + 3]);
+          *reinterpret_cast<float4*>(part + ch) = make_float4(o[q][dt][4 * g], o[q][dt][4 * g + 1], o[q][dt][4 * g + 2], o[q][dt][4 * g + 3]);
         }
       }
     }
     if (lh == 0 && kw == 0) {
-      if (!whole) *reinterpret_cast<float2*>(part + ROWS * D + 2 * r) = make_float2(m[q], l[q]);
+      if (!whole) part_stats<ROWS, D>(a, w.place)[r] = make_float2(m[q], l[q]);
       else if (a.lse != nullptr) a.lse[out_row] = (m[q] + __log2f(l[q])) * 0.6931471805599453f;
     }
   }
 }
 
-// Adds the parts of the tiles that are cut: 8 rows of a tile to a workgroup, 32 lanes to a row.
+// Adds the parts of the tiles that are cut.  A workgroup takes 8 rows at a time, 32 lanes to a row; where there are fewer rows,
+// 2, 4 or 8 times 32 lanes share the parts of one.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Args a) {
-  Part w;
-  if (!find_part<ROWS, true>(a, blockIdx.x, w)) return;
-  const int parts = (tile_units<ROWS>(a, w) + w.units - 1) / w.units;
-  if (parts < 2) return;
-  constexpr int E = D / 32;                        // channels of a lane
+  constexpr int E = D / 32, DEEP = 8;              // channels of a lane; parts asked for at a time
   typedef __attribute__((ext_vector_type(E))) float fE;
   typedef __attribute__((ext_vector_type(E))) typename T::x1 tE;
-  const int r = (int)blockIdx.y * 8 + ((int)threadIdx.x >> 5), row = w.tile * ROWS + r, ch = ((int)threadIdx.x & 31) * E;
-  if (row >= w.s.n_new * a.group) return;
-  const float* const from = a.parts + (w.place + (int64_t)w.head * w.chunks * w.tiles + w.tile) * (ROWS * (D + 2));
-  const int64_t step = (int64_t)w.tiles * (ROWS * (D + 2));
-  float top = -FLT_MAX;
-  for (int p = 0; p < parts; ++p) top = fmaxf(top, from[p * step + ROWS * D + 2 * r]);
-  float sum = 0.f;
-  fE acc = (fE)0.f;
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float2 st = *reinterpret_cast<const float2*>(from + p * step + ROWS * D + 2 * r);
-    const float weight = __builtin_amdgcn_exp2f(st.x - top);
-    const fE x = *reinterpret_cast<const fE*>(from + p * step + r * D + ch);
-    sum = fmaf(st.y, weight, sum);
+  __shared__ fE sums[8][32];
+  __shared__ float2 totals[8];
+  const int half = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const int count = *joints_count(a);
+  for (int task = (int)blockIdx.x; task < count; task += (int)gridDim.x) {
+    const Joint j = joints(a)[task];
+    if (j.parts == 0) continue;
+    const int share = j.n_rows > 4 ? 0 : j.n_rows > 2 ? 1 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
+    const bool there = r < j.n_rows;
+    fE acc = (fE)0.f;
+    float top = -FLT_MAX, sum = 0.f;
+    auto take = [&](float at, float total, const fE& x) __attribute__((always_inline)) {
+      const float weight = __builtin_amdgcn_exp2f(at - top);
+      sum = fmaf(total, weight, sum);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[e], weight, acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(x[e], weight, acc[e]);
+    };
+    auto reach = [&](float at) __attribute__((always_inline)) {
+      const float to = fmaxf(top, at), alpha = __builtin_amdgcn_exp2f(top - to);
+      top = to;
+      sum *= alpha;
+      acc *= alpha;
+    };
+    for (int p0 = half & (every - 1); there && p0 < j.parts; p0 += every * DEEP) {
+      float2 st[DEEP];
+      fE x[DEEP];
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i) {
+        const int p = p0 + i * every, place = j.place + min(p, j.parts - 1) * j.step, row = j.row % ROWS + r;
+        st[i] = part_stats<ROWS, D>(a, place)[row];
+        x[i] = *reinterpret_cast<const fE*>(part_sums<ROWS, D>(a, place) + row * D + lane * E);
+        if (p >= j.parts) st[i] = make_float2(-FLT_MAX, 0.f), x[i] = (fE)0.f;
+      }
+      float most = st[0].x;
+#pragma unroll
+      for (int i = 1; i < DEEP; ++i) most = fmaxf(most, st[i].x);
+      reach(most);
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i) take(st[i].x, st[i].y, x[i]);
+    }
+    if (share > 0) {                               // (the same for the whole workgroup)
+      sums[half][lane] = acc;
+      if (lane == 0) totals[half] = make_float2(top, sum);
+      __syncthreads();
+      if ((half & (every - 1)) == 0)
+        for (int k = 1; k < every; ++k) {
+          reach(totals[half + k].x);
+          take(totals[half + k].x, totals[half + k].y, sums[half + k][lane]);
+        }
+      __syncthreads();
+    }
+    if (!there || (half & (every - 1)) != 0) continue;
+    const float f = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+    const int row = j.row + r;
+    const int64_t out = (int64_t)(j.first + row / a.group) * a.heads + j.head * a.group + row % a.group;
+    tE pk;
+#pragma unroll
+    for (int e = 0; e < E; ++e) pk[e] = (typename T::x1)(acc[e] * f);
+    *reinterpret_cast<tE*>((typename T::x1*)a.o + out * D + lane * E) = pk;
+    if (a.lse != nullptr && lane == 0) a.lse[out] = (top + __log2f(sum)) * 0.6931471805599453f;
   }
-  const float f = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
-  const int t = row / a.group;
-  const int64_t out = (int64_t)(w.s.first + t) * a.heads + w.head * a.group + row % a.group;
-  tE pk;
-#pragma unroll
-  for (int e = 0; e < E; ++e) pk[e] = (typename T::x1)(acc[e] * f);
-  *reinterpret_cast<tE*>((typename T::x1*)a.o + out * D + ch) = pk;
-  if (a.lse != nullptr && ch == 0) a.lse[out] = (top + __log2f(sum)) * 0.6931471805599453f;
 }
 
 template <class T, int D, int QT, int RW, int KW>
@@ -679,6 +735,8 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
   constexpr int ROWS = 32 * QT * RW;
   const rf2_paged_config& c = plan->cfg;
   a.aimed = rf2_paged_parts_per_head(c.kv_heads);
+  a.places = 2 * a.aimed * c.kv_heads;
+  a.most_joints = a.aimed * c.kv_heads * (RF2_PAGED_ROWS_MANY / 8);
   a.least = KW > 1 ? 16 : 8;
   // tiles there can be: a sequence has at most one that is not full
   const int64_t rows = (int64_t)a.n_tokens * a.group;
@@ -689,10 +747,8 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
   paged_attn_kernel<T, D, QT, RW, KW><<<dim3((unsigned)grid), dim3(64 * RW * KW), 0, st>>>(a);
   RF2_LAUNCH_CHECK();
   if (can_be_cut) {
-    // (of tiles that are cut there are at most as many as parts are aimed at)
-    const unsigned some = (unsigned)(std::min(tiles, (int64_t)a.aimed) * c.kv_heads);
-    const unsigned rows_of_tile = (unsigned)std::min((int64_t)ROWS, rows);
-    join_kernel<T, D, ROWS><<<dim3(some, (rows_of_tile + 7) / 8), dim3(256), 0, st>>>(a);
+    const int64_t eights = std::min((int64_t)a.most_joints, (rows / 8 + std::min(a.n_seqs, a.n_tokens)) * c.kv_heads);
+    join_kernel<T, D, ROWS><<<dim3((unsigned)std::min(eights, (int64_t)1024)), dim3(256), 0, st>>>(a);
     RF2_LAUNCH_CHECK();
   }
   return RF2_OK;

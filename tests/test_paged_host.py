@@ -43,7 +43,7 @@ def test_sizes(over):
     p = make(**over)
     c = p.cfg
     assert p.info.cache_elements == c.n_pages * c.kv_heads * c.page * c.head_dim
-    assert 0 < p.info.workspace_bytes <= 2 * 1024 * 128 * (c.head_dim + 2) * 4 + 4096
+    assert 0 < p.info.workspace_bytes <= 1024 * (2 * 128 * (c.head_dim + 2) * 4 + 16 * 32) + 32
     buf = p.alloc("cpu")
     assert buf["k_cache"].numel() == buf["v_cache"].numel() == p.info.cache_elements
     assert buf["free_pages"].tolist() == list(range(c.n_pages - 1, -1, -1)) and buf["n_free"].item() == c.n_pages
