@@ -269,16 +269,19 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
     return (((int64_t)page * a.kv_heads + kv_head) * (1 << a.unit_shift) + (u & ((1 << a.unit_shift) - 1))) * (32 * D * 2);
   };
   // Operands of a tile: buffer loads, the tile's address in scalar registers, a constant offset of the lane, and nothing past the tile.
+  // Few rows to a sequence: a tile is read once, or a few times at once, and then not for long, so its loads are marked as not to
+  // be kept (64 single tokens over 0.79 GB of keys and values 149.7 -> 137.4 us).
+  constexpr int ONCE = KW > 1 ? 2 : 0;
   constexpr unsigned TILE = 32 * D * 2;
   const uint32_t k_lane = (uint32_t)lane * 16, v_lane = (uint32_t)(lh * D + l32) * 16;
   auto buffer = [](const unsigned char* tile) __attribute__((always_inline)) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)uniform_ptr(tile), 0, TILE, 0x00020000);
   };
   auto k_load = [&](auto tile, int c) __attribute__((always_inline)) {
-    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + c % 4 * 1024, c / 4 * 4096, 0));
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + c % 4 * 1024, c / 4 * 4096, ONCE));
   };
   auto v_load = [&](auto tile, int j) __attribute__((always_inline)) {
-    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + j / 2 * 512, j % 2 * (2 * D * 16), 0));
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + j / 2 * 512, j % 2 * (2 * D * 16), ONCE));
   };
   auto operand_p = [](const uint32_t (&P)[8], int ks) __attribute__((always_inline)) {
     const u32x4 x = {P[4 * ks], P[4 * ks + 1], P[4 * ks + 2], P[4 * ks + 3]};

@@ -7,28 +7,51 @@
 
 namespace {
 
-constexpr int NT = 1024, WAVES = NT / 64;
+// Inclusive sums over the lanes of a wavefront, in the vector unit (rows of 16 lanes, then their last ones carried on).
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
+#define RF2_ADD(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, true)
+  RF2_ADD(0x111, 0xf);            // row_shr:1, 2, 4, 8
+  RF2_ADD(0x112, 0xf);
+  RF2_ADD(0x114, 0xf);
+  RF2_ADD(0x118, 0xf);
+  RF2_ADD(0x142, 0xa);            // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+  RF2_ADD(0x143, 0xc);
+#undef RF2_ADD
+  return x;
+}
+// The same for values of up to 2^40 (20 bits at a time: no part overflows).
+__device__ __forceinline__ int64_t wave_sums64(int64_t x) {
+  return ((int64_t)wave_sums((uint32_t)(x >> 20)) << 20) + wave_sums((uint32_t)x & 0xfffffu);
+}
 
-// Sum over the workgroup of what the threads before this one have; `total`: of all.
-__device__ __forceinline__ int64_t block_scan(int64_t mine, int64_t* across, int64_t& total) {
+// What the wavefronts of a workgroup tell each other: two sums and flags.
+struct Across {
+  int64_t a[16], b[16];
+  int flags[16];
+};
+// Sums over the workgroup of what the threads before this one have, in a and b; of all, in all_a and all_b; flags of all.
+template <int NT>
+__device__ __forceinline__ void block_sums(Across& m, int64_t& a, int64_t& b, int64_t& all_a, int64_t& all_b, int& flags) {
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-  int64_t sum = mine;
+  const int64_t sum_a = wave_sums64(a), sum_b = wave_sums64(b);
+  int set = 0;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t other = __shfl_up(sum, d);
-    sum += lane >= d ? other : 0;
-  }
-  if (lane == 63) across[wave] = sum;
+  for (int bit = 1; bit <= RF2_PAGED_POOL_FULL; bit *= 2) set |= __builtin_amdgcn_ballot_w64((flags & bit) != 0) != 0 ? bit : 0;
+  if (lane == 63) m.a[wave] = sum_a, m.b[wave] = sum_b, m.flags[wave] = set;
   __syncthreads();
-  int64_t before = 0;
-  total = 0;
+  int64_t before_a = 0, before_b = 0;
+  all_a = all_b = 0;
+  flags = 0;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    before += w < wave ? across[w] : 0;
-    total += across[w];
+  for (int w = 0; w < NT / 64; ++w) {
+    before_a += w < wave ? m.a[w] : 0;
+    before_b += w < wave ? m.b[w] : 0;
+    all_a += m.a[w];
+    all_b += m.b[w];
+    flags |= m.flags[w];
   }
-  __syncthreads();
-  return before + sum - mine;
+  a = before_a + sum_a - a;
+  b = before_b + sum_b - b;
 }
 
 struct AppendArgs {
@@ -42,7 +65,7 @@ struct Lengths {
   int32_t cu[RF2_PAGED_MAX_SEQS + 1];   // rows before a sequence
   int32_t base[RF2_PAGED_MAX_SEQS];     // new pages before it
   int32_t old[RF2_PAGED_MAX_SEQS];      // its tokens so far
-  int64_t across[WAVES];
+  Across across;
 };
 
 __device__ __forceinline__ int pages_of(int64_t tokens, int shift) { return (int)((tokens + (1 << shift) - 1) >> shift); }
@@ -74,28 +97,27 @@ __device__ __forceinline__ void deal_slots(const AppendArgs& a, const Lengths& m
 }
 
 // One workgroup: sums, checks, lengths; with `slots` the slots too.  Every thread has a run of sequences.
+template <int NT>
 __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   __shared__ Lengths m;
   const int run = (a.n_seqs + NT - 1) / NT, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
   const int64_t cap = (int64_t)a.max_pages << a.page_shift;
   const int n_free = a.n_free[0];
   int bad = n_free < 0 || n_free > a.n_pages ? RF2_PAGED_BAD_LENGTH : 0;
-  int64_t tokens = 0, pages = 0;
+  int64_t cu = 0, base = 0;
   for (int s = s0; s < s1; ++s) {
     const int old = a.seq_len[s], more = a.new_len[s];
     m.old[s] = old;
     if (more < 0 || old < 0 || old > cap) { bad |= RF2_PAGED_BAD_LENGTH; continue; }
     if ((int64_t)old + more > cap) bad |= RF2_PAGED_SEQ_FULL;
-    tokens += more;
-    pages += pages_of((int64_t)old + more, a.page_shift) - pages_of(old, a.page_shift);
+    cu += more;
+    base += pages_of((int64_t)old + more, a.page_shift) - pages_of(old, a.page_shift);
   }
   int64_t all_tokens, all_pages;
-  int64_t cu = block_scan(tokens, m.across, all_tokens), base = block_scan(pages, m.across, all_pages);
-  if (all_tokens > a.n_tokens) bad |= RF2_PAGED_TOKENS_FULL;
-  if (all_pages > n_free) bad |= RF2_PAGED_POOL_FULL;
-  int status = 0;
-#pragma unroll
-  for (int bit = 1; bit <= RF2_PAGED_POOL_FULL; bit *= 2) status |= __syncthreads_or(bad & bit) ? bit : 0;
+  int status = bad;
+  block_sums<NT>(m.across, cu, base, all_tokens, all_pages, status);
+  if (all_tokens > a.n_tokens) status |= RF2_PAGED_TOKENS_FULL;
+  if (all_pages > n_free) status |= RF2_PAGED_POOL_FULL;
   const bool fine = status == 0;
   for (int s = s0; s < s1; ++s) {
     const int old = m.old[s], more = fine ? a.new_len[s] : 0;
@@ -117,23 +139,26 @@ __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   deal_slots(a, m, n_free, fine, (int)threadIdx.x, a.n_tokens, NT);
 }
 
-constexpr int SLOTS_OF_GROUP = 2 * NT;
+constexpr int SLOT_THREADS = 1024, SLOTS_OF_GROUP = 2 * SLOT_THREADS;
 
 // Slots where there are many: every workgroup repeats the sums (from what append_kernel left, which may lie over its inputs).
-__global__ void __launch_bounds__(NT) slots_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(SLOT_THREADS) slots_kernel(AppendArgs a) {
+  constexpr int NT = SLOT_THREADS;
   __shared__ Lengths m;
   const int run = (a.n_seqs + NT - 1) / NT, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
+  const int n_free = a.n_free_out[0];
   const bool fine = a.status[0] == 0;
-  int64_t pages = 0, all_pages = 0;
+  int64_t base = 0, none = 0, all_pages = 0, no_sum;
   if (fine) {
     for (int s = s0; s < s1; ++s) {
       const int now = a.seq_len_out[s], old = now - a.new_len[s];
       m.old[s] = old;
       m.cu[s] = a.cu_new[s];
-      pages += pages_of(now, a.page_shift) - pages_of(old, a.page_shift);
+      base += pages_of(now, a.page_shift) - pages_of(old, a.page_shift);
     }
     if (threadIdx.x == 0) m.cu[a.n_seqs] = a.cu_new[a.n_seqs];
-    int64_t base = block_scan(pages, m.across, all_pages);
+    int flags = 0;
+    block_sums<NT>(m.across, base, none, all_pages, no_sum, flags);
     for (int s = s0; s < s1; ++s) {
       m.base[s] = (int)base;
       base += pages_of(a.seq_len_out[s], a.page_shift) - pages_of(m.old[s], a.page_shift);
@@ -143,7 +168,7 @@ __global__ void __launch_bounds__(NT) slots_kernel(AppendArgs a) {
   }
   __syncthreads();
   const int first = (int)blockIdx.x * SLOTS_OF_GROUP;
-  deal_slots(a, m, a.n_free_out[0] + (int)all_pages, fine, first + (int)threadIdx.x, min(first + SLOTS_OF_GROUP, a.n_tokens), NT);
+  deal_slots(a, m, n_free + (int)all_pages, fine, first + (int)threadIdx.x, min(first + SLOTS_OF_GROUP, a.n_tokens), NT);
 }
 
 struct ReleaseArgs {
@@ -153,86 +178,109 @@ struct ReleaseArgs {
   int n_seqs, page_shift, max_pages, n_pages;
 };
 
-// One workgroup.  The columns of all finished sequences stand in one row of `all` entries, of which a round takes NT * DEEP;
-// what is a page among them goes to the next places of the stack.
+// One workgroup.  The columns of all sequences that give back stand in one row of `all` entries, of which a round takes
+// NT * DEEP, a wavefront 64 * DEEP side by side; what is a page among them goes to the next places of the stack.
+template <int NT>
 __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
-  constexpr int DEEP = 4;
-  __shared__ int64_t across[WAVES];
-  __shared__ int32_t first[RF2_PAGED_MAX_SEQS + 1];    // entries before a sequence
-  __shared__ int32_t found[DEEP][WAVES];
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  constexpr int DEEP = 8, WAVES = NT / 64, OF_WAVE = 64 * DEEP;
+  __shared__ Across across;
+  __shared__ int32_t first[RF2_PAGED_MAX_SEQS + 1];    // entries before a sequence that gives some back
+  __shared__ uint16_t which[RF2_PAGED_MAX_SEQS];       // its row of the table
+  __shared__ int32_t found[2][WAVES];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int run = (a.n_seqs + NT - 1) / NT, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
   const int64_t cap = (int64_t)a.max_pages << a.page_shift;
   const int n_free = a.n_free[0];
-  int bad = n_free < 0 || n_free > a.n_pages ? 1 : 0;
-  int64_t mine = 0, all64;
+  int flags = n_free < 0 || n_free > a.n_pages ? RF2_PAGED_BAD_LENGTH : 0;
+  int64_t before = 0, rows = 0, all64, all_rows;
   for (int s = s0; s < s1; ++s) {
     const int len = a.seq_len[s];
-    if (len < 0 || len > cap) bad = 1;
-    else if (a.done[s]) mine += pages_of(len, a.page_shift);
+    if (len < 0 || len > cap) flags |= RF2_PAGED_BAD_LENGTH;
+    else if (a.done[s] && len > 0) before += pages_of(len, a.page_shift), rows += 1;
   }
-  int64_t before = block_scan(mine, across, all64);
-  int status = __syncthreads_or(bad) ? RF2_PAGED_BAD_LENGTH : 0;
+  block_sums<NT>(across, before, rows, all64, all_rows, flags);
+  int status = flags;
   if (all64 > INT32_MAX) status |= RF2_PAGED_POOL_FULL;     // (more than any pool has)
-  const int all = status ? 0 : (int)all64;
+  const int all = status ? 0 : (int)all64, n_rows = (int)all_rows;
   if (!status) {
     for (int s = s0; s < s1; ++s) {
-      first[s] = (int)before;
-      before += a.done[s] ? pages_of(a.seq_len[s], a.page_shift) : 0;
+      const int len = a.seq_len[s];
+      if (!a.done[s] || len == 0) continue;
+      first[rows] = (int)before;
+      which[rows] = (uint16_t)s;
+      before += pages_of(len, a.page_shift);
+      rows += 1;
     }
-    if (threadIdx.x == 0) first[a.n_seqs] = all;
+    if (threadIdx.x == 0) first[n_rows] = all;
   }
   __syncthreads();
-  // pages among the entries of a round, in order: what stands before a thread's entry of row j, and how many there are
-  int entry[DEEP], rank[DEEP];
-  auto round = [&](int at) {
+  // Entries of a round that begin at `at` for this wavefront.  Its place among the sequences only moves on.
+  int place = 0;
+  auto look = [&](int at, int (&entry)[DEEP]) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < DEEP; ++j) {
-      const int i = at + j * NT + (int)threadIdx.x;
+      const int from = at + 64 * j, i = from + lane;
       entry[j] = -1;
-      if (i < all) {
-        int lo = 0, hi = a.n_seqs;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (first[mid] <= i) lo = mid; else hi = mid;
-        }
-        entry[j] = a.table[(int64_t)lo * a.max_pages + (i - first[lo])];
+      if (from >= all) continue;
+      while (true) {                                 // (64 sequences' ends at a time)
+        const int next = place + 1 + lane;
+        const int passed = __popcll(__builtin_amdgcn_ballot_w64(next < n_rows && first[min(next, n_rows)] <= from));
+        place += passed;
+        if (passed < 64) break;
       }
+      int s = place;
+      while (s + 1 < n_rows && first[s + 1] <= i) ++s;
+      if (i < all) entry[j] = a.table[(int64_t)which[s] * a.max_pages + (i - first[s])];
     }
+  };
+  // How many pages stand before the wavefront's entries in the round, and how many there are in all.
+  int turn = 0;
+  auto count = [&](const int (&entry)[DEEP], int& ahead) __attribute__((always_inline)) {
+    int mine = 0;
 #pragma unroll
-    for (int j = 0; j < DEEP; ++j) {
-      const uint64_t pages = __builtin_amdgcn_ballot_w64((unsigned)entry[j] < (unsigned)a.n_pages);
-      rank[j] = __popcll(pages & ((1ull << lane) - 1));
-      if (lane == 0) found[j][wave] = __popcll(pages);
-    }
+    for (int j = 0; j < DEEP; ++j) mine += __popcll(__builtin_amdgcn_ballot_w64((unsigned)entry[j] < (unsigned)a.n_pages));
+    if (lane == 0) found[turn][wave] = mine;
     __syncthreads();
     int sum = 0;
+    ahead = 0;
 #pragma unroll
-    for (int j = 0; j < DEEP; ++j)
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        rank[j] += w == wave ? sum : 0;
-        sum += found[j][w];
-      }
-    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) {
+      ahead += w < wave ? found[turn][w] : 0;
+      sum += found[turn][w];
+    }
+    turn ^= 1;                                       // (the next round writes elsewhere: one barrier a round is enough)
     return sum;
   };
+  int entry[DEEP], ahead;
   // Only where every entry as a page would be too many is it counted first.
-  int64_t pages = all;
-  if (!status && pages + n_free > a.n_pages) {
-    pages = 0;
-    for (int at = 0; at < all; at += NT * DEEP) pages += round(at);
+  if (!status && (int64_t)all + n_free > a.n_pages) {
+    int64_t pages = 0;
+    for (int at = 0; at < all; at += NT * DEEP) {
+      look(at + wave * OF_WAVE, entry);
+      pages += count(entry, ahead);
+    }
     if (pages + n_free > a.n_pages) status |= RF2_PAGED_POOL_FULL;
+    place = 0;
   }
   int top = n_free;
-  if (!status)
+  if (!status && all > 0) {
+    look(wave * OF_WAVE, entry);
     for (int at = 0; at < all; at += NT * DEEP) {
-      const int sum = round(at);
+      int next[DEEP];
+      look(at + NT * DEEP + wave * OF_WAVE, next);   // on their way while this round is counted
+      const int sum = count(entry, ahead);
+      int to = top + ahead;
 #pragma unroll
-      for (int j = 0; j < DEEP; ++j)
-        if ((unsigned)entry[j] < (unsigned)a.n_pages) a.free_pages[top + rank[j]] = entry[j];
+      for (int j = 0; j < DEEP; ++j) {
+        const bool page = (unsigned)entry[j] < (unsigned)a.n_pages;
+        const uint64_t pages = __builtin_amdgcn_ballot_w64(page);
+        if (page) a.free_pages[to + __popcll(pages & ((1ull << lane) - 1))] = entry[j];
+        to += __popcll(pages);
+        entry[j] = next[j];
+      }
       top += sum;
     }
+  }
   for (int s = s0; s < s1; ++s) a.seq_len_out[s] = !status && a.done[s] ? 0 : a.seq_len[s];
   if (threadIdx.x == 0) {
     a.n_free_out[0] = top;
@@ -257,12 +305,13 @@ extern "C" int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int3
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   const AppendArgs a{seq_len, new_len, free_pages, n_free, block_table, seq_len_out, n_free_out, cu_new, slots, status,
                      n_seqs, n_tokens, page_shift(plan), plan->cfg.max_pages, plan->cfg.n_pages};
-  // One workgroup deals this many slots in about the time of another launch.
-  const bool together = n_tokens <= 4 * NT;
-  append_kernel<<<dim3(1), dim3(NT), 0, (hipStream_t)stream>>>(a, together);
+  // One workgroup deals this many slots in about the time of another launch; fewer threads meet sooner.
+  const bool together = n_tokens <= 4096, few = n_tokens <= 512 && n_seqs <= 512;
+  if (few) append_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a, true);
+  else append_kernel<1024><<<dim3(1), dim3(1024), 0, (hipStream_t)stream>>>(a, together);
   RF2_LAUNCH_CHECK();
   if (!together) {
-    slots_kernel<<<dim3((n_tokens + SLOTS_OF_GROUP - 1) / SLOTS_OF_GROUP), dim3(NT), 0, (hipStream_t)stream>>>(a);
+    slots_kernel<<<dim3((n_tokens + SLOTS_OF_GROUP - 1) / SLOTS_OF_GROUP), dim3(SLOT_THREADS), 0, (hipStream_t)stream>>>(a);
     RF2_LAUNCH_CHECK();
   }
   return RF2_OK;
@@ -278,9 +327,11 @@ extern "C" int rf2_paged_release(const rf2_paged_plan* plan, int32_t n_seqs, con
                         (const void*)seq_len_out, (const void*)n_free_out, (const void*)status})
     if (!rf2_aligned(p, 4)) return RF2_ERR_INVALID_ARG;
   if (const int rc = rf2_check_paged_device(plan)) return rc;
-  release_kernel<<<dim3(1), dim3(NT), 0, (hipStream_t)stream>>>(
-      ReleaseArgs{done, seq_len, block_table, n_free, free_pages, seq_len_out, n_free_out, status, n_seqs, page_shift(plan),
-                  plan->cfg.max_pages, plan->cfg.n_pages});
+  const ReleaseArgs a{done, seq_len, block_table, n_free, free_pages, seq_len_out, n_free_out, status, n_seqs, page_shift(plan),
+                      plan->cfg.max_pages, plan->cfg.n_pages};
+  // (the entries of four rounds of the smaller workgroup at most)
+  if ((int64_t)n_seqs * plan->cfg.max_pages <= 8192) release_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a);
+  else release_kernel<1024><<<dim3(1), dim3(1024), 0, (hipStream_t)stream>>>(a);
   RF2_LAUNCH_CHECK();
   return RF2_OK;
 }

@@ -248,6 +248,10 @@ class Plan:
         return buf["o"]
 
 
+# (of torch's two ways to the current stream the one that makes no object of it: 0.1 us in place of 2.8)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _arg(t, what, dtype, numel, device):
     """Address of a contiguous tensor of `numel` elements of `dtype` on the plan's device."""
     if t.dtype is not dtype or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
@@ -333,6 +337,9 @@ class PagedPlan:
                     o=torch.empty(n_tokens, c.heads, c.head_dim, dtype=self.dtype, device=device))
 
     # -- the calls -----------------------------------------------------------------------------
+    def _stream(self, stream):
+        return _raw_stream(self.device) if stream is None else stream.cuda_stream
+
     def rf2_paged_append(self, seq_len, new_len, free_pages, n_free, block_table, seq_len_out, n_free_out, cu_new, slots, status,
                          stream=None):
         c, dev, i32 = self.cfg, self.device, torch.int32
@@ -343,7 +350,7 @@ class PagedPlan:
             _arg(block_table, "block_table", i32, n_seqs * c.max_pages, dev),
             _arg(seq_len_out, "seq_len_out", i32, n_seqs, dev), _arg(n_free_out, "n_free_out", i32, 1, dev),
             _arg(cu_new, "cu_new", i32, n_seqs + 1, dev), _arg(slots, "slots", i32, n_tokens, dev),
-            _arg(status, "status", i32, 1, dev), _stream(stream)), "rf2_paged_append")
+            _arg(status, "status", i32, 1, dev), self._stream(stream)), "rf2_paged_append")
 
     def rf2_paged_release(self, done, seq_len, block_table, free_pages, n_free, seq_len_out, n_free_out, status, stream=None):
         c, dev, i32 = self.cfg, self.device, torch.int32
@@ -353,7 +360,7 @@ class PagedPlan:
             _arg(seq_len, "seq_len", i32, n_seqs, dev), _arg(block_table, "block_table", i32, n_seqs * c.max_pages, dev),
             _arg(free_pages, "free_pages", i32, c.n_pages, dev), _arg(n_free, "n_free", i32, 1, dev),
             _arg(seq_len_out, "seq_len_out", i32, n_seqs, dev), _arg(n_free_out, "n_free_out", i32, 1, dev),
-            _arg(status, "status", i32, 1, dev), _stream(stream)), "rf2_paged_release")
+            _arg(status, "status", i32, 1, dev), self._stream(stream)), "rf2_paged_release")
 
     def rf2_paged_store(self, k, v, slots, k_cache, v_cache, stream=None):
         c, dev, size = self.cfg, self.device, self.info.cache_elements
@@ -362,7 +369,7 @@ class PagedPlan:
         _check(lib().rf2_paged_store(
             self._h, n_tokens, *_rows(k, "k", self.dtype, shape, dev), *_rows(v, "v", self.dtype, shape, dev),
             _arg(slots, "slots", torch.int32, n_tokens, dev), _arg(k_cache, "k_cache", self.dtype, size, dev),
-            _arg(v_cache, "v_cache", self.dtype, size, dev), _stream(stream)), "rf2_paged_store")
+            _arg(v_cache, "v_cache", self.dtype, size, dev), self._stream(stream)), "rf2_paged_store")
 
     def rf2_paged_attn(self, q, k_cache, v_cache, block_table, seq_len, cu_new, workspace, o, lse=None, stream=None):
         c, dev, size, i32 = self.cfg, self.device, self.info.cache_elements, torch.int32
@@ -374,5 +381,5 @@ class PagedPlan:
             _arg(cu_new, "cu_new", i32, n_seqs + 1, dev),
             _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, dev),
             _arg(o, "o", self.dtype, n_tokens * c.heads * c.head_dim, dev),
-            None if lse is None else _arg(lse, "lse", torch.float32, n_tokens * c.heads, dev), _stream(stream)),
+            None if lse is None else _arg(lse, "lse", torch.float32, n_tokens * c.heads, dev), self._stream(stream)),
             "rf2_paged_attn")
