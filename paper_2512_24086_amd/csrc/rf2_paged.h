@@ -17,6 +17,8 @@ constexpr int RF2_PAGED_MAX_SEQS = 4096;
 constexpr int RF2_PAGED_PARTS = 1024;
 // Query rows of a workgroup: few rows to a sequence, and many.
 constexpr int RF2_PAGED_ROWS_FEW = 32, RF2_PAGED_ROWS_MANY = 128;
+// Groups of rows of a tile whose parts are added together (32 bytes each).
+constexpr int RF2_PAGED_JOINTS = 16;
 
 inline int rf2_paged_parts_per_head(int kv_heads) { return std::max(1, RF2_PAGED_PARTS / kv_heads); }
 
@@ -25,7 +27,7 @@ inline int rf2_paged_parts_per_head(int kv_heads) { return std::max(1, RF2_PAGED
 // (rf2_paged_attn.hip).
 inline int64_t rf2_paged_workspace(const rf2_paged_config& c) {
   const int64_t aimed = (int64_t)rf2_paged_parts_per_head(c.kv_heads) * c.kv_heads;
-  return 2 * aimed * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4 + 32 * (aimed * (RF2_PAGED_ROWS_MANY / 8) + 1);
+  return 2 * aimed * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4 + 32 * (aimed * RF2_PAGED_JOINTS + 1);
 }
 
 inline bool rf2_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }

@@ -84,7 +84,7 @@ struct Part {
   int seq, head, tile, chunk;     // chunk: number of the part
   int tiles, units;               // of the sequence; units of a part of it
   Seq s;
-  int place, joint;               // of the part among those of the sequences that are cut, of the tile's first 8 rows; -1: it is not cut
+  int place, joint;               // of the part among those of the sequences that are cut, of the tile's first rows; -1: it is not cut
 };
 
 // Inclusive sums over the lanes of a wavefront, in the vector unit (rows of 16 lanes, then their last ones carried on).
@@ -100,7 +100,7 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
   return x;
 }
 
-// What is to be added up, 8 rows of a tile that is cut at a time: written by the workgroup of the tile's first part, in the
+// What is to be added up, a few rows of a tile that is cut at a time: written by the workgroup of the tile's first part, in the
 // workspace behind their number.
 struct Joint {
   int parts, place, step;         // parts of the tile (0: the tile has one and is done); place of the first, places to the next
@@ -116,6 +116,10 @@ template <int ROWS, int D>
 __device__ __forceinline__ float2* part_stats(const Args& a, int place) {
   return (float2*)(a.parts + 8 * (a.most_joints + 1) + (int64_t)a.places * (ROWS * D)) + (int64_t)place * ROWS;
 }
+
+// Rows of a joint: a workgroup of join_kernel has 32 lanes for each, and more where there are few rows and many parts.
+template <int ROWS>
+constexpr int JOINT = ROWS == RF2_PAGED_ROWS_FEW ? 2 : 8;
 
 // Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.
 // (Sums are of 32 bits: of rows there are at most 2^20 tokens.  Rows that overlap, which no table of this library has, may be left out.)
@@ -140,13 +144,13 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   // Workgroups with equal number % 8 share an XCD and its L2.  Where the K/V heads can be dealt to the XCDs evenly, they are.
   const bool dealt = a.kv_heads % 8 == 0;
   const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
-  unsigned before = 0, places = 0, eights = 0;       // of the sequences before, one head's
+  unsigned before = 0, places = 0, joined = 0;       // of the sequences before, one head's
   bool found = false;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
     if (a.n_seqs > 64) look(s0 + lane);
     const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units;
-    const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, eight = chunks > 1 ? (unsigned)(s.n_new * a.group + 7) / 8 : 0;
-    const unsigned sum = before + wave_sums(items), cut_sum = places + wave_sums(cut), eight_sum = eights + wave_sums(eight);
+    const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, joint = chunks > 1 ? (unsigned)(s.n_new * a.group + JOINT<ROWS> - 1) / JOINT<ROWS> : 0;
+    const unsigned sum = before + wave_sums(items), cut_sum = places + wave_sums(cut), joint_sum = joined + wave_sums(joint);
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum <= at);
     if (!found && past != ~0ull) {                   // (a lane's sum only grows: the first lane that is beyond)
       const int l = __builtin_ctzll(~past);
@@ -161,15 +165,15 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
       w.chunk = (int)(x / (unsigned)w.tiles);
       w.tile = w.tiles - 1 - (int)(x % (unsigned)w.tiles);                 // (under a causal mask the last tile is the longest: it goes first)
       w.place = n > 1 ? (int)(((unsigned)pick((int)(cut_sum - cut)) * a.kv_heads + w.head * each) + x) : -1;
-      w.joint = (int)((unsigned)pick((int)(eight_sum - eight)) * a.kv_heads + w.head * (unsigned)pick((int)eight)) + w.tile * (ROWS / 8);
-      found = w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / 8 <= a.most_joints;
+      w.joint = (int)((unsigned)pick((int)(joint_sum - joint)) * a.kv_heads + w.head * (unsigned)pick((int)joint)) + w.tile * (ROWS / JOINT<ROWS>);
+      found = w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / JOINT<ROWS> <= a.most_joints;
       if (block != 0) return found;
     }
     before = (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
     places = (unsigned)__builtin_amdgcn_readlane((int)cut_sum, 63);
-    eights = (unsigned)__builtin_amdgcn_readlane((int)eight_sum, 63);
+    joined = (unsigned)__builtin_amdgcn_readlane((int)joint_sum, 63);
   }
-  if (block == 0 && threadIdx.x == 0) *joints_count(a) = (int)min(eights * (unsigned)a.kv_heads, (unsigned)a.most_joints);
+  if (block == 0 && threadIdx.x == 0) *joints_count(a) = (int)min(joined * (unsigned)a.kv_heads, (unsigned)a.most_joints);
   return found;
 }
 
@@ -205,10 +209,10 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
   static_assert(RW == 1 || KW == 1, "a wavefront without rows leaves here");
   if (row0 >= n_rows) return;
   const int all = tile_units<ROWS>(a, w), u0 = w.chunk * w.units;
-  if (w.place >= 0 && w.chunk == 0 && threadIdx.x < ROWS / 8) {
-    const int row = w.tile * ROWS + 8 * (int)threadIdx.x;
+  if (w.place >= 0 && w.chunk == 0 && threadIdx.x < ROWS / JOINT<ROWS>) {
+    const int row = w.tile * ROWS + JOINT<ROWS> * (int)threadIdx.x;
     if (row < n_rows)
-      joints(a)[w.joint + threadIdx.x] = {all > w.units ? (all + w.units - 1) / w.units : 0, w.place, w.tiles, row, min(n_rows - row, 8),
+      joints(a)[w.joint + threadIdx.x] = {all > w.units ? (all + w.units - 1) / w.units : 0, w.place, w.tiles, row, min(n_rows - row, JOINT<ROWS>),
                                           w.s.first, w.head, 0};
   }
   if (w.chunk > 0 && u0 >= all) return;                      // this tile ends before
@@ -663,8 +667,8 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
   }
 }
 
-// Adds the parts of the tiles that are cut.  A workgroup takes 8 rows at a time, 32 lanes to a row; where there are fewer rows,
-// 2, 4 or 8 times 32 lanes share the parts of one.
+// Adds the parts of the tiles that are cut.  A workgroup takes a joint at a time, 32 lanes to a row; where there are fewer than 8
+// rows, 2, 4 or 8 times 32 lanes share the parts of one.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Args a) {
   constexpr int E = D / 32, DEEP = 8;              // channels of a lane; parts asked for at a time
@@ -673,9 +677,11 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
   __shared__ fE sums[8][32];
   __shared__ float2 totals[8];
   const int half = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  // (the first joint is asked for beside their number: there is memory for it either way)
   const int count = *joints_count(a);
+  Joint j = joints(a)[blockIdx.x];
   for (int task = (int)blockIdx.x; task < count; task += (int)gridDim.x) {
-    const Joint j = joints(a)[task];
+    if (task != (int)blockIdx.x) j = joints(a)[task];
     if (j.parts == 0) continue;
     const int share = j.n_rows > 4 ? 0 : j.n_rows > 2 ? 1 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
     const bool there = r < j.n_rows;
@@ -739,7 +745,8 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
   const rf2_paged_config& c = plan->cfg;
   a.aimed = rf2_paged_parts_per_head(c.kv_heads);
   a.places = 2 * a.aimed * c.kv_heads;
-  a.most_joints = a.aimed * c.kv_heads * (RF2_PAGED_ROWS_MANY / 8);
+  a.most_joints = a.aimed * c.kv_heads * RF2_PAGED_JOINTS;
+  static_assert(ROWS / JOINT<ROWS> <= RF2_PAGED_JOINTS, "the workspace has room for so many to a tile");
   a.least = KW > 1 ? 16 : 8;
   // tiles there can be: a sequence has at most one that is not full
   const int64_t rows = (int64_t)a.n_tokens * a.group;
@@ -750,8 +757,8 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
   paged_attn_kernel<T, D, QT, RW, KW><<<dim3((unsigned)grid), dim3(64 * RW * KW), 0, st>>>(a);
   RF2_LAUNCH_CHECK();
   if (can_be_cut) {
-    const int64_t eights = std::min((int64_t)a.most_joints, (rows / 8 + std::min(a.n_seqs, a.n_tokens)) * c.kv_heads);
-    join_kernel<T, D, ROWS><<<dim3((unsigned)std::min(eights, (int64_t)1024)), dim3(256), 0, st>>>(a);
+    const int64_t joints = std::min((int64_t)a.most_joints, (rows / JOINT<ROWS> + std::min(a.n_seqs, a.n_tokens)) * c.kv_heads);
+    join_kernel<T, D, ROWS><<<dim3((unsigned)std::min(joints, (int64_t)1024)), dim3(256), 0, st>>>(a);
     RF2_LAUNCH_CHECK();
   }
   return RF2_OK;
@@ -759,8 +766,9 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
 
 template <class T, int D>
 int dispatch(const rf2_paged_plan* plan, const Args& a, hipStream_t st) {
-  // Up to 64 rows a sequence on average: one tile of 32 rows, four wavefronts share its keys.  More: two wavefronts of 64 rows.
-  if ((int64_t)a.n_tokens * a.group <= 64 * (int64_t)a.n_seqs) return launch<T, D, 1, 1, 4>(plan, a, st);
+  // Up to 32 rows a sequence on average, one tile: four wavefronts share its keys.  More: two wavefronts of 64 rows.  (16 sequences of
+  // 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 74.9 as one of 128; 128 rows: 131 and 97.)
+  if ((int64_t)a.n_tokens * a.group <= 32 * (int64_t)a.n_seqs) return launch<T, D, 1, 1, 4>(plan, a, st);
   return launch<T, D, 2, 2, 1>(plan, a, st);
 }
 
