@@ -140,7 +140,30 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
   // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
-  const int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
+  int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
+  if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
+    // Where tiles are long, how many of them and of their parts fill the chip's places (PLACES workgroups) counts.  Lane i holds what
+    // a launch takes with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more,
+    // in units; START more for a part's first loads and its last stores, and as much again where sums are written and joined.
+    constexpr float PLACES = 512.f, START = 8.f;
+    const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
+    const float per = 1.f / (float)mine;
+    float items = 0.f, cut = 0.f, longest = 0.f;
+    for (int i = 0; i < a.n_seqs; ++i) {
+      const float n = (float)__builtin_amdgcn_readlane(tiles, i), u = (float)__builtin_amdgcn_readlane(units_of(s.len), i);
+      const float c = ceilf(u * per);
+      items += n * c;
+      cut += c > 1.f ? n * c : 0.f;
+      longest = n > 0.f ? fmaxf(longest, fminf(u, (float)mine)) : longest;
+    }
+    const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
+    float cost = ceilf(items * heads / PLACES) * (mean + START * (1.f + cut / fmaxf(items, 1.f))) + (longest - mean);
+    float best = cost;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) best = fminf(best, __shfl_xor(best, d));
+    const uint64_t those = __builtin_amdgcn_ballot_w64(cost <= best);
+    units = __builtin_amdgcn_readlane(mine, those == 0 ? 63 : __builtin_ctzll(those));
+  }
   // Workgroups with equal number % 8 share an XCD and its L2.  Where the K/V heads can be dealt to the XCDs evenly, they are.
   const bool dealt = a.kv_heads % 8 == 0;
   const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
