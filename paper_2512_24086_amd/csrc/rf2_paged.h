@@ -15,8 +15,8 @@ constexpr int RF2_PAGED_MAX_SEQS = 4096;
 
 // Attention launches are cut into parts (rf2_paged_attn.hip): as many as this are aimed at, in all K/V heads together.
 constexpr int RF2_PAGED_PARTS = 1024;
-// Query rows of a workgroup: few rows to a sequence, and many.
-constexpr int RF2_PAGED_ROWS_FEW = 32, RF2_PAGED_ROWS_MANY = 128;
+// Query rows of a workgroup where a sequence has many (16 or 32 where it has few).
+constexpr int RF2_PAGED_ROWS_MANY = 128;
 // Groups of rows of a tile whose parts are added together (32 bytes each).
 constexpr int RF2_PAGED_JOINTS = 16;
 

@@ -30,6 +30,7 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 struct Bf16 {
@@ -40,6 +41,7 @@ struct Bf16 {
   // P = exp2(x - m): bf16 and fp32 carry 2^40 as well as 1
   static constexpr float RANGE = 1.0995e12f, HEAD = 0.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
   static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
 };
@@ -52,6 +54,7 @@ struct F16 {
   // 2^15, and what is rounded away below 2^-25 is 2^-33 of it
   static constexpr float RANGE = 32768.f, HEAD = 8.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
   static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
 };
@@ -119,7 +122,7 @@ __device__ __forceinline__ float2* part_stats(const Args& a, int place) {
 
 // Rows of a joint: a workgroup of join_kernel has 32 lanes for each, and more where there are few rows and many parts.
 template <int ROWS>
-constexpr int JOINT = ROWS == RF2_PAGED_ROWS_FEW ? 2 : 8;
+constexpr int JOINT = ROWS < RF2_PAGED_ROWS_MANY ? 2 : 8;
 
 // Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.
 // (Sums are of 32 bits: of rows there are at most 2^20 tokens.  Rows that overlap, which no table of this library has, may be left out.)
@@ -216,52 +219,115 @@ __device__ __forceinline__ const unsigned char* uniform_ptr(const void* p) {
   return (const unsigned char*)(((uint64_t)hi << 32) | lo);
 }
 
-__device__ __attribute__((aligned(16))) const unsigned char zeros[8192] = {};      // a tile
-
-// QT: tiles of 32 rows to a wavefront; RW wavefronts with rows of their own, times KW that share a part's keys.
-template <class T, int D, int QT, int RW, int KW>
-__global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kernel(Args a) {
-  constexpr int DS = D / 16, DT = D / 32, ROWS = 32 * QT * RW;
-  constexpr int WINDOW = KW > 1 ? 256 : 512;      // columns of the table that a wavefront has listed at a time
-  typedef typename T::x8 x8;
-  Part w;
-  if (!find_part<ROWS>(a, blockIdx.x, w)) return;
-  const int lane = (int)threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
-  const int wave = RW * KW > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, rw = wave / KW, kw = wave % KW;
-  const int n_rows = w.s.n_new * a.group, row0 = w.tile * ROWS + rw * 32 * QT;
-  static_assert(RW == 1 || KW == 1, "a wavefront without rows leaves here");
-  if (row0 >= n_rows) return;
+// What a wavefront of a part does.
+struct Span {
+  int n_rows, row0;               // rows of the sequence and K/V head; this wavefront's first
+  int begin, end;                 // its units
+  int free_units;                 // units that every row of it sees whole
+  int kv_head;
+  bool whole;                     // the tile has no other part
+};
+// Finds a wavefront's work: OWN rows of the ROWS of a tile from row `first` on, share kw of KW of the part's keys.
+template <int ROWS, int OWN, int KW>
+__device__ __forceinline__ bool enter(const Args& a, int first, int kw, Part& w, Span& p) {
+  if (!find_part<ROWS>(a, blockIdx.x, w)) return false;
+  p.n_rows = uniform(w.s.n_new * a.group);
+  p.row0 = uniform(w.tile * ROWS + first);
+  p.kv_head = uniform(w.head);
+  if (p.row0 >= p.n_rows) return false;
   const int all = tile_units<ROWS>(a, w), u0 = w.chunk * w.units;
   if (w.place >= 0 && w.chunk == 0 && threadIdx.x < ROWS / JOINT<ROWS>) {
     const int row = w.tile * ROWS + JOINT<ROWS> * (int)threadIdx.x;
-    if (row < n_rows)
-      joints(a)[w.joint + threadIdx.x] = {all > w.units ? (all + w.units - 1) / w.units : 0, w.place, w.tiles, row, min(n_rows - row, JOINT<ROWS>),
+    if (row < p.n_rows)
+      joints(a)[w.joint + threadIdx.x] = {all > w.units ? (all + w.units - 1) / w.units : 0, w.place, w.tiles, row, min(p.n_rows - row, JOINT<ROWS>),
                                           w.s.first, w.head, 0};
   }
-  if (w.chunk > 0 && u0 >= all) return;                      // this tile ends before
-  const bool whole = all <= w.units;                         // its only part: no other has to be added
-  const int last_row = min(row0 + 32 * QT, n_rows) - 1;
-  const int most = (limit_of(a, w.s, last_row) + 31) >> 5;    // units that a row of this wavefront sees
-  const int share = (min(u0 + w.units, all) - u0 + KW - 1) / KW;
-  const int begin = uniform(u0 + kw * share), end = uniform(min(min(begin + share, most), min(u0 + w.units, all)));
-  const int free_units = uniform(limit_of(a, w.s, row0) >> 5);         // units that every row sees whole
-  const int kv_head = uniform(w.head);
+  if (w.chunk > 0 && u0 >= all) return false;                // this tile ends before
+  p.whole = all <= w.units;
+  const int most = (limit_of(a, w.s, min(p.row0 + OWN, p.n_rows) - 1) + 31) >> 5;    // units that a row of this wavefront sees
+  const int u1 = min(u0 + w.units, all), share = (u1 - u0 + KW - 1) / KW;
+  p.begin = uniform(u0 + kw * share);
+  p.end = uniform(min(min(p.begin + share, most), u1));
+  p.free_units = uniform(limit_of(a, w.s, p.row0) >> 5);
+  return true;
+}
+
+// Pages of the columns p to p1 - 1 of a row of the table that exist, in order, with their columns: a wavefront's own list in LDS.
+// Unit x of the list is unit x % 2^unit_shift of page x / 2^unit_shift; units x0 to x1 - 1 are those from `begin` on and before `stop`.
+template <int WINDOW>
+__device__ __forceinline__ void list_pages(const Args& a, const int32_t* table, int2* pages, int p, int p1, int begin, int stop, int& x0, int& x1) {
+  const int lane = (int)threadIdx.x & 63;
+  int ids[WINDOW / 64], n = 0;
+#pragma unroll
+  for (int i = 0; i < WINDOW / 64; ++i) ids[i] = table[min(p + 64 * i + lane, a.max_pages - 1)];
+  wave_fence();
+#pragma unroll
+  for (int i = 0; i < WINDOW / 64; ++i) {
+    const bool there = p + 64 * i + lane < p1 && (unsigned)ids[i] < (unsigned)a.n_pages;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(there);
+    if (there) pages[n + __popcll(some & ((1ull << lane) - 1))] = make_int2(ids[i], p + 64 * i + lane);
+    n += __popcll(some);
+  }
+  wave_fence();
+  const int per = 1 << a.unit_shift;
+  x0 = n > 0 && uniform(pages[0].y) == begin >> a.unit_shift ? begin & (per - 1) : 0;
+  x1 = n * per;
+  if (n > 0 && uniform(pages[n - 1].y) == (stop - 1) >> a.unit_shift) x1 -= per - 1 - ((stop - 1) & (per - 1));
+}
+
+// Operands of a tile: buffer loads, the tile's address in scalar registers, a constant offset of the lane, and nothing past the
+// tile; of no tile (`there` false) they are zeros that are not fetched.
+template <int D>
+__device__ __forceinline__ int64_t tile_at(const Args& a, int kv_head, int u, int page) {
+  return (((int64_t)page * a.kv_heads + kv_head) * (1 << a.unit_shift) + (u & ((1 << a.unit_shift) - 1))) * (32 * D * 2);
+}
+template <int D>
+__device__ __forceinline__ auto tile_buffer(const void* cache, int64_t at, bool there) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)uniform_ptr((const unsigned char*)cache + at), 0, uniform(there ? 32 * D * 2 : 0), 0x00020000);
+}
+
+// V behind the last token of the sequence: 0 times whatever is there has to be 0.  A lane's eight keys of an operand are 4 from
+// the one that `left` keys are left of, and 4 from eight further.
+template <class x8>
+__device__ __forceinline__ x8 clear_behind(x8 v, int left) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int key = e / 2 * 8 + e % 2 * 2;
+    x[e] &= (key < left ? 0xffffu : 0u) | (key + 1 < left ? 0xffff0000u : 0u);
+  }
+  return __builtin_bit_cast(x8, x);
+}
+
+// 1 / l of a finished row; a row that sees no key yields zeros, one whose sum is not a number that.
+__device__ __forceinline__ float weight_of(float l) { return l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l); }
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(l)) * 0.6931471805599453f; }
+
+// Many rows: two wavefronts of 64 rows each (two tiles of 32) walk a part's keys.
+template <class T, int D>
+__global__ void __launch_bounds__(128, 1) many_attn_kernel(Args a) {
+  constexpr int DS = D / 16, DT = D / 32, ROWS = RF2_PAGED_ROWS_MANY;
+  constexpr int WINDOW = 512;      // columns of the table that a wavefront has listed at a time
+  typedef typename T::x8 x8;
+  const int wave = uniform((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, l32 = lane & 31, lh = lane >> 5;
+  Part w;
+  Span sp;
+  if (!enter<ROWS, 64, 1>(a, 64 * wave, 0, w, sp)) return;
 
   // this lane's rows: query column l32 of each tile (rows past the last stand for the last and are not written)
-  auto row_of = [&](int q) __attribute__((always_inline)) { return row0 + 32 * q + l32; };
-  x8 qf[QT][DS];
+  auto row_of = [&](int q) __attribute__((always_inline)) { return sp.row0 + 32 * q + l32; };
+  x8 qf[2][DS];
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    const int r = min(row_of(q), n_rows - 1), t = r / a.group, head = kv_head * a.group + r % a.group;
+  for (int q = 0; q < 2; ++q) {
+    const int r = min(row_of(q), sp.n_rows - 1), t = r / a.group, head = sp.kv_head * a.group + r % a.group;
     const typename T::x1* const from = (const typename T::x1*)a.q + (w.s.first + t) * a.q_stride + head * D + 8 * lh;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) qf[q][ds] = *reinterpret_cast<const x8*>(from + 16 * ds);
   }
-
-  f32x16 o[QT][DT];
-  float m[QT], l[QT];           // reference (in the exponent of 2), sum of the probabilities of this lane's keys
+  f32x16 o[2][DT];
+  float m[2], l[2];             // reference (in the exponent of 2), sum of the probabilities of this lane's keys
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
+  for (int q = 0; q < 2; ++q) {
     m[q] = -FLT_MAX;
     l[q] = 0.f;
 #pragma unroll
@@ -270,51 +336,25 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
       for (int i = 0; i < 16; ++i) o[q][dt][i] = 0.f;
   }
 
-  // Rows of a unit that a row does not see.
+  // Keys of unit u that a row does not see.
   auto mask = [&](f32x16& S, int q, int u) __attribute__((always_inline)) {
-    const int left = limit_of(a, w.s, min(row_of(q), n_rows - 1)) - 32 * u - 4 * lh;
+    const int left = limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - 4 * lh;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (8 * (i / 4) + i % 4 >= left) S[i] = -INFINITY;
   };
-  // V behind the last token: 0 times whatever is there has to be 0.  (The last unit of a sequence alone can have such keys.)
-  auto clear_v = [&](x8 (&v)[2 * DT], int u) __attribute__((always_inline)) {
-    if (32 * u + 32 <= w.s.len) return;
-#pragma unroll
-    for (int j = 0; j < 2 * DT; ++j) {
-      const int left = w.s.len - 32 * u - 16 * (j % 2) - 4 * lh;
-      u32x4 x = __builtin_bit_cast(u32x4, v[j]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = e / 2 * 8 + e % 2 * 2;
-        x[e] &= (key < left ? 0xffffu : 0u) | (key + 1 < left ? 0xffff0000u : 0u);
-      }
-      v[j] = __builtin_bit_cast(x8, x);
-    }
-  };
-  auto tile_at = [&](int u, int page) __attribute__((always_inline)) {      // byte offset of a unit's tile in either cache
-    return (((int64_t)page * a.kv_heads + kv_head) * (1 << a.unit_shift) + (u & ((1 << a.unit_shift) - 1))) * (32 * D * 2);
-  };
-  // Operands of a tile: buffer loads, the tile's address in scalar registers, a constant offset of the lane, and nothing past the tile.
-  // Few rows to a sequence: a tile is read once, or a few times at once, and then not for long, so its loads are marked as not to
-  // be kept (64 single tokens over 0.79 GB of keys and values 149.7 -> 137.4 us).
-  constexpr int ONCE = KW > 1 ? 2 : 0;
-  constexpr unsigned TILE = 32 * D * 2;
   const uint32_t k_lane = (uint32_t)lane * 16, v_lane = (uint32_t)(lh * D + l32) * 16;
-  auto buffer = [](const unsigned char* tile) __attribute__((always_inline)) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)uniform_ptr(tile), 0, TILE, 0x00020000);
-  };
   auto k_load = [&](auto tile, int c) __attribute__((always_inline)) {
-    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + c % 4 * 1024, c / 4 * 4096, ONCE));
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + c % 4 * 1024, c / 4 * 4096, 0));
   };
   auto v_load = [&](auto tile, int j) __attribute__((always_inline)) {
-    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + j / 2 * 512, j % 2 * (2 * D * 16), ONCE));
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + j / 2 * 512, j % 2 * (2 * D * 16), 0));
   };
   auto operand_p = [](const uint32_t (&P)[8], int ks) __attribute__((always_inline)) {
     const u32x4 x = {P[4 * ks], P[4 * ks + 1], P[4 * ks + 2], P[4 * ks + 3]};
     return __builtin_bit_cast(x8, x);
   };
-  // The reference of tile q moves to the largest exponent of S, if that is larger; what has been summed is rescaled.
+  // The reference of tile q moves to the largest exponent of S, if that is larger; returns what has been summed is to be scaled by.
   auto move_reference = [&](int q, const f32x16& S) __attribute__((always_inline)) {
     float top = S[0];
 #pragma unroll
@@ -336,344 +376,212 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
     }
     return sum;
   };
-  // Pages of the columns p to p1 - 1 of the table that exist, in order, with their columns; a wavefront's own list.  Unit x of the
-  // list is unit x % 2^unit_shift of page x / 2^unit_shift; units x0 to x1 - 1 are those from `begin` on and before `stop`.
   const int32_t* const table = a.table + (int64_t)uniform(w.seq) * a.max_pages;
-  __shared__ int2 page_lists[RW * KW][WINDOW];
+  __shared__ int2 page_lists[2][WINDOW];
   int2* const pages = page_lists[wave];
-  auto list_pages = [&](int p, int p1, int from, int stop, int& x0, int& x1) __attribute__((always_inline)) {
-    int ids[WINDOW / 64], n = 0;
+  constexpr int NQ = DS, NP = 2 * DT, PAIRS = 16 / (NQ + NP);
+  x8 kr[2][NQ], vr[2][NP];
+  float last[2] = {};                      // sums of the latest unit, still to be added to l
+  // O of tile q times alpha.  In accumulation registers it is scaled where it is, through one vector register (left to the
+  // compiler, the copies cost the registers of the loop); the wait states cover a product in flight and one that follows.
+  auto rescale = [&](int q, float alpha) __attribute__((always_inline)) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < WINDOW / 64; ++i) ids[i] = table[min(p + 64 * i + lane, a.max_pages - 1)];
-    wave_fence();
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < WINDOW / 64; ++i) {
-      const bool there = p + 64 * i + lane < p1 && (unsigned)ids[i] < (unsigned)a.n_pages;
-      const uint64_t some = __builtin_amdgcn_ballot_w64(there);
-      if (there) pages[n + __popcll(some & ((1ull << lane) - 1))] = make_int2(ids[i], p + 64 * i + lane);
-      n += __popcll(some);
-    }
-    wave_fence();
-    const int per = 1 << a.unit_shift;
-    x0 = n > 0 && uniform(pages[0].y) == from >> a.unit_shift ? from & (per - 1) : 0;
-    x1 = n * per;
-    if (n > 0 && uniform(pages[n - 1].y) == (stop - 1) >> a.unit_shift) x1 -= per - 1 - ((stop - 1) & (per - 1));
+      for (int i = 0; i < 16; ++i) {
+        float x = o[q][dt][i], t;
+        asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
+                     : "+a"(x), "=&v"(t) : "v"(alpha));
+        o[q][dt][i] = x;
+      }
+    asm volatile("s_nop 7" ::: "memory");
   };
-  if constexpr (QT == 2) {
-    constexpr int NQ = DS, NP = 2 * DT, PAIRS = 16 / (NQ + NP);
-    x8 kr[2][NQ], vr[2][NP];
-    float last[2] = {};                      // sums of the latest unit, still to be added to l
-    // O of tile q times alpha.  In accumulation registers it is scaled where it is, through one vector register (left to the
-    // compiler, the copies cost the registers of the loop); the wait states cover a product in flight and one that follows.
-    auto rescale = [&](int q, float alpha) __attribute__((always_inline)) {
-      asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  // Step: S of the next unit, O += V P of the one before, the softmax arithmetic of the present one, operand by operand.  The
+  // operands' registers are loaded again as soon as both MFMAs that read them are issued: K at k_at, V at v_at.
+  auto step = [&](auto odd, f32x16 (&Scur)[2], f32x16 (&Snext)[2], uint32_t (&Pprev)[2][8], uint32_t (&Pcur)[2][8], auto kb, auto vb,
+                  int u_next) __attribute__((always_inline)) {
+    constexpr int B = decltype(odd)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    float rs[2] = {}, e0[PAIRS], e1[PAIRS];
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+    for (int g = 0; g < NQ + NP; ++g) {
+      const int j = g - NQ;
+      if (g % 2 == 0) {                    // (one wait for two operands)
+        if (g < NQ) asm volatile("" ::"v"(kr[B][g + 1]));
+        else asm volatile("" ::"v"(vr[B][j + 1]));
+      }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x = o[q][dt][i], t;
-          asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
-                       : "+a"(x), "=&v"(t) : "v"(alpha));
-          o[q][dt][i] = x;
+      for (int q = 0; q < 2; ++q) {
+        if (g < NQ) {
+          if (g == 0) T::first(Snext[q], kr[B][g], qf[q][g]);
+          else T::more(Snext[q], kr[B][g], qf[q][g]);
+        } else {
+          o[q][j / 2] = T::mfma(vr[B][j], operand_p(Pprev[q], j % 2), o[q][j / 2]);
         }
-      asm volatile("s_nop 7" ::: "memory");
-    };
-    // Step: S of the next unit, O += V P of the one before, the softmax arithmetic of the present one, operand by operand.  The
-    // operands' registers are loaded again as soon as both MFMAs that read them are issued: K at k_at, V at v_at.
-    auto step = [&](auto odd, f32x16 (&Scur)[2], f32x16 (&Snext)[2], uint32_t (&Pprev)[2][8], uint32_t (&Pcur)[2][8], const unsigned char* k_at, const unsigned char* v_at,
-                    int u_next) __attribute__((always_inline)) {
-      constexpr int B = decltype(odd)::value;
-      const auto kb = buffer(k_at), vb = buffer(v_at);
-      __builtin_amdgcn_sched_barrier(0);
-      float rs[2] = {}, e0[PAIRS], e1[PAIRS];
+        __builtin_amdgcn_sched_barrier(0);
+        if (q == 0) {
 #pragma unroll
-      for (int g = 0; g < NQ + NP; ++g) {
-        const int j = g - NQ;
-        if (g % 2 == 0) {                    // (one wait for two operands)
-          if (g < NQ) asm volatile("" ::"v"(kr[B][g + 1]));
-          else asm volatile("" ::"v"(vr[B][j + 1]));
+          for (int p = 0; p < PAIRS; ++p) {
+            const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
+            e0[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i], a.scale_log2, -m[tile]));
+            e1[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i + 1], a.scale_log2, -m[tile]));
+            asm volatile("" : "+v"(e0[p]), "+v"(e1[p]));
+          }
+        } else {
+          if (g < NQ) kr[B][g] = k_load(kb, g);
+          else vr[B][j] = v_load(vb, j);
+          asm volatile("" ::: "memory");   // (the load stays here)
+#pragma unroll
+          for (int p = 0; p < PAIRS; ++p) {
+            const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
+            const typename T::x2 pk = {(typename T::x1)e0[p], (typename T::x1)e1[p]};
+            uint32_t word = __builtin_bit_cast(uint32_t, pk);
+            rs[tile] = i == 0 ? e0[p] + e1[p] : rs[tile] + (e0[p] + e1[p]);
+            asm volatile("" : "+v"(word), "+v"(rs[tile]));
+            Pcur[tile][i / 2] = word;
+            if (i == 0) {
+              l[tile] += last[tile];
+              asm volatile("" : "+v"(l[tile]));
+            }
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    last[0] = rs[0];
+    last[1] = rs[1];
+    // One branch, hardly ever taken: the present unit is out of range, or rows do not see all of the next one.
+    // (the limit is an integer select: as a float one it would be two branches, and the step twice)
+    int bound = u_next >= sp.free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
+    asm volatile("" : "+s"(bound));
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
+      if (__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= T::RANGE)) != 0ull)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          if (g < NQ) {
-            if (g == 0) T::first(Snext[q], kr[B][g], qf[q][g]);
-            else T::more(Snext[q], kr[B][g], qf[q][g]);
-          } else {
-            o[q][j / 2] = T::mfma(vr[B][j], operand_p(Pprev[q], j % 2), o[q][j / 2]);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-          if (q == 0) {
-#pragma unroll
-            for (int p = 0; p < PAIRS; ++p) {
-              const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
-              e0[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i], a.scale_log2, -m[tile]));
-              e1[p] = __builtin_amdgcn_exp2f(fmaf(Scur[tile][i + 1], a.scale_log2, -m[tile]));
-              asm volatile("" : "+v"(e0[p]), "+v"(e1[p]));
-            }
-          } else {
-            if (g < NQ) kr[B][g] = k_load(kb, g);
-            else vr[B][j] = v_load(vb, j);
-            asm volatile("" ::: "memory");   // (the load stays here)
-#pragma unroll
-            for (int p = 0; p < PAIRS; ++p) {
-              const int x = g * PAIRS + p, tile = x / 8, i = 2 * (x % 8);
-              const typename T::x2 pk = {(typename T::x1)e0[p], (typename T::x1)e1[p]};
-              uint32_t word = __builtin_bit_cast(uint32_t, pk);
-              rs[tile] = i == 0 ? e0[p] + e1[p] : rs[tile] + (e0[p] + e1[p]);
-              asm volatile("" : "+v"(word), "+v"(rs[tile]));
-              Pcur[tile][i / 2] = word;
-              if (i == 0) {
-                l[tile] += last[tile];
-                asm volatile("" : "+v"(l[tile]));
-              }
-            }
-          }
-          __builtin_amdgcn_sched_barrier(0);
+          const float alpha = move_reference(q, Scur[q]);
+          l[q] *= alpha;
+          rescale(q, alpha);
+          last[q] = probabilities(q, Scur[q], Pcur[q]);
         }
-      }
-      last[0] = rs[0];
-      last[1] = rs[1];
-      // One branch, hardly ever taken: the present unit is out of range, or rows do not see all of the next one.
-      // (the limit is an integer select: as a float one it would be two branches, and the step twice)
-      int bound = u_next >= free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
-      asm volatile("" : "+s"(bound));
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
-        if (__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= T::RANGE)) != 0ull)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const float alpha = move_reference(q, Scur[q]);
-            l[q] *= alpha;
-            rescale(q, alpha);
-            last[q] = probabilities(q, Scur[q], Pcur[q]);
-          }
-        if (u_next >= free_units) mask(Snext[0], 0, u_next), mask(Snext[1], 1, u_next);
-      }
-    };
-    // Units x0 to x1 - 1 of the list (behind unit `lead` of page `lead_page`, where there is one).
-    auto walk = [&](int x0, int x1, int lead, int lead_page, bool begins) __attribute__((always_inline)) {
-      // units s to s + 3 and their tiles; past the last one: none, in a tile of zeros
-      constexpr int NONE = 1 << 25;
-      int us[4], x = x0;
-      const unsigned char *k_at[4], *v_at[4];
-      auto fetch = [&](int i, int u, int page) __attribute__((always_inline)) {
-        const int64_t at = tile_at(u, page);
-        us[i] = u;
-        k_at[i] = (const unsigned char*)a.k_cache + at;
-        v_at[i] = (const unsigned char*)a.v_cache + at;
-      };
-      int2 entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];       // of unit x, read a step before it is turned into addresses
-      auto following = [&](int i) __attribute__((always_inline)) {
-        const int page = uniform(entry.x), u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
-        const int64_t at = tile_at(u, page);
-        const bool there = x < x1;
-        us[i] = there ? u : NONE;
-        k_at[i] = there ? (const unsigned char*)a.k_cache + at : zeros;
-        v_at[i] = there ? (const unsigned char*)a.v_cache + at : zeros;
-        ++x;
-        entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];
-      };
-      auto shift = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) us[i] = us[i + 1], k_at[i] = k_at[i + 1], v_at[i] = v_at[i + 1];
-      };
-      if (lead >= 0) fetch(0, lead, lead_page);
-      else following(0);
-      following(1);
-      following(2);
-      x8 k0[NQ];
-#pragma unroll
-      for (int c = 0; c < NQ; ++c) k0[c] = k_load(buffer(k_at[0]), c);
-#pragma unroll
-      for (int c = 0; c < NQ; ++c) kr[0][c] = k_load(buffer(k_at[1]), c);
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int c = 0; c < NQ; ++c) kr[1][c] = k_load(buffer(k_at[2]), c);
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        vr[1][j] = v_load(buffer(v_at[0]), j);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vr[0][j][e] = (typename T::x1)0.f;     // step 0 has no unit before it: it adds 0 x 0
-      }
-      f32x16 Sa[2], Sb[2];
-      uint32_t Pa[2][8], Pb[2][8];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-#pragma unroll
-        for (int ds = 0; ds < DS; ++ds) {
-          if (ds == 0) T::first(Sa[q], k0[ds], qf[q][ds]);
-          else T::more(Sa[q], k0[ds], qf[q][ds]);
-        }
-        asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(Sa[q]));
-        if (us[0] >= free_units) mask(Sa[q], q, us[0]);
-        if (begins) (void)move_reference(q, Sa[q]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) Pb[q][e] = 0u;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) Sb[q][i] = 0.f;
-      }
-      if (lead >= 0) clear_v(vr[1], lead);
-      // (arrived before the loop, whose waits would else be those of its first round)
-#pragma unroll
-      for (int c = 0; c < NQ; ++c) asm volatile("" : "+v"(kr[0][c]));
-      // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
-      do {
-        following(3);
-        step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_at[3], v_at[1], us[1]);
-        shift();
-        following(3);
-        step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_at[3], v_at[1], us[1]);
-        shift();
-      } while (us[0] != NONE);
-      // last product
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        l[q] += last[q];
-        last[q] = 0.f;
-#pragma unroll
-        for (int j = 0; j < NP; ++j) o[q][j / 2] = T::mfma(vr[0][j], operand_p(Pb[q], j % 2), o[q][j / 2]);
-      }
-    };
-    // The last unit of a sequence can have keys behind its last token, whose V has to be cleared: it goes first, so that no step
-    // has to look for it.
-    int stop = end, lead = -1, lead_page = 0;
-    if (begin < end && 32 * end > w.s.len) {
-      stop = end - 1;
-      lead_page = uniform(table[stop >> a.unit_shift]);
-      lead = (unsigned)lead_page < (unsigned)a.n_pages ? stop : -1;
+      if (u_next >= sp.free_units) mask(Snext[0], 0, u_next), mask(Snext[1], 1, u_next);
     }
-    bool begins = true;
-    for (int p = begin >> a.unit_shift, p1 = (stop + (1 << a.unit_shift) - 1) >> a.unit_shift; p < p1 || lead >= 0; p += WINDOW) {
-      int x0, x1;
-      list_pages(p, min(p + WINDOW, p1), begin, stop, x0, x1);
-      if (x0 < x1 || lead >= 0) {
-        walk(x0, x1, lead, lead_page, begins);
-        begins = false;
-        lead = -1;
-      }
+  };
+  // Units x0 to x1 - 1 of the list (behind unit `lead` of page `lead_page`, where there is one).
+  auto walk = [&](int x0, int x1, int lead, int lead_page, bool begins) __attribute__((always_inline)) {
+    // Units s to s + 3 and where they lie in either cache; past the last one none.
+    constexpr int NONE = 1 << 25;
+    int us[4], x = x0;
+    int64_t at[4];
+    int2 entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];       // of unit x, read a step before it is used
+    auto following = [&](int i) __attribute__((always_inline)) {
+      const int u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
+      at[i] = tile_at<D>(a, sp.kv_head, u, uniform(entry.x));
+      us[i] = x < x1 ? u : NONE;
+      ++x;
+      entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];
+    };
+    auto shift = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) us[i] = us[i + 1], at[i] = at[i + 1];
+    };
+    auto k_of = [&](int i) __attribute__((always_inline)) { return tile_buffer<D>(a.k_cache, at[i], us[i] != NONE); };
+    auto v_of = [&](int i) __attribute__((always_inline)) { return tile_buffer<D>(a.v_cache, at[i], us[i] != NONE); };
+    if (lead >= 0) us[0] = lead, at[0] = tile_at<D>(a, sp.kv_head, lead, lead_page);
+    else following(0);
+    following(1);
+    following(2);
+    x8 k0[NQ];
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) k0[c] = k_load(k_of(0), c);
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) kr[0][c] = k_load(k_of(1), c);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) kr[1][c] = k_load(k_of(2), c);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      vr[1][j] = v_load(v_of(0), j);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vr[0][j][e] = (typename T::x1)0.f;     // step 0 has no unit before it: it adds 0 x 0
     }
-  } else {
-    x8 kr[2][DS], vr[2 * DT];
-    auto load = [&](auto odd, int x, int& u) __attribute__((always_inline)) {
-      const int2 entry = pages[x >> a.unit_shift];
-      u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
-      const int64_t at = tile_at(u, uniform(entry.x));
-      const auto kb = buffer((const unsigned char*)a.k_cache + at);
+    f32x16 Sa[2], Sb[2];
+    uint32_t Pa[2][8], Pb[2][8];
 #pragma unroll
-      for (int c = 0; c < DS; ++c) kr[decltype(odd)::value][c] = k_load(kb, c);
-      return (const unsigned char*)a.v_cache + at;
-    };
-    auto load_v = [&](const unsigned char* at) __attribute__((always_inline)) {
-      const auto vb = buffer(at);
+    for (int q = 0; q < 2; ++q) {
 #pragma unroll
-      for (int j = 0; j < 2 * DT; ++j) vr[j] = v_load(vb, j);
-    };
-    // Unit u, whose K is in registers B.
-    auto unit = [&](auto odd, int u) __attribute__((always_inline)) {
-      constexpr int B = decltype(odd)::value;
-      f32x16 S;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) S[i] = 0.f;
-#pragma unroll
-      for (int ds = 0; ds < DS; ++ds) S = T::mfma(kr[B][ds], qf[0][ds], S);
-      if (u >= free_units) mask(S, 0, u);
-      clear_v(vr, u);
-      uint32_t P[8];
-      float sum = probabilities(0, S, P);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= T::RANGE)) != 0ull, 0)) {
-        const float alpha = move_reference(0, S);
-        l[0] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[0][dt][i] *= alpha;
-        sum = probabilities(0, S, P);
+      for (int ds = 0; ds < DS; ++ds) {
+        if (ds == 0) T::first(Sa[q], k0[ds], qf[q][ds]);
+        else T::more(Sa[q], k0[ds], qf[q][ds]);
       }
-      l[0] += sum;
+      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(Sa[q]));
+      if (us[0] >= sp.free_units) mask(Sa[q], q, us[0]);
+      if (begins) (void)move_reference(q, Sa[q]);
 #pragma unroll
-      for (int j = 0; j < 2 * DT; ++j) o[0][j / 2] = T::mfma(vr[j], operand_p(P, j % 2), o[0][j / 2]);
-    };
-    for (int p = begin >> a.unit_shift, p1 = (end + (1 << a.unit_shift) - 1) >> a.unit_shift; begin < end && p < p1; p += WINDOW) {
-      int x, x1, ua, ub;
-      list_pages(p, min(p + WINDOW, p1), begin, end, x, x1);
-      if (x >= x1) continue;
-      const unsigned char* va = load(std::integral_constant<int, 0>{}, x, ua);
-      // (past the last unit it is fetched again: no branch stands between a load and its use)
-      while (true) {
-        load_v(va);
-        const unsigned char* const vb = load(std::integral_constant<int, 1>{}, min(x + 1, x1 - 1), ub);
-        unit(std::integral_constant<int, 0>{}, ua);
-        if (++x >= x1) break;
-        load_v(vb);
-        va = load(std::integral_constant<int, 0>{}, min(x + 1, x1 - 1), ua);
-        unit(std::integral_constant<int, 1>{}, ub);
-        if (++x >= x1) break;
-      }
+      for (int e = 0; e < 8; ++e) Pb[q][e] = 0u;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) Sb[q][i] = 0.f;
+    }
+    if (lead >= 0)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) vr[1][j] = clear_behind(vr[1][j], w.s.len - 32 * lead - 16 * (j % 2) - 4 * lh);
+    // (arrived before the loop, whose waits would else be those of its first round)
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) asm volatile("" : "+v"(kr[0][c]));
+    // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
+    do {
+      following(3);
+      step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_of(3), v_of(1), us[1]);
+      shift();
+      following(3);
+      step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_of(3), v_of(1), us[1]);
+      shift();
+    } while (us[0] != NONE);
+    // last product
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      l[q] += last[q];
+      last[q] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) o[q][j / 2] = T::mfma(vr[0][j], operand_p(Pb[q], j % 2), o[q][j / 2]);
+    }
+  };
+  // The last unit of a sequence can have keys behind its last token, whose V has to be cleared: it goes first, so that no step
+  // has to look for it.
+  int stop = sp.end, lead = -1, lead_page = 0;
+  if (sp.begin < sp.end && 32 * sp.end > w.s.len) {
+    stop = sp.end - 1;
+    lead_page = uniform(table[stop >> a.unit_shift]);
+    lead = (unsigned)lead_page < (unsigned)a.n_pages ? stop : -1;
+  }
+  bool begins = true;
+  for (int p = sp.begin >> a.unit_shift, p1 = (stop + (1 << a.unit_shift) - 1) >> a.unit_shift; p < p1 || lead >= 0; p += WINDOW) {
+    int x0, x1;
+    list_pages<WINDOW>(a, table, pages, p, min(p + WINDOW, p1), sp.begin, stop, x0, x1);
+    if (x0 < x1 || lead >= 0) {
+      walk(x0, x1, lead, lead_page, begins);
+      begins = false;
+      lead = -1;
     }
   }
 
-  // sums of the two lane halves, which have different keys of a row
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
+  for (int q = 0; q < 2; ++q) {
+    // sums of the two lane halves, which have different keys of a row
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[q]), __float_as_uint(l[q]), false, false);
     l[q] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  }
-  // Wavefronts that share the keys: each finishes the channels of one tile of O (those beyond DT none).
-  if constexpr (KW > 1) {
-    static_assert(QT == 1 && KW >= DT, "a tile to a wavefront");
-    __shared__ float4 tiles[KW][DT][4][64];
-    __shared__ float2 stats[KW][32];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      if (dt != kw)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          tiles[kw][dt][g][lane] = make_float4(o[0][dt][4 * g], o[0][dt][4 * g + 1], o[0][dt][4 * g + 2], o[0][dt][4 * g + 3]);
-    if (lh == 0) stats[kw][l32] = make_float2(m[0], l[0]);
-    __syncthreads();
-    float top = m[0], sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < KW; ++k) top = fmaxf(top, stats[k][l32].x);
-    const float own = __builtin_amdgcn_exp2f(m[0] - top);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      if (dt == kw)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[0][dt][i] *= own;
-#pragma unroll
-    for (int k = 0; k < KW; ++k) {
-      const float2 st = stats[k][l32];
-      const float weight = __builtin_amdgcn_exp2f(st.x - top);
-      sum = fmaf(st.y, weight, sum);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        if (dt == kw && k != kw)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 x = tiles[k][dt][g][lane];
-            o[0][dt][4 * g] = fmaf(x.x, weight, o[0][dt][4 * g]);
-            o[0][dt][4 * g + 1] = fmaf(x.y, weight, o[0][dt][4 * g + 1]);
-            o[0][dt][4 * g + 2] = fmaf(x.z, weight, o[0][dt][4 * g + 2]);
-            o[0][dt][4 * g + 3] = fmaf(x.w, weight, o[0][dt][4 * g + 3]);
-          }
-    }
-    m[0] = top;
-    l[0] = sum;
-  }
-#pragma unroll
-  for (int q = 0; q < QT; ++q) {
     const int r = row_of(q) - w.tile * ROWS;
-    if (row_of(q) >= n_rows) continue;
-    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + kv_head * a.group + row_of(q) % a.group;
-    const float f = whole ? (l[q] > 0.f ? 1.0f / l[q] : (l[q] == 0.f ? 0.f : l[q])) : 1.0f;     // a row that sees no key yields zeros
+    if (row_of(q) >= sp.n_rows) continue;
+    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + sp.kv_head * a.group + row_of(q) % a.group;
+    const float f = weight_of(l[q]);
     float* const part = part_sums<ROWS, D>(a, w.place) + r * D;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      if (KW > 1 && dt != kw) continue;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int ch = 32 * dt + 8 * g + 4 * lh;
-        if (whole) {
+        if (sp.whole) {
           typename T::x4 pk;
 #pragma unroll
           for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(o[q][dt][4 * g + e] * f);
@@ -682,10 +590,217 @@ __global__ void __launch_bounds__(64 * RW * KW, QT == 1 ? 2 : 1) paged_attn_kern
           *reinterpret_cast<float4*>(part + ch) = make_float4(o[q][dt][4 * g], o[q][dt][4 * g + 1], o[q][dt][4 * g + 2], o[q][dt][4 * g + 3]);
         }
       }
+    if (lh == 0) {
+      if (!sp.whole) part_stats<ROWS, D>(a, w.place)[r] = make_float2(m[q], l[q]);
+      else if (a.lse != nullptr) a.lse[out_row] = lse_of(m[q], l[q]);
     }
-    if (lh == 0 && kw == 0) {
-      if (!whole) part_stats<ROWS, D>(a, w.place)[r] = make_float2(m[q], l[q]);
-      else if (a.lse != nullptr) a.lse[out_row] = (m[q] + __log2f(l[q])) * 0.6931471805599453f;
+  }
+}
+
+// Few rows: QT tiles of 16, whose keys four wavefronts share (v_mfma_f32_16x16x32).  A product of 16 keys takes the keys of a unit
+// that S^T's accumulators then hold as V^T's storage groups have them: rows 4 i + e of the first are keys 0-3, 4-7, 16-19, 20-23, those
+// of the second eight more, and a lane's eight probabilities are the eight keys of storage group lane / 16.
+//
+// Bound by memory: operands of two units are on their way (each is asked for as soon as the one two before has been read).
+template <class T, int D, int QT>
+__global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
+  constexpr int KW = 4, CS = D / 32, CT = D / 16, ROWS = 16 * QT;
+  constexpr int WINDOW = 256;      // columns of the table that a wavefront has listed at a time
+  typedef typename T::x8 x8;
+  const int kw = uniform((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+  Part w;
+  Span sp;
+  if (!enter<ROWS, ROWS, KW>(a, 0, kw, w, sp)) return;
+
+  auto row_of = [&](int q) __attribute__((always_inline)) { return sp.row0 + 16 * q + l16; };
+  x8 qf[QT][CS];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    const int r = min(row_of(q), sp.n_rows - 1), t = r / a.group, head = sp.kv_head * a.group + r % a.group;
+    const typename T::x1* const from = (const typename T::x1*)a.q + (w.s.first + t) * a.q_stride + head * D + 8 * lq;
+#pragma unroll
+    for (int cs = 0; cs < CS; ++cs) qf[q][cs] = *reinterpret_cast<const x8*>(from + 32 * cs);
+  }
+  f32x4 o[QT][CT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    m[q] = -FLT_MAX;
+    l[q] = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) o[q][ct] = (f32x4)0.f;
+  }
+  const int key0 = (lq & 1) * 4 + (lq >> 1) * 16;                     // first of this lane's keys of a unit (the other four: 8 further)
+  const uint32_t k_lane = (uint32_t)(lq * 512 + ((l16 & 7) + (l16 >> 3) * 16) * 16), v_lane = (uint32_t)(lq * D + l16) * 16;
+  // Tiles are read once, or a few times at the same time, and then not for long: the loads are marked as not to be kept (64 single
+  // tokens over 0.79 GB of keys and values 149.7 -> 137.4 us).
+  constexpr int ONCE = 2;
+  auto k_load = [&](auto tile, int t, int cs) __attribute__((always_inline)) {
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, k_lane + t * 128 + cs % 2 * 2048, cs / 2 * 4096, ONCE));
+  };
+  auto v_load = [&](auto tile, int ct) __attribute__((always_inline)) {
+    return __builtin_bit_cast(x8, __builtin_amdgcn_raw_buffer_load_b128(tile, v_lane + ct * 256, 0, ONCE));
+  };
+  const int32_t* const table = a.table + (int64_t)uniform(w.seq) * a.max_pages;
+  __shared__ int2 page_lists[KW][WINDOW];
+  int2* const pages = page_lists[kw];
+  constexpr int AHEAD = QT == 2 && D == 128 ? 1 : 2;      // units that V is asked for ahead: what registers there are for
+  x8 kr[2][2][CS], vr[AHEAD][CT];
+  int us[2];
+  for (int p = sp.begin >> a.unit_shift, p1 = (sp.end + (1 << a.unit_shift) - 1) >> a.unit_shift; sp.begin < sp.end && p < p1; p += WINDOW) {
+    int x0, x1;
+    list_pages<WINDOW>(a, table, pages, p, min(p + WINDOW, p1), sp.begin, sp.end, x0, x1);
+    if (x0 >= x1) continue;
+    int64_t at[2];
+    auto place = [&](int x, int& u, int64_t& at) __attribute__((always_inline)) {
+      const int2 entry = pages[min(x, x1 - 1) >> a.unit_shift];
+      u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
+      at = tile_at<D>(a, sp.kv_head, u, uniform(entry.x));
+    };
+    // unit x, whose place is held in us and at
+    auto fetch_k = [&](auto odd, int x) __attribute__((always_inline)) {
+      const auto kb = tile_buffer<D>(a.k_cache, at[decltype(odd)::value], x < x1);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs) kr[decltype(odd)::value][t][cs] = k_load(kb, t, cs);
+      asm volatile("" ::: "memory");
+    };
+    auto fetch_v = [&](auto odd, int x) __attribute__((always_inline)) {
+      const auto vb = tile_buffer<D>(a.v_cache, at[decltype(odd)::value], x < x1);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) vr[decltype(odd)::value % AHEAD][ct] = v_load(vb, ct);
+      asm volatile("" ::: "memory");
+    };
+    auto unit = [&](auto odd, int x) __attribute__((always_inline)) {
+      constexpr int B = decltype(odd)::value;
+      const int u = us[B];
+      place(x + 2, us[B], at[B]);
+      f32x4 S[QT][2];
+#pragma unroll
+      for (int q = 0; q < QT; ++q)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          S[q][t] = (f32x4)0.f;
+#pragma unroll
+          for (int cs = 0; cs < CS; ++cs) S[q][t] = T::mfma16(kr[B][t][cs], qf[q][cs], S[q][t]);
+        }
+      fetch_k(odd, x + 2);
+      x8 P[QT];
+#pragma unroll
+      for (int q = 0; q < QT; ++q) {
+        if (u >= sp.free_units) {                            // keys that a row does not see
+          const int left = limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - key0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (8 * (i / 4) + i % 4 >= left) S[q][i / 4][i % 4] = -INFINITY;
+        }
+        float sum;
+        auto probabilities = [&]() __attribute__((always_inline)) {
+          sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(S[q][i / 4][i % 4], a.scale_log2, -m[q]));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(S[q][i / 4][i % 4 + 1], a.scale_log2, -m[q]));
+            P[q][i] = (typename T::x1)p0;
+            P[q][i + 1] = (typename T::x1)p1;
+            sum += p0 + p1;
+          }
+        };
+        probabilities();
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= T::RANGE)) != 0ull, 0)) {
+          // Out of range, or the first unit with a key: the reference moves to the largest exponent, what is there is rescaled.
+          float top = S[q][0][0];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) top = fmaxf(top, S[q][i / 4][i % 4]);
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          top = fmaxf(top * a.scale_log2 - T::HEAD, -FLT_MAX);
+          const float to = fmaxf(m[q], top), alpha = __builtin_amdgcn_exp2f(m[q] - to);
+          m[q] = to;
+          l[q] *= alpha;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[q][ct] *= alpha;
+          probabilities();
+        }
+        l[q] += sum;
+      }
+      if (32 * u + 32 > w.s.len)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) vr[B % AHEAD][ct] = clear_behind(vr[B % AHEAD][ct], w.s.len - 32 * u - key0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int q = 0; q < QT; ++q) o[q][ct] = T::mfma16(vr[B % AHEAD][ct], P[q], o[q][ct]);
+      fetch_v(std::integral_constant<int, (B + AHEAD) % 2>{}, x + AHEAD);
+    };
+    place(x0, us[0], at[0]);
+    place(x0 + 1, us[1], at[1]);
+    fetch_k(std::integral_constant<int, 0>{}, x0);
+    fetch_v(std::integral_constant<int, 0>{}, x0);
+    fetch_k(std::integral_constant<int, 1>{}, x0 + 1);
+    if constexpr (AHEAD == 2) fetch_v(std::integral_constant<int, 1>{}, x0 + 1);
+    for (int x = x0;; x += 2) {
+      unit(std::integral_constant<int, 0>{}, x);
+      if (x + 1 >= x1) break;
+      unit(std::integral_constant<int, 1>{}, x + 1);
+      if (x + 2 >= x1) break;
+    }
+  }
+
+  // Sums of the lanes with different keys of a row; then of the wavefronts, each of which finishes a quarter of the channels.
+  constexpr int OWN = CT / KW;
+  __shared__ float4 tiles[KW][QT][CT][64];
+  __shared__ float2 stats[KW][QT][16];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    l[q] += __shfl_xor(l[q], 16);
+    l[q] += __shfl_xor(l[q], 32);
+    if (lq == 0) stats[kw][q][l16] = make_float2(m[q], l[q]);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) tiles[kw][q][ct][lane] = make_float4(o[q][ct][0], o[q][ct][1], o[q][ct][2], o[q][ct][3]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    float2 st[KW];
+    float top = -FLT_MAX, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) st[k] = stats[k][q][l16], top = fmaxf(top, st[k].x);
+    f32x4 mine[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) mine[i] = (f32x4)0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const float weight = __builtin_amdgcn_exp2f(st[k].x - top);
+      sum = fmaf(st[k].y, weight, sum);
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        const float4 x = tiles[k][q][kw * OWN + i][lane];
+        mine[i][0] = fmaf(x.x, weight, mine[i][0]);
+        mine[i][1] = fmaf(x.y, weight, mine[i][1]);
+        mine[i][2] = fmaf(x.z, weight, mine[i][2]);
+        mine[i][3] = fmaf(x.w, weight, mine[i][3]);
+      }
+    }
+    if (row_of(q) >= sp.n_rows) continue;
+    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + sp.kv_head * a.group + row_of(q) % a.group;
+    const float f = weight_of(sum);
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const int ch = 16 * (kw * OWN + i) + 4 * lq;
+      if (sp.whole) {
+        typename T::x4 pk;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(mine[i][e] * f);
+        *reinterpret_cast<typename T::x4*>((typename T::x1*)a.o + out_row * D + ch) = pk;
+      } else {
+        *reinterpret_cast<float4*>(part_sums<ROWS, D>(a, w.place) + (16 * q + l16) * D + ch) = make_float4(mine[i][0], mine[i][1], mine[i][2], mine[i][3]);
+      }
+    }
+    if (kw == 0 && lq == 0) {
+      if (!sp.whole) part_stats<ROWS, D>(a, w.place)[16 * q + l16] = make_float2(top, sum);
+      else if (a.lse != nullptr) a.lse[out_row] = lse_of(top, sum);
     }
   }
 }
@@ -751,36 +866,35 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
       __syncthreads();
     }
     if (!there || (half & (every - 1)) != 0) continue;
-    const float f = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+    const float f = weight_of(sum);
     const int row = j.row + r;
     const int64_t out = (int64_t)(j.first + row / a.group) * a.heads + j.head * a.group + row % a.group;
     tE pk;
 #pragma unroll
     for (int e = 0; e < E; ++e) pk[e] = (typename T::x1)(acc[e] * f);
     *reinterpret_cast<tE*>((typename T::x1*)a.o + out * D + lane * E) = pk;
-    if (a.lse != nullptr && lane == 0) a.lse[out] = (top + __log2f(sum)) * 0.6931471805599453f;
+    if (a.lse != nullptr && lane == 0) a.lse[out] = lse_of(top, sum);
   }
 }
 
-template <class T, int D, int QT, int RW, int KW>
-int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
-  constexpr int ROWS = 32 * QT * RW;
+template <class T, int D, int ROWS, class Kernel>
+int launch(const rf2_paged_plan* plan, Args a, Kernel kernel, int threads, int least, hipStream_t st) {
   const rf2_paged_config& c = plan->cfg;
   a.aimed = rf2_paged_parts_per_head(c.kv_heads);
+  a.least = least;
   a.places = 2 * a.aimed * c.kv_heads;
   a.most_joints = a.aimed * c.kv_heads * RF2_PAGED_JOINTS;
   static_assert(ROWS / JOINT<ROWS> <= RF2_PAGED_JOINTS, "the workspace has room for so many to a tile");
-  a.least = KW > 1 ? 16 : 8;
   // tiles there can be: a sequence has at most one that is not full
-  const int64_t rows = (int64_t)a.n_tokens * a.group;
-  const int64_t tiles = std::min(rows / ROWS + std::min(a.n_seqs, a.n_tokens), (int64_t)a.n_tokens * ((a.group + ROWS - 1) / ROWS));
+  const int64_t rows = (int64_t)a.n_tokens * a.group, some = std::min(a.n_seqs, a.n_tokens);
+  const int64_t tiles = std::min(rows / ROWS + some, (int64_t)a.n_tokens * ((a.group + ROWS - 1) / ROWS));
   const bool can_be_cut = (int64_t)c.max_pages * c.page > 32 * a.least;
   const int64_t grid = (tiles + (can_be_cut ? a.aimed : 0)) * c.kv_heads;
-  if (grid * 64 * RW * KW >= (int64_t)1 << 32) return RF2_ERR_UNSUPPORTED;
-  paged_attn_kernel<T, D, QT, RW, KW><<<dim3((unsigned)grid), dim3(64 * RW * KW), 0, st>>>(a);
+  if (grid * threads >= (int64_t)1 << 32) return RF2_ERR_UNSUPPORTED;
+  kernel<<<dim3((unsigned)grid), dim3(threads), 0, st>>>(a);
   RF2_LAUNCH_CHECK();
   if (can_be_cut) {
-    const int64_t joints = std::min((int64_t)a.most_joints, (rows / JOINT<ROWS> + std::min(a.n_seqs, a.n_tokens)) * c.kv_heads);
+    const int64_t joints = std::min((int64_t)a.most_joints, (rows / JOINT<ROWS> + some) * c.kv_heads);
     join_kernel<T, D, ROWS><<<dim3((unsigned)std::min(joints, (int64_t)1024)), dim3(256), 0, st>>>(a);
     RF2_LAUNCH_CHECK();
   }
@@ -789,10 +903,13 @@ int launch(const rf2_paged_plan* plan, Args a, hipStream_t st) {
 
 template <class T, int D>
 int dispatch(const rf2_paged_plan* plan, const Args& a, hipStream_t st) {
-  // Up to 32 rows a sequence on average, one tile: four wavefronts share its keys.  More: two wavefronts of 64 rows.  (16 sequences of
-  // 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 74.9 as one of 128; 128 rows: 131 and 97.)
-  if ((int64_t)a.n_tokens * a.group <= 32 * (int64_t)a.n_seqs) return launch<T, D, 1, 1, 4>(plan, a, st);
-  return launch<T, D, 2, 2, 1>(plan, a, st);
+  // Up to 32 rows a sequence on average: four wavefronts share the keys of one or two tiles of 16.  More: two wavefronts of 64 rows.
+  // (16 sequences of 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 62.1 as one of 128; 128 rows: 131 and 78.6.)
+  // No sequence is cut below 16 units (for single tokens of 2,000 keys 13.1 us, 16.2 with 32), and 8.
+  const int64_t rows = (int64_t)a.n_tokens * a.group;
+  if (rows <= 16 * (int64_t)a.n_seqs) return launch<T, D, 16>(plan, a, few_attn_kernel<T, D, 1>, 256, 16, st);
+  if (rows <= 32 * (int64_t)a.n_seqs) return launch<T, D, 32>(plan, a, few_attn_kernel<T, D, 2>, 256, 16, st);
+  return launch<T, D, RF2_PAGED_ROWS_MANY>(plan, a, many_attn_kernel<T, D>, 128, 8, st);
 }
 
 }  // namespace
