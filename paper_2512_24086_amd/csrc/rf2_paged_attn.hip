@@ -42,8 +42,16 @@ struct Bf16 {
   static constexpr float RANGE = 1.0995e12f, HEAD = 0.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
-  static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
+  template <bool ACC>
+  static __device__ __forceinline__ void qk(f32x16& s, const x8& a, const x8& b, bool first) {
+    if constexpr (ACC) {
+      if (first) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+      else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
+    } else {
+      if (first) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+      else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+    }
+  }
 };
 struct F16 {
   typedef f16x8 x8;
@@ -55,8 +63,16 @@ struct F16 {
   static constexpr float RANGE = 32768.f, HEAD = 8.f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ void first(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b)); }
-  static __device__ __forceinline__ void more(f32x16& s, const x8& a, const x8& b) { asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b)); }
+  template <bool ACC>
+  static __device__ __forceinline__ void qk(f32x16& s, const x8& a, const x8& b, bool first) {
+    if constexpr (ACC) {
+      if (first) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+      else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
+    } else {
+      if (first) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+      else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+    }
+  }
 };
 
 struct Args {
@@ -66,7 +82,7 @@ struct Args {
   void* o;
   float* lse;
   int64_t q_stride;
-  int n_seqs, n_tokens, heads, kv_heads, group, unit_shift, n_pages, max_pages, causal, aimed, least, places, most_joints;
+  int n_seqs, n_tokens, heads, kv_heads, group, unit_shift, n_pages, max_pages, causal, aimed, least, places, most_joints, at_once;
   float scale_log2;
 };
 
@@ -145,10 +161,10 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
   int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
   if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
-    // Where tiles are long, how many of them and of their parts fill the chip's places (PLACES workgroups) counts.  Lane i holds what
+    // Where tiles are long, how many of them and of their parts fill the chip's places (for at_once workgroups) counts.  Lane i holds what
     // a launch takes with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more,
     // in units; START more for a part's first loads and its last stores, and as much again where sums are written and joined.
-    constexpr float PLACES = 512.f, START = 8.f;
+    constexpr float START = 8.f;
     const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
     const float per = 1.f / (float)mine;
     float items = 0.f, cut = 0.f, longest = 0.f;
@@ -160,7 +176,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
       longest = n > 0.f ? fmaxf(longest, fminf(u, (float)mine)) : longest;
     }
     const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
-    float cost = ceilf(items * heads / PLACES) * (mean + START * (1.f + cut / fmaxf(items, 1.f))) + (longest - mean);
+    float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + cut / fmaxf(items, 1.f))) + (longest - mean);
     float best = cost;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) best = fminf(best, __shfl_xor(best, d));
@@ -305,7 +321,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(
 
 // Many rows: two wavefronts of 64 rows each (two tiles of 32) walk a part's keys.
 template <class T, int D>
-__global__ void __launch_bounds__(128, 1) many_attn_kernel(Args a) {
+__global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a) {
   constexpr int DS = D / 16, DT = D / 32, ROWS = RF2_PAGED_ROWS_MANY;
   constexpr int WINDOW = 512;      // columns of the table that a wavefront has listed at a time
   typedef typename T::x8 x8;
@@ -414,8 +430,7 @@ __global__ void __launch_bounds__(128, 1) many_attn_kernel(Args a) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         if (g < NQ) {
-          if (g == 0) T::first(Snext[q], kr[B][g], qf[q][g]);
-          else T::more(Snext[q], kr[B][g], qf[q][g]);
+          T::template qk<true>(Snext[q], kr[B][g], qf[q][g], g == 0);
         } else {
           o[q][j / 2] = T::mfma(vr[B][j], operand_p(Pprev[q], j % 2), o[q][j / 2]);
         }
@@ -491,60 +506,162 @@ __global__ void __launch_bounds__(128, 1) many_attn_kernel(Args a) {
     else following(0);
     following(1);
     following(2);
-    x8 k0[NQ];
+    if constexpr (D == 128) {
+      x8 k0[NQ];
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) k0[c] = k_load(k_of(0), c);
+      for (int c = 0; c < NQ; ++c) k0[c] = k_load(k_of(0), c);
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) kr[0][c] = k_load(k_of(1), c);
-    asm volatile("" ::: "memory");
+      for (int c = 0; c < NQ; ++c) kr[0][c] = k_load(k_of(1), c);
+      asm volatile("" ::: "memory");
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) kr[1][c] = k_load(k_of(2), c);
-    asm volatile("" ::: "memory");
+      for (int c = 0; c < NQ; ++c) kr[1][c] = k_load(k_of(2), c);
+      asm volatile("" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      vr[1][j] = v_load(v_of(0), j);
+      for (int j = 0; j < NP; ++j) {
+        vr[1][j] = v_load(v_of(0), j);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vr[0][j][e] = (typename T::x1)0.f;     // step 0 has no unit before it: it adds 0 x 0
-    }
-    f32x16 Sa[2], Sb[2];
-    uint32_t Pa[2][8], Pb[2][8];
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-#pragma unroll
-      for (int ds = 0; ds < DS; ++ds) {
-        if (ds == 0) T::first(Sa[q], k0[ds], qf[q][ds]);
-        else T::more(Sa[q], k0[ds], qf[q][ds]);
+        for (int e = 0; e < 8; ++e) vr[0][j][e] = (typename T::x1)0.f;     // step 0 has no unit before it: it adds 0 x 0
       }
-      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(Sa[q]));
-      if (us[0] >= sp.free_units) mask(Sa[q], q, us[0]);
-      if (begins) (void)move_reference(q, Sa[q]);
+      f32x16 Sa[2], Sb[2];
+      uint32_t Pa[2][8], Pb[2][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) Pb[q][e] = 0u;
+      for (int q = 0; q < 2; ++q) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) Sb[q][i] = 0.f;
-    }
-    if (lead >= 0)
+        for (int ds = 0; ds < DS; ++ds) {
+          T::template qk<true>(Sa[q], k0[ds], qf[q][ds], ds == 0);
+        }
+        asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(Sa[q]));
+        if (us[0] >= sp.free_units) mask(Sa[q], q, us[0]);
+        if (begins) (void)move_reference(q, Sa[q]);
 #pragma unroll
-      for (int j = 0; j < NP; ++j) vr[1][j] = clear_behind(vr[1][j], w.s.len - 32 * lead - 16 * (j % 2) - 4 * lh);
-    // (arrived before the loop, whose waits would else be those of its first round)
+        for (int e = 0; e < 8; ++e) Pb[q][e] = 0u;
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) asm volatile("" : "+v"(kr[0][c]));
-    // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
-    do {
-      following(3);
-      step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_of(3), v_of(1), us[1]);
-      shift();
-      following(3);
-      step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_of(3), v_of(1), us[1]);
-      shift();
-    } while (us[0] != NONE);
-    // last product
+        for (int i = 0; i < 16; ++i) Sb[q][i] = 0.f;
+      }
+      if (lead >= 0)
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      l[q] += last[q];
-      last[q] = 0.f;
+        for (int j = 0; j < NP; ++j) vr[1][j] = clear_behind(vr[1][j], w.s.len - 32 * lead - 16 * (j % 2) - 4 * lh);
+      // (arrived before the loop, whose waits would else be those of its first round)
 #pragma unroll
-      for (int j = 0; j < NP; ++j) o[q][j / 2] = T::mfma(vr[0][j], operand_p(Pb[q], j % 2), o[q][j / 2]);
+      for (int c = 0; c < NQ; ++c) asm volatile("" : "+v"(kr[0][c]));
+      // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
+      do {
+        following(3);
+        step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_of(3), v_of(1), us[1]);
+        shift();
+        following(3);
+        step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_of(3), v_of(1), us[1]);
+        shift();
+      } while (us[0] != NONE);
+      // last product
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        l[q] += last[q];
+        last[q] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NP; ++j) o[q][j / 2] = T::mfma(vr[0][j], operand_p(Pb[q], j % 2), o[q][j / 2]);
+      }
+    } else {
+      // The two tiles of rows half a step apart, so that one S and one P of each are enough (two wavefronts per SIMD).
+      x8 k0[NQ];
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) k0[c] = k_load(k_of(0), c);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+          kr[1 - i][j] = k_load(k_of(i + 1), j);
+          asm volatile("" ::: "memory");
+          vr[i][j] = v_load(v_of(i), j);
+          asm volatile("" ::: "memory");
+        }
+      }
+      f32x16 S[2];
+      uint32_t P[2][8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) T::template qk<false>(S[q], k0[ds], qf[q][ds], ds == 0);
+        asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(S[q]));
+        if (us[0] >= sp.free_units) mask(S[q], q, us[0]);
+        if (begins) (void)move_reference(q, S[q]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) P[q][e] = 0u;
+      }
+      if (lead >= 0)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) vr[0][j] = clear_behind(vr[0][j], w.s.len - 32 * lead - 16 * (j % 2) - 4 * lh);
+      // Probabilities of a tile whose unit was out of range, or is the first of a list: O and l have all earlier units.
+      auto redo = [&](int q) __attribute__((always_inline)) {
+        const float alpha = move_reference(q, S[q]);
+        l[q] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[q][dt][i] *= alpha;
+        last[q] = probabilities(q, S[q], P[q]);
+      };
+      redo(0);
+      // Half of a step for tile Q: S of the next unit and O += V P of the present one, in turn, around the softmax arithmetic of the
+      // other tile X (the present unit of tile 1 in the first half, the next one of tile 0 in the second).  In the second half the
+      // operands' registers are loaded again.
+      auto half = [&](auto tile, auto odd, auto kb, auto vb, int u_next) __attribute__((always_inline)) {
+        constexpr int Q = decltype(tile)::value, X = 1 - Q, ODD = decltype(odd)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        float rs = 0.f, e[2][2];
+        // sum and packing of pair p, a slot behind its exponentials: no instruction waits for the one before it
+        auto finish_pair = [&](int p) __attribute__((always_inline)) {
+          const typename T::x2 pk = {(typename T::x1)e[p & 1][0], (typename T::x1)e[p & 1][1]};
+          uint32_t word = __builtin_bit_cast(uint32_t, pk);
+          rs = p == 0 ? e[0][0] + e[0][1] : rs + (e[p & 1][0] + e[p & 1][1]);
+          asm volatile("" : "+v"(word), "+v"(rs));
+          P[X][p] = word;
+        };
+#pragma unroll
+        for (int g = 0; g < NQ + NP; ++g) {
+          const int j = g / 2;
+          if (g % 2 == 0) T::template qk<false>(S[Q], kr[1 - ODD][j], qf[Q][j], j == 0);
+          else o[Q][j / 2] = T::mfma(vr[ODD][j], operand_p(P[Q], j % 2), o[Q][j / 2]);
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (Q == 1) {
+            if (g % 2 == 0) kr[1 - ODD][j] = k_load(kb, j);
+            else vr[ODD][j] = v_load(vb, j);
+            asm volatile("" ::: "memory");
+          }
+          if (g > 0) finish_pair(g - 1);
+          if (g == 0) {
+            l[Q] += last[Q];
+            asm volatile("" : "+v"(l[Q]));
+          }
+          e[g & 1][0] = __builtin_amdgcn_exp2f(fmaf(S[X][2 * g], a.scale_log2, -m[X]));
+          e[g & 1][1] = __builtin_amdgcn_exp2f(fmaf(S[X][2 * g + 1], a.scale_log2, -m[X]));
+          asm volatile("" : "+v"(e[g & 1][0]), "+v"(e[g & 1][1]));
+          if (g == 7) finish_pair(7);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        last[X] = rs;
+        // One branch, hardly ever taken, as above.
+        int bound = u_next >= sp.free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
+        asm volatile("" : "+s"(bound));
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
+          if (__builtin_amdgcn_ballot_w64(!(rs <= T::RANGE)) != 0ull) redo(X);
+          if (u_next >= sp.free_units) mask(S[Q], Q, u_next);
+        }
+      };
+      constexpr std::integral_constant<int, 0> zero{};
+      constexpr std::integral_constant<int, 1> one{};
+      do {
+        following(3);
+        half(zero, zero, k_of(3), v_of(2), us[1]);
+        half(one, zero, k_of(3), v_of(2), us[1]);
+        shift();
+        following(3);
+        half(zero, one, k_of(3), v_of(2), us[1]);
+        half(one, one, k_of(3), v_of(2), us[1]);
+        shift();
+      } while (us[0] != NONE);
+      last[0] = last[1] = 0.f;               // (of no unit)
     }
   };
   // The last unit of a sequence can have keys behind its last token, whose V has to be cleared: it goes first, so that no step
@@ -878,10 +995,11 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
 }
 
 template <class T, int D, int ROWS, class Kernel>
-int launch(const rf2_paged_plan* plan, Args a, Kernel kernel, int threads, int least, hipStream_t st) {
+int launch(const rf2_paged_plan* plan, Args a, Kernel kernel, int threads, int least, int at_once, hipStream_t st) {
   const rf2_paged_config& c = plan->cfg;
   a.aimed = rf2_paged_parts_per_head(c.kv_heads);
   a.least = least;
+  a.at_once = at_once;
   a.places = 2 * a.aimed * c.kv_heads;
   a.most_joints = a.aimed * c.kv_heads * RF2_PAGED_JOINTS;
   static_assert(ROWS / JOINT<ROWS> <= RF2_PAGED_JOINTS, "the workspace has room for so many to a tile");
@@ -907,9 +1025,9 @@ int dispatch(const rf2_paged_plan* plan, const Args& a, hipStream_t st) {
   // (16 sequences of 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 62.1 as one of 128; 128 rows: 131 and 78.6.)
   // No sequence is cut below 16 units (for single tokens of 2,000 keys 13.1 us, 16.2 with 32), and 8.
   const int64_t rows = (int64_t)a.n_tokens * a.group;
-  if (rows <= 16 * (int64_t)a.n_seqs) return launch<T, D, 16>(plan, a, few_attn_kernel<T, D, 1>, 256, 16, st);
-  if (rows <= 32 * (int64_t)a.n_seqs) return launch<T, D, 32>(plan, a, few_attn_kernel<T, D, 2>, 256, 16, st);
-  return launch<T, D, RF2_PAGED_ROWS_MANY>(plan, a, many_attn_kernel<T, D>, 128, 8, st);
+  if (rows <= 16 * (int64_t)a.n_seqs) return launch<T, D, 16>(plan, a, few_attn_kernel<T, D, 1>, 256, 16, 512, st);
+  if (rows <= 32 * (int64_t)a.n_seqs) return launch<T, D, 32>(plan, a, few_attn_kernel<T, D, 2>, 256, 16, 512, st);
+  return launch<T, D, RF2_PAGED_ROWS_MANY>(plan, a, many_attn_kernel<T, D>, 128, 8, D == 128 ? 512 : 1024, st);
 }
 
 }  // namespace
