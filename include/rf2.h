@@ -357,7 +357,8 @@ int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k,
  *   block_table, seq_len, cu_new : as left by rf2_paged_append (seq_len is its seq_len_out), or a program's own.  Token
  *                 t of the n new ones of sequence s sees the keys j < seq_len[s] - n + t + 1 (causal) or j < seq_len[s].
  *                 An entry of the table outside [0, n_pages) is a hole: its keys are left out (pages that were evicted).
- *                 Lengths are clamped to [0, max_pages * page], rows to [0, n_tokens).     (in)
+ *                 Lengths are clamped to [0, max_pages * page], rows to [0, n_tokens); if the rows of all sequences
+ *                 are more than n_tokens (they overlap) nothing is computed.               (in)
  *   workspace   : rf2_paged_info.workspace_bytes, written and read by this call alone: calls that may run at the same time
  *                 need one each                                                            (scratch)
  *   o           : [n_tokens, heads, head_dim]; a token that sees no key gets zeros         (out)

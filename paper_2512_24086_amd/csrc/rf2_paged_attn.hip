@@ -141,7 +141,6 @@ template <int ROWS>
 constexpr int JOINT = ROWS < RF2_PAGED_ROWS_MANY ? 2 : 8;
 
 // Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.
-// (Sums are of 32 bits: of rows there are at most 2^20 tokens.  Rows that overlap, which no table of this library has, may be left out.)
 template <int ROWS>
 __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w) {
   const int lane = (int)threadIdx.x & 63;
@@ -151,13 +150,17 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     s = at < a.n_seqs ? seq_of(a, at) : Seq{0, 0, 0};
     tiles = (int)((unsigned)(s.n_new * a.group + ROWS - 1) / (unsigned)ROWS);
   };
-  float work = 0.f;
+  float work = 0.f, tokens = 0.f;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
     look(s0 + lane);
     work += (float)tiles * (float)units_of(s.len);
+    tokens += (float)s.n_new;
   }
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d);
+  for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d), tokens += __shfl_xor(tokens, d);
+  // Rows that overlap, which no table of this library has, can be more than the grid and the workspace are made for: nothing is done.
+  // (Sums up to 2^24 are exact, n_tokens is at most 2^20.)
+  const int n_seqs = uniform(tokens <= (float)a.n_tokens) ? a.n_seqs : 0;
   // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
   int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
   if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
@@ -188,7 +191,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
   unsigned before = 0, places = 0, joined = 0;       // of the sequences before, one head's
   bool found = false;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+  for (int s0 = 0; s0 < n_seqs; s0 += 64) {
     if (a.n_seqs > 64) look(s0 + lane);
     const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units;
     const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, joint = chunks > 1 ? (unsigned)(s.n_new * a.group + JOINT<ROWS> - 1) / JOINT<ROWS> : 0;

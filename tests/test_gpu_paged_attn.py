@@ -40,6 +40,11 @@ CASES = {
     # more sequences than a wavefront has lanes
     "many_seqs": dict(new=[1] * 150, ctx=[(37 * i) % 301 for i in range(150)], heads=4, kv=2, d=64, page=32),
     "many_mixed": dict(new=[(i % 7 == 3) * 40 + i % 3 for i in range(100)], ctx=[(91 * i) % 500 for i in range(100)], heads=4, kv=1, d=128, page=64),
+    # single tokens of long sequences beside chunks
+    "mixed": dict(new=[1, 300, 1, 1, 2, 90, 1, 0, 1, 5, 1, 1], ctx=[3000, 700, 20, 9000, 5, 0, 1, 60, 4100, 333, 2500, 31], heads=8, kv=2, d=128, page=64, pad=3),
+    "mixed_d64": dict(new=[1, 1, 260, 1, 1, 1, 130, 1, 1], ctx=[5000, 2100, 900, 64, 63, 0, 2000, 3000, 1500], heads=4, kv=4, d=64, page=32, dtype=FP),
+    "mixed_group_20": dict(new=[1, 1, 60, 1, 1, 1, 30, 1, 1], ctx=[5000, 2100, 900, 64, 63, 0, 2000, 3000, 1500], heads=20, kv=1, d=128, page=128),
+    "chunks_alone": dict(new=[64, 40, 90, 33, 70, 50, 41, 65, 77], ctx=[600, 0, 900, 64, 63, 10, 2000, 30, 1500], heads=4, kv=4, d=64, page=64),
 }
 
 
@@ -129,6 +134,17 @@ def test_holes_in_the_table_are_left_out():
             b.check(o, lse, causal)
 
 
+def test_holes_beside_chunks_and_single_tokens():
+    holes = [(s, p, -1) for s in range(9) for p in range(1, 1 + 3 * s)] + [(1, 0, 10 ** 6)]
+    for d, dtype, page in ((64, FP, 128), (128, BF, 32)):
+        b = Batch(seed=17, new=[1, 1, 200, 1, 1, 1, 150, 1, 1], ctx=[30 * page] * 9, heads=8, kv=4, d=d, page=page, dtype=dtype, holes=holes)
+        o, lse = b.run(b.plan())
+        b.check(o, lse)
+        b = Batch(seed=18, new=[1] * 9, ctx=[30 * page + 5] * 9, heads=8, kv=4, d=d, page=page, dtype=dtype, holes=holes)
+        o, lse = b.run(b.plan())
+        b.check(o, lse)
+
+
 def test_a_sequence_of_holes_alone_yields_zeros():
     b = Batch(seed=8, new=[1, 1], ctx=[99, 300], heads=4, kv=2, d=64, page=32, holes=[(0, p, -1) for p in range(4)])
     o, lse = b.run(b.plan())
@@ -162,6 +178,17 @@ def test_lengths_out_of_range_are_clamped():
     b.seq_len.fill_(64)
     b.run(plan)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n", [3, 70])
+def test_rows_that_overlap_are_refused_by_the_kernel(n):
+    """cu_new goes up and down, so that the sequences' rows are together more than there are."""
+    b = Batch(seed=16, new=[30] + [0] * n, ctx=[2000] + [1000] * n, heads=8, kv=4, d=64, page=32)
+    plan = b.plan()
+    b.cu.copy_(torch.tensor([0, 30] * ((n + 2) // 2) + [0] * (n % 2)))
+    o, lse = b.run(plan)
+    torch.cuda.synchronize()
+    assert (o == 7.0).all() and (lse == 7.0).all()
 
 
 def test_values_that_are_not_finite_stay_with_their_rows():
