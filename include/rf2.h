@@ -364,9 +364,9 @@ int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k,
  *   o           : [n_tokens, heads, head_dim]; a token that sees no key gets zeros         (out)
  *   lse         : optional [n_tokens, heads] fp32, natural-log sum-exp of the scaled logits, -inf where there is no key;
  *                 may be NULL                                                              (out)
- * Rows from cu_new[n_seqs] on are neither read nor written.  Memory of the cache behind a sequence's last token may
- * hold anything, infinities and NaN included.  The same call gives the same bits each time; in a batch of other
- * sequences a token's result may differ by fp32 rounding.
+ * Rows from cu_new[n_seqs] on are neither read nor written.  What a token does not see does not reach it: the cache behind a
+ * sequence's last token, and tokens of the chunk behind its own, may hold anything, infinities and NaN included.  The same
+ * call gives the same bits each time; in a batch of other sequences a token's result may differ by fp32 rounding.
  */
 int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens, const void* q, int64_t q_stride,
                    const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* seq_len,

@@ -40,6 +40,7 @@ struct Bf16 {
   typedef __bf16 x1;
   // P = exp2(x - m): bf16 and fp32 carry 2^40 as well as 1
   static constexpr float RANGE = 1.0995e12f, HEAD = 0.f;
+  static constexpr uint32_t EXPONENT = 0x7f80, MANTISSA = 0x7f;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   template <bool ACC>
@@ -61,6 +62,7 @@ struct F16 {
   // fp16 ends at 65,504 and loses its steps below 2^-14: the largest P stands at 2^8 when the reference is set (HEAD), may grow to
   // 2^15, and what is rounded away below 2^-25 is 2^-33 of it
   static constexpr float RANGE = 32768.f, HEAD = 8.f;
+  static constexpr uint32_t EXPONENT = 0x7c00, MANTISSA = 0x3ff;
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   template <bool ACC>
@@ -166,7 +168,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
     // Where tiles are long, how many of them and of their parts fill the chip's places (for at_once workgroups) counts.  Lane i holds what
     // a launch takes with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more,
-    // in units; START more for a part's first loads and its last stores, and as much again where sums are written and joined.
+    // in units; START more for a part's first loads and its last stores, three times that where sums are written and joined.
     constexpr float START = 8.f;
     const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
     const float per = 1.f / (float)mine;
@@ -179,7 +181,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
       longest = n > 0.f ? fmaxf(longest, fminf(u, (float)mine)) : longest;
     }
     const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
-    float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + cut / fmaxf(items, 1.f))) + (longest - mean);
+    float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + 3.f * cut / fmaxf(items, 1.f))) + (longest - mean);
     float best = cost;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) best = fminf(best, __shfl_xor(best, d));
@@ -318,6 +320,58 @@ __device__ __forceinline__ x8 clear_behind(x8 v, int left) {
   return __builtin_bit_cast(x8, x);
 }
 
+// Values of V that are not finite, in units that some rows of a tile see more of than others: 0 times such a value is no 0, so they
+// are taken out of V, and rows that see them get them by products of their own: the largest bf16 number where a value is +infinity
+// or not a number, times the same where a row sees the key, is +infinity in fp32 and 0 elsewhere; the negative one likewise.
+// (Two halves of a register at a time: an exponent of all ones carries into the sign's place.)
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+  constexpr uint32_t E = T::EXPONENT | T::EXPONENT << 16, ONE = (0x8000u - T::EXPONENT) | (0x8000u - T::EXPONENT) << 16;
+  return ((x & E) + ONE) & 0x80008000u;
+}
+__device__ __forceinline__ uint32_t halves(uint32_t signs) { return (signs >> 15) * 0xffffu; }     // whole halves from their sign places
+template <class T, class x8>
+__device__ __forceinline__ uint32_t any_not_finite(const x8& v) {
+  const u32x4 x = __builtin_bit_cast(u32x4, v);
+  return not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+}
+// The places of those that count as +infinity (or as -infinity; what is not a number counts as both), as bf16 numbers.
+template <class T, bool MINUS, class x8>
+__device__ __forceinline__ bf16x8 infinities(const x8& v) {
+  constexpr uint32_t M = T::MANTISSA | T::MANTISSA << 16;
+  const u32x4 x = __builtin_bit_cast(u32x4, v);
+  u32x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t nan = (x[e] & M) + (0x80008000u - 0x00010001u);        // (a mantissa above 0 carries into the sign's place)
+    y[e] = halves(not_finite<T>(x[e]) & (nan | (MINUS ? x[e] : ~x[e]))) & (MINUS ? 0xff7fff7fu : 0x7f7f7f7fu);
+  }
+  return __builtin_bit_cast(bf16x8, y);
+}
+// Zeros in all their places.  (In the registers that hold v: as other values they would be copied around the branch.)
+template <class T, class x8>
+__device__ __forceinline__ void take_out(x8& v) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint32_t y = x[e];
+    asm("v_and_b32 %0, %1, %0" : "+v"(y) : "v"(~halves(not_finite<T>(y))));
+    x[e] = y;
+  }
+  v = __builtin_bit_cast(x8, x);
+}
+// The largest bf16 number for each of a lane's eight keys of an operand (4 in a row, and 4 from eight further) that is among the
+// first `left`, else 0.
+__device__ __forceinline__ bf16x8 seen(int left) {
+  u32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int key = e / 2 * 8 + e % 2 * 2;
+    x[e] = (key < left ? 0x7f7fu : 0u) | (key + 1 < left ? 0x7f7f0000u : 0u);
+  }
+  return __builtin_bit_cast(bf16x8, x);
+}
+
 // 1 / l of a finished row; a row that sees no key yields zeros, one whose sum is not a number that.
 __device__ __forceinline__ float weight_of(float l) { return l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l); }
 __device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(l)) * 0.6931471805599453f; }
@@ -401,6 +455,28 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
   constexpr int NQ = DS, NP = 2 * DT, PAIRS = 16 / (NQ + NP);
   x8 kr[2][NQ], vr[2][NP];
   float last[2] = {};                      // sums of the latest unit, still to be added to l
+  constexpr int NONE = 1 << 25;            // a unit that no sequence has
+  // V of unit u, of which rows do not all see the same, without values that are not finite (see take_out).
+  const bool rows_differ = uniform(limit_of(a, w.s, sp.row0) != limit_of(a, w.s, min(sp.row0 + 64, sp.n_rows) - 1));
+  auto guard = [&](x8 (&v)[NP], int u) __attribute__((always_inline)) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) any |= any_not_finite<T>(v[j]);
+    if (__builtin_amdgcn_ballot_w64(any != 0) == 0ull) return;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      __builtin_amdgcn_sched_barrier(0);     // (one operand after the other: there are no registers for more)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const bf16x8 sees = seen(limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - 16 * (j % 2) - 4 * lh);
+        o[q][j / 2] = Bf16::mfma(infinities<T, false>(v[j]), sees, o[q][j / 2]);
+        __builtin_amdgcn_sched_barrier(0);
+        o[q][j / 2] = Bf16::mfma(infinities<T, true>(v[j]), sees, o[q][j / 2]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      take_out<T>(v[j]);
+    }
+  };
   // O of tile q times alpha.  In accumulation registers it is scaled where it is, through one vector register (left to the
   // compiler, the copies cost the registers of the loop); the wait states cover a product in flight and one that follows.
   auto rescale = [&](int q, float alpha) __attribute__((always_inline)) {
@@ -419,7 +495,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
   // Step: S of the next unit, O += V P of the one before, the softmax arithmetic of the present one, operand by operand.  The
   // operands' registers are loaded again as soon as both MFMAs that read them are issued: K at k_at, V at v_at.
   auto step = [&](auto odd, f32x16 (&Scur)[2], f32x16 (&Snext)[2], uint32_t (&Pprev)[2][8], uint32_t (&Pcur)[2][8], auto kb, auto vb,
-                  int u_next) __attribute__((always_inline)) {
+                  int u, int u_next) __attribute__((always_inline)) {
     constexpr int B = decltype(odd)::value;
     __builtin_amdgcn_sched_barrier(0);
     float rs[2] = {}, e0[PAIRS], e1[PAIRS];
@@ -471,7 +547,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
     last[1] = rs[1];
     // One branch, hardly ever taken: the present unit is out of range, or rows do not see all of the next one.
     // (the limit is an integer select: as a float one it would be two branches, and the step twice)
-    int bound = u_next >= sp.free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
+    int bound = max(u, u_next) >= sp.free_units ? __builtin_bit_cast(int, -1.f) : __builtin_bit_cast(int, T::RANGE);
     asm volatile("" : "+s"(bound));
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
       if (__builtin_amdgcn_ballot_w64(!(rs[0] + rs[1] <= T::RANGE)) != 0ull)
@@ -483,12 +559,12 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
           last[q] = probabilities(q, Scur[q], Pcur[q]);
         }
       if (u_next >= sp.free_units) mask(Snext[0], 0, u_next), mask(Snext[1], 1, u_next);
+      if (rows_differ && u >= sp.free_units && u != NONE) guard(vr[1 - B], u);
     }
   };
   // Units x0 to x1 - 1 of the list (behind unit `lead` of page `lead_page`, where there is one).
   auto walk = [&](int x0, int x1, int lead, int lead_page, bool begins) __attribute__((always_inline)) {
     // Units s to s + 3 and where they lie in either cache; past the last one none.
-    constexpr int NONE = 1 << 25;
     int us[4], x = x0;
     int64_t at[4];
     int2 entry = pages[max(min(x, x1 - 1), 0) >> a.unit_shift];       // of unit x, read a step before it is used
@@ -550,10 +626,10 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
       // Steps in pairs: behind an odd number of units comes one of which no row sees anything.
       do {
         following(3);
-        step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_of(3), v_of(1), us[1]);
+        step(std::integral_constant<int, 0>{}, Sa, Sb, Pb, Pa, k_of(3), v_of(1), us[0], us[1]);
         shift();
         following(3);
-        step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_of(3), v_of(1), us[1]);
+        step(std::integral_constant<int, 1>{}, Sb, Sa, Pa, Pb, k_of(3), v_of(1), us[0], us[1]);
         shift();
       } while (us[0] != NONE);
       // last product
@@ -605,6 +681,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
           for (int i = 0; i < 16; ++i) o[q][dt][i] *= alpha;
         last[q] = probabilities(q, S[q], P[q]);
       };
+      if (rows_differ && us[0] >= sp.free_units) guard(vr[0], us[0]);
       redo(0);
       // Half of a step for tile Q: S of the next unit and O += V P of the present one, in turn, around the softmax arithmetic of the
       // other tile X (the present unit of tile 1 in the first half, the next one of tile 0 in the second).  In the second half the
@@ -650,6 +727,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
           if (__builtin_amdgcn_ballot_w64(!(rs <= T::RANGE)) != 0ull) redo(X);
           if (u_next >= sp.free_units) mask(S[Q], Q, u_next);
+          if (Q == 1 && rows_differ && u_next >= sp.free_units && u_next != NONE) guard(vr[1 - ODD], u_next);
         }
       };
       constexpr std::integral_constant<int, 0> zero{};
@@ -723,7 +801,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
 //
 // Bound by memory: operands of two units are on their way (each is asked for as soon as the one two before has been read).
 template <class T, int D, int QT>
-__global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
+__global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kernel(Args a) {
   constexpr int KW = 4, CS = D / 32, CT = D / 16, ROWS = 16 * QT;
   constexpr int WINDOW = 256;      // columns of the table that a wavefront has listed at a time
   typedef typename T::x8 x8;
@@ -741,6 +819,7 @@ __global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
 #pragma unroll
     for (int cs = 0; cs < CS; ++cs) qf[q][cs] = *reinterpret_cast<const x8*>(from + 32 * cs);
   }
+  const bool rows_differ = uniform(limit_of(a, w.s, sp.row0) != limit_of(a, w.s, min(sp.row0 + ROWS, sp.n_rows) - 1));
   f32x4 o[QT][CT];
   float m[QT], l[QT];
 #pragma unroll
@@ -751,6 +830,9 @@ __global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
     for (int ct = 0; ct < CT; ++ct) o[q][ct] = (f32x4)0.f;
   }
   const int key0 = (lq & 1) * 4 + (lq >> 1) * 16;                     // first of this lane's keys of a unit (the other four: 8 further)
+  int limit[QT];                                                      // keys that a row sees, less that
+#pragma unroll
+  for (int q = 0; q < QT; ++q) limit[q] = limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - key0;
   const uint32_t k_lane = (uint32_t)(lq * 512 + ((l16 & 7) + (l16 >> 3) * 16) * 16), v_lane = (uint32_t)(lq * D + l16) * 16;
   // Tiles are read once, or a few times at the same time, and then not for long: the loads are marked as not to be kept (64 single
   // tokens over 0.79 GB of keys and values 149.7 -> 137.4 us).
@@ -764,38 +846,40 @@ __global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
   const int32_t* const table = a.table + (int64_t)uniform(w.seq) * a.max_pages;
   __shared__ int2 page_lists[KW][WINDOW];
   int2* const pages = page_lists[kw];
-  constexpr int AHEAD = QT == 2 && D == 128 ? 1 : 2;      // units that V is asked for ahead: what registers there are for
-  x8 kr[2][2][CS], vr[AHEAD][CT];
-  int us[2];
+  constexpr int AHEAD = QT == 2 && D == 128 ? 1 : 2;      // units that are asked for ahead: what registers there are for
+  x8 kr[AHEAD][2][CS], vr[AHEAD][CT];
+  int us[AHEAD];
   for (int p = sp.begin >> a.unit_shift, p1 = (sp.end + (1 << a.unit_shift) - 1) >> a.unit_shift; sp.begin < sp.end && p < p1; p += WINDOW) {
     int x0, x1;
     list_pages<WINDOW>(a, table, pages, p, min(p + WINDOW, p1), sp.begin, sp.end, x0, x1);
     if (x0 >= x1) continue;
-    int64_t at[2];
+    int64_t at[AHEAD];
     auto place = [&](int x, int& u, int64_t& at) __attribute__((always_inline)) {
       const int2 entry = pages[min(x, x1 - 1) >> a.unit_shift];
       u = (uniform(entry.y) << a.unit_shift) + (x & ((1 << a.unit_shift) - 1));
       at = tile_at<D>(a, sp.kv_head, u, uniform(entry.x));
     };
     // unit x, whose place is held in us and at
-    auto fetch_k = [&](auto odd, int x) __attribute__((always_inline)) {
-      const auto kb = tile_buffer<D>(a.k_cache, at[decltype(odd)::value], x < x1);
+    auto fetch_k = [&](auto slot, int x) __attribute__((always_inline)) {
+      constexpr int B = decltype(slot)::value;
+      const auto kb = tile_buffer<D>(a.k_cache, at[B], x < x1);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int cs = 0; cs < CS; ++cs) kr[decltype(odd)::value][t][cs] = k_load(kb, t, cs);
+        for (int cs = 0; cs < CS; ++cs) kr[B][t][cs] = k_load(kb, t, cs);
       asm volatile("" ::: "memory");
     };
-    auto fetch_v = [&](auto odd, int x) __attribute__((always_inline)) {
-      const auto vb = tile_buffer<D>(a.v_cache, at[decltype(odd)::value], x < x1);
+    auto fetch_v = [&](auto slot, int x) __attribute__((always_inline)) {
+      constexpr int B = decltype(slot)::value;
+      const auto vb = tile_buffer<D>(a.v_cache, at[B], x < x1);
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) vr[decltype(odd)::value % AHEAD][ct] = v_load(vb, ct);
+      for (int ct = 0; ct < CT; ++ct) vr[B][ct] = v_load(vb, ct);
       asm volatile("" ::: "memory");
     };
-    auto unit = [&](auto odd, int x) __attribute__((always_inline)) {
-      constexpr int B = decltype(odd)::value;
+    auto unit = [&](auto slot, int x) __attribute__((always_inline)) {
+      constexpr int B = decltype(slot)::value;
       const int u = us[B];
-      place(x + 2, us[B], at[B]);
+      place(x + AHEAD, us[B], at[B]);
       f32x4 S[QT][2];
 #pragma unroll
       for (int q = 0; q < QT; ++q)
@@ -805,12 +889,12 @@ __global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
 #pragma unroll
           for (int cs = 0; cs < CS; ++cs) S[q][t] = T::mfma16(kr[B][t][cs], qf[q][cs], S[q][t]);
         }
-      fetch_k(odd, x + 2);
+      fetch_k(slot, x + AHEAD);
       x8 P[QT];
 #pragma unroll
       for (int q = 0; q < QT; ++q) {
         if (u >= sp.free_units) {                            // keys that a row does not see
-          const int left = limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - key0;
+          const int left = limit[q] - 32 * u;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (8 * (i / 4) + i % 4 >= left) S[q][i / 4][i % 4] = -INFINITY;
@@ -847,23 +931,47 @@ __global__ void __launch_bounds__(256, 2) few_attn_kernel(Args a) {
       }
       if (32 * u + 32 > w.s.len)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) vr[B % AHEAD][ct] = clear_behind(vr[B % AHEAD][ct], w.s.len - 32 * u - key0);
+        for (int ct = 0; ct < CT; ++ct) vr[B][ct] = clear_behind(vr[B][ct], w.s.len - 32 * u - key0);
+      uint32_t any = 0;
+      if (rows_differ && u >= sp.free_units)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) any |= any_not_finite<T>(vr[B][ct]);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0ull, 0)) {
+        // values of V that are not finite, where rows differ in what they see (see take_out); one operand after the other
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int q = 0; q < QT; ++q) {
+            int left = limit[q] - 32 * u;
+            asm volatile("" : "+v"(left));                     // (worked out anew each time)
+            const bf16x8 sees = seen(left);
+            o[q][ct] = Bf16::mfma16(infinities<T, false>(vr[B][ct]), sees, o[q][ct]);
+            o[q][ct] = Bf16::mfma16(infinities<T, true>(vr[B][ct]), sees, o[q][ct]);
+          }
+          take_out<T>(vr[B][ct]);
+        }
+      }
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int q = 0; q < QT; ++q) o[q][ct] = T::mfma16(vr[B % AHEAD][ct], P[q], o[q][ct]);
-      fetch_v(std::integral_constant<int, (B + AHEAD) % 2>{}, x + AHEAD);
+        for (int q = 0; q < QT; ++q) o[q][ct] = T::mfma16(vr[B][ct], P[q], o[q][ct]);
+      fetch_v(slot, x + AHEAD);
     };
+    constexpr std::integral_constant<int, 0> zero{};
+    constexpr std::integral_constant<int, AHEAD - 1> one{};
     place(x0, us[0], at[0]);
-    place(x0 + 1, us[1], at[1]);
-    fetch_k(std::integral_constant<int, 0>{}, x0);
-    fetch_v(std::integral_constant<int, 0>{}, x0);
-    fetch_k(std::integral_constant<int, 1>{}, x0 + 1);
-    if constexpr (AHEAD == 2) fetch_v(std::integral_constant<int, 1>{}, x0 + 1);
+    fetch_k(zero, x0);
+    fetch_v(zero, x0);
+    if constexpr (AHEAD == 2) {
+      place(x0 + 1, us[1], at[1]);
+      fetch_k(one, x0 + 1);
+      fetch_v(one, x0 + 1);
+    }
     for (int x = x0;; x += 2) {
-      unit(std::integral_constant<int, 0>{}, x);
+      unit(zero, x);
       if (x + 1 >= x1) break;
-      unit(std::integral_constant<int, 1>{}, x + 1);
+      unit(one, x + 1);
       if (x + 2 >= x1) break;
     }
   }

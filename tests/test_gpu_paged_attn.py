@@ -202,6 +202,69 @@ def test_values_that_are_not_finite_stay_with_their_rows():
     assert torch.isfinite(o.float()).all(2)[keep].all()
 
 
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", [dict(new=[6, 3], ctx=[40, 61], heads=4, kv=2, d=64), dict(new=[6, 3], ctx=[40, 61], heads=4, kv=2, d=128),
+                                   dict(new=[20, 9], ctx=[700, 13], heads=2, kv=2, d=128), dict(new=[150, 70], ctx=[0, 90], heads=4, kv=2, d=64),
+                                   dict(new=[150, 70], ctx=[333, 0], heads=4, kv=2, d=128), dict(new=[300], ctx=[2000], heads=1, kv=1, d=128),
+                                   dict(new=[300], ctx=[2000], heads=1, kv=1, d=64)], ids=str)
+def test_tokens_behind_that_are_not_finite_stay_unseen(shape, dtype):
+    """K and V of some new tokens hold infinities and NaN: tokens before them get the bits that they get with zeros there, and from
+    them on V's go through as the sum has them (a channel with both infinities, or with a NaN, is not a number)."""
+    b = Batch(seed=20, page=64, dtype=dtype, **shape)
+    plan = b.plan()
+    places = {0: (3, 5), 1: (1, 2)}                       # sequence -> tokens of its chunk
+    inf, nan = float("inf"), float("nan")
+    values = [(0, inf), (1, -inf), (2, nan), (3, inf)]
+
+    def write(s, pos, ch, v=None, k=None):
+        page, r = int(b.table[s, pos // 64]), pos % 64
+        if v is not None:
+            b.v_cache[page, :, r // 32, r % 32 // 16 * 2 + r % 8 // 4, ch, r % 16 // 8 * 4 + r % 4] = v
+        if k is not None:
+            b.k_cache[page, :, r // 32, ch // 8, r % 32, ch % 8] = k
+
+    for s, (first, second) in list(places.items())[:len(b.new)]:
+        for ch, _ in values:
+            for t in (first, second):
+                write(s, b.ctx[s] + t, ch, v=0.0)
+    clean, _ = b.run(plan)
+    for s, (first, second) in list(places.items())[:len(b.new)]:
+        for ch, x in values:
+            write(s, b.ctx[s] + first, ch, v=x)
+        write(s, b.ctx[s] + second, 3, v=-inf)             # channel 3: both
+    o, _ = b.run(plan)
+    at = 0
+    for s, n in enumerate(b.new):
+        first, second = places[s]
+        got, want = o[at:at + n], clean[at:at + n]
+        assert torch.equal(got[:first].view(torch.int16), want[:first].view(torch.int16)), s
+        assert torch.equal(got[:, :, 4:].contiguous().view(torch.int16), want[:, :, 4:].contiguous().view(torch.int16)), s
+        seen = got[first:].float()
+        assert (seen[:, :, 0] == inf).all() and (seen[:, :, 1] == -inf).all() and torch.isnan(seen[:, :, 2]).all(), s
+        assert (got[first:second, :, 3].float() == inf).all() and torch.isnan(got[second:, :, 3].float()).all(), s
+        at += n
+    # K of one token: all channels of the tokens from it on.  A row that is out of range makes the rows of its wavefront move their
+    # references, so those before it may be rounded otherwise: they are held to the definition, like every result.
+    from tests.paged_ref import attention
+    for s, (first, second) in list(places.items())[:len(b.new)]:
+        for ch, _ in values:
+            for t in (first, second):
+                write(s, b.ctx[s] + t, ch, v=0.0)
+                b.v[s][b.ctx[s] + t, :, ch] = 0.0
+    for x in (nan, inf):
+        for s in range(len(b.new)):
+            write(s, b.ctx[s] + places[s][0], 7, k=x)
+        o, _ = b.run(plan)
+        at = 0
+        for s, n in enumerate(b.new):
+            first = places[s][0]
+            want, _, tol, _ = attention(b.q[at:at + n], b.k[s].cuda(), b.v[s].cuda(), b.kept[s].cuda(), n, True, 1 / b.d ** 0.5, torch.finfo(dtype).eps / 2)
+            assert ((o[at:at + first].double() - want[:first]).abs() <= tol[:first]).all(), s
+            if x != inf:
+                assert torch.isnan(o[at + first:at + n].float()).all(), s
+            at += n
+
+
 @pytest.mark.parametrize("n", [1, 63, 64, 65, 200, 1024])
 def test_numbers_of_sequences(n):
     b = Batch(seed=12, new=[1] * n, ctx=[(i * 53) % 90 for i in range(n)], heads=2, kv=1, d=64, page=32)
