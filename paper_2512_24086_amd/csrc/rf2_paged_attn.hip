@@ -85,8 +85,13 @@ struct Args {
   float* lse;
   int64_t q_stride;
   int n_seqs, n_tokens, heads, kv_heads, group, unit_shift, n_pages, max_pages, causal, aimed, least, places, most_joints, at_once;
+  uint32_t group_magic, group_shift;      // see token_of
   float scale_log2;
 };
+
+// Token of a row: row / group, for rows below 2^29, as (row * ceil(2^(29 + k) / group)) >> (29 + k) with 2^k >= group: the factor is
+// too large by less than 2^k / 2^(29 + k) of a row.
+__device__ __forceinline__ int token_of(const Args& a, int row) { return (int)((uint64_t)(uint32_t)row * a.group_magic >> a.group_shift); }
 
 // A sequence of the call.
 struct Seq {
@@ -121,6 +126,32 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
   return x;
 }
 
+// The same of floats, all of them: the sum, and the least.
+__device__ __forceinline__ float wave_total(float x) {
+#define RF2_ADD(ctrl, rows) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, true))
+  RF2_ADD(0x111, 0xf);
+  RF2_ADD(0x112, 0xf);
+  RF2_ADD(0x114, 0xf);
+  RF2_ADD(0x118, 0xf);
+  RF2_ADD(0x142, 0xa);
+  RF2_ADD(0x143, 0xc);
+#undef RF2_ADD
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ __forceinline__ float wave_least(float x) {
+  // (a lane without a neighbour in a step takes itself)
+#define RF2_MIN(ctrl, rows) \
+  x = fminf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), ctrl, rows, 0xf, false)))
+  RF2_MIN(0x111, 0xf);
+  RF2_MIN(0x112, 0xf);
+  RF2_MIN(0x114, 0xf);
+  RF2_MIN(0x118, 0xf);
+  RF2_MIN(0x142, 0xa);
+  RF2_MIN(0x143, 0xc);
+#undef RF2_MIN
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
 // What is to be added up, a few rows of a tile that is cut at a time: written by the workgroup of the tile's first part, in the
 // workspace behind their number.
 struct Joint {
@@ -136,6 +167,13 @@ __device__ __forceinline__ float* part_sums(const Args& a, int place) { return a
 template <int ROWS, int D>
 __device__ __forceinline__ float2* part_stats(const Args& a, int place) {
   return (float2*)(a.parts + 8 * (a.most_joints + 1) + (int64_t)a.places * (ROWS * D)) + (int64_t)place * ROWS;
+}
+
+// Where the sum of channel ch (a multiple of 2) of row r of a tile lies.  Few rows: row by row.  Many: as the accumulators of
+// v_mfma_f32_32x32x16 have it, so that a wavefront stores 1 KiB at a time: four channels of 32 rows side by side.
+template <int ROWS, int D>
+__device__ __forceinline__ int part_at(int r, int ch) {
+  return ROWS < RF2_PAGED_ROWS_MANY ? r * D + ch : (r / 32 * (D / 4) + ch / 4) * 128 + r % 32 * 4 + ch % 4;
 }
 
 // Rows of a joint: a workgroup of join_kernel has 32 lanes for each, and more where there are few rows and many parts.
@@ -158,8 +196,8 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     work += (float)tiles * (float)units_of(s.len);
     tokens += (float)s.n_new;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) work += __shfl_xor(work, d), tokens += __shfl_xor(tokens, d);
+  work = wave_total(work);
+  tokens = wave_total(tokens);
   // Rows that overlap, which no table of this library has, can be more than the grid and the workspace are made for: nothing is done.
   // (Sums up to 2^24 are exact, n_tokens is at most 2^20.)
   const int n_seqs = uniform(tokens <= (float)a.n_tokens) ? a.n_seqs : 0;
@@ -174,7 +212,8 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     const float per = 1.f / (float)mine;
     float items = 0.f, cut = 0.f, longest = 0.f;
     for (int i = 0; i < a.n_seqs; ++i) {
-      const float n = (float)__builtin_amdgcn_readlane(tiles, i), u = (float)__builtin_amdgcn_readlane(units_of(s.len), i);
+      const float n = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)tiles), i));
+      const float u = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)units_of(s.len)), i));
       const float c = ceilf(u * per);
       items += n * c;
       cut += c > 1.f ? n * c : 0.f;
@@ -182,9 +221,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     }
     const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
     float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + 3.f * cut / fmaxf(items, 1.f))) + (longest - mean);
-    float best = cost;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) best = fminf(best, __shfl_xor(best, d));
+    const float best = wave_least(cost);
     const uint64_t those = __builtin_amdgcn_ballot_w64(cost <= best);
     units = __builtin_amdgcn_readlane(mine, those == 0 ? 63 : __builtin_ctzll(those));
   }
@@ -226,7 +263,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
 
 // Keys that row r of a sequence sees.
 __device__ __forceinline__ int limit_of(const Args& a, const Seq& s, int row) {
-  return a.causal ? min(max(s.len - s.n_new + row / a.group + 1, 0), s.len) : s.len;
+  return a.causal ? min(max(s.len - s.n_new + token_of(a, row) + 1, 0), s.len) : s.len;
 }
 // Units of a tile whose rows end before row `end`, and parts of it.
 template <int ROWS>
@@ -238,6 +275,13 @@ __device__ __forceinline__ const unsigned char* uniform_ptr(const void* p) {
   const uint64_t v = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
   return (const unsigned char*)(((uint64_t)hi << 32) | lo);
+}
+
+// Place of 16-byte chunk `chunk` of row `row` among rows of CPR chunks in LDS: 16 lanes that move the same chunk of neighbouring
+// rows, or the chunks of a row in turn, meet different banks.
+template <int CPR>
+__device__ __forceinline__ int row_slot(int row, int chunk) {
+  return row * CPR + (chunk ^ (row / (16 / CPR) % CPR));
 }
 
 // What a wavefront of a part does.
@@ -278,16 +322,22 @@ __device__ __forceinline__ bool enter(const Args& a, int first, int kw, Part& w,
 template <int WINDOW>
 __device__ __forceinline__ void list_pages(const Args& a, const int32_t* table, int2* pages, int p, int p1, int begin, int stop, int& x0, int& x1) {
   const int lane = (int)threadIdx.x & 63;
-  int ids[WINDOW / 64], n = 0;
-#pragma unroll
-  for (int i = 0; i < WINDOW / 64; ++i) ids[i] = table[min(p + 64 * i + lane, a.max_pages - 1)];
-  wave_fence();
-#pragma unroll
-  for (int i = 0; i < WINDOW / 64; ++i) {
-    const bool there = p + 64 * i + lane < p1 && (unsigned)ids[i] < (unsigned)a.n_pages;
+  int n = 0;
+  const auto note = [&](int id, int column) __attribute__((always_inline)) {
+    const bool there = column < p1 && (unsigned)id < (unsigned)a.n_pages;
     const uint64_t some = __builtin_amdgcn_ballot_w64(there);
-    if (there) pages[n + __popcll(some & ((1ull << lane) - 1))] = make_int2(ids[i], p + 64 * i + lane);
+    if (there) pages[n + __popcll(some & ((1ull << lane) - 1))] = make_int2(id, column);
     n += __popcll(some);
+  };
+  wave_fence();
+  if (p1 - p <= 64) {                                        // (the usual length of a part: one request)
+    note(table[min(p + lane, a.max_pages - 1)], p + lane);
+  } else {
+    int ids[WINDOW / 64];
+#pragma unroll
+    for (int i = 0; i < WINDOW / 64; ++i) ids[i] = table[min(p + 64 * i + lane, a.max_pages - 1)];
+#pragma unroll
+    for (int i = 0; i < WINDOW / 64; ++i) note(ids[i], p + 64 * i + lane);
   }
   wave_fence();
   const int per = 1 << a.unit_shift;
@@ -392,7 +442,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
   x8 qf[2][DS];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const int r = min(row_of(q), sp.n_rows - 1), t = r / a.group, head = sp.kv_head * a.group + r % a.group;
+    const int r = min(row_of(q), sp.n_rows - 1), t = token_of(a, r), head = sp.kv_head * a.group + r - t * a.group;
     const typename T::x1* const from = (const typename T::x1*)a.q + (w.s.first + t) * a.q_stride + head * D + 8 * lh;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) qf[q][ds] = *reinterpret_cast<const x8*>(from + 16 * ds);
@@ -409,9 +459,14 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
       for (int i = 0; i < 16; ++i) o[q][dt][i] = 0.f;
   }
 
+  // Keys that the wavefront's rows see; in LDS, where they are hardly ever read.
+  __shared__ int row_limits[2][64];
+  int* const limits = row_limits[wave];
+  limits[lane] = limit_of(a, w.s, min(sp.row0 + lane, sp.n_rows - 1));
+  wave_fence();
   // Keys of unit u that a row does not see.
   auto mask = [&](f32x16& S, int q, int u) __attribute__((always_inline)) {
-    const int left = limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - 4 * lh;
+    const int left = limits[32 * q + l32] - 32 * u - 4 * lh;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (8 * (i / 4) + i % 4 >= left) S[i] = -INFINITY;
@@ -468,7 +523,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
       __builtin_amdgcn_sched_barrier(0);     // (one operand after the other: there are no registers for more)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const bf16x8 sees = seen(limit_of(a, w.s, min(row_of(q), sp.n_rows - 1)) - 32 * u - 16 * (j % 2) - 4 * lh);
+        const bf16x8 sees = seen(limits[32 * q + l32] - 32 * u - 16 * (j % 2) - 4 * lh);
         o[q][j / 2] = Bf16::mfma(infinities<T, false>(v[j]), sees, o[q][j / 2]);
         __builtin_amdgcn_sched_barrier(0);
         o[q][j / 2] = Bf16::mfma(infinities<T, true>(v[j]), sees, o[q][j / 2]);
@@ -764,33 +819,48 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
     }
   }
 
+  // Results leave as whole rows, through LDS (8 or 16 bytes a lane at a stride of a row keep the address unit of a compute unit busy
+  // for 64 cycles an instruction); sums of a part as the registers have them (see part_at).
+  __shared__ uint4 out_rows[2][32 * (D / 8)];
+  uint4* const staged = out_rows[wave];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     // sums of the two lane halves, which have different keys of a row
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[q]), __float_as_uint(l[q]), false, false);
     l[q] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    const int r = row_of(q) - w.tile * ROWS;
-    if (row_of(q) >= sp.n_rows) continue;
-    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + sp.kv_head * a.group + row_of(q) % a.group;
-    const float f = weight_of(l[q]);
-    float* const part = part_sums<ROWS, D>(a, w.place) + r * D;
+    const int first = sp.row0 + 32 * q;        // of the tile's rows
+    if (!sp.whole) {
+      if (row_of(q) < sp.n_rows) {
+        const int r = row_of(q) - w.tile * ROWS;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int ch = 32 * dt + 8 * g + 4 * lh;
-        if (sp.whole) {
-          typename T::x4 pk;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(o[q][dt][4 * g + e] * f);
-          *reinterpret_cast<typename T::x4*>((typename T::x1*)a.o + out_row * D + ch) = pk;
-        } else {
-          *reinterpret_cast<float4*>(part + ch) = make_float4(o[q][dt][4 * g], o[q][dt][4 * g + 1], o[q][dt][4 * g + 2], o[q][dt][4 * g + 3]);
-        }
+        for (int x = 0; x < 4 * DT; ++x)
+          *reinterpret_cast<float4*>(part_sums<ROWS, D>(a, w.place) + part_at<ROWS, D>(r, 8 * x + 4 * lh)) =
+              make_float4(o[q][x / 4][4 * (x % 4)], o[q][x / 4][4 * (x % 4) + 1], o[q][x / 4][4 * (x % 4) + 2], o[q][x / 4][4 * (x % 4) + 3]);
+        if (lh == 0) part_stats<ROWS, D>(a, w.place)[r] = make_float2(m[q], l[q]);
       }
-    if (lh == 0) {
-      if (!sp.whole) part_stats<ROWS, D>(a, w.place)[r] = make_float2(m[q], l[q]);
-      else if (a.lse != nullptr) a.lse[out_row] = lse_of(m[q], l[q]);
+      continue;
+    }
+    const float f = weight_of(l[q]);
+    wave_fence();
+#pragma unroll
+    for (int x = 0; x < 4 * DT; ++x) {
+      typename T::x4 pk;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[e] = (typename T::x1)(o[q][x / 4][4 * (x % 4) + e] * f);
+      reinterpret_cast<typename T::x4*>(&staged[row_slot<D / 8>(l32, x)])[lh] = pk;
+    }
+    wave_fence();
+    if (a.lse != nullptr && lh == 0 && row_of(q) < sp.n_rows) {
+      const int t = token_of(a, row_of(q));
+      a.lse[(int64_t)(w.s.first + t) * a.heads + (sp.kv_head - t) * a.group + row_of(q)] = lse_of(m[q], l[q]);
+    }
+    constexpr int CPR = D / 8, STEP = 64 / CPR;      // 16-byte chunks of a row, rows that the wavefront moves at a time
+#pragma unroll
+    for (int i = 0; i < 32 / STEP; ++i) {
+      const int r = lane / CPR + i * STEP, row = first + r, t = token_of(a, row);
+      const uint4 piece = staged[row_slot<CPR>(r, lane % CPR)];
+      if (row < sp.n_rows)
+        *reinterpret_cast<uint4*>((typename T::x1*)a.o + ((int64_t)(w.s.first + t) * a.heads + (sp.kv_head - t) * a.group + row) * D + lane % CPR * 8) = piece;
     }
   }
 }
@@ -814,7 +884,7 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
   x8 qf[QT][CS];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    const int r = min(row_of(q), sp.n_rows - 1), t = r / a.group, head = sp.kv_head * a.group + r % a.group;
+    const int r = min(row_of(q), sp.n_rows - 1), t = token_of(a, r), head = sp.kv_head * a.group + r - t * a.group;
     const typename T::x1* const from = (const typename T::x1*)a.q + (w.s.first + t) * a.q_stride + head * D + 8 * lq;
 #pragma unroll
     for (int cs = 0; cs < CS; ++cs) qf[q][cs] = *reinterpret_cast<const x8*>(from + 32 * cs);
@@ -1012,7 +1082,8 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
       }
     }
     if (row_of(q) >= sp.n_rows) continue;
-    const int64_t out_row = (int64_t)(w.s.first + row_of(q) / a.group) * a.heads + sp.kv_head * a.group + row_of(q) % a.group;
+    const int t = token_of(a, row_of(q));
+    const int64_t out_row = (int64_t)(w.s.first + t) * a.heads + (sp.kv_head - t) * a.group + row_of(q);
     const float f = weight_of(sum);
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
@@ -1072,7 +1143,7 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
       for (int i = 0; i < DEEP; ++i) {
         const int p = p0 + i * every, place = j.place + min(p, j.parts - 1) * j.step, row = j.row % ROWS + r;
         st[i] = part_stats<ROWS, D>(a, place)[row];
-        x[i] = *reinterpret_cast<const fE*>(part_sums<ROWS, D>(a, place) + row * D + lane * E);
+        x[i] = *reinterpret_cast<const fE*>(part_sums<ROWS, D>(a, place) + part_at<ROWS, D>(row, lane * E));
         if (p >= j.parts) st[i] = make_float2(-FLT_MAX, 0.f), x[i] = (fE)0.f;
       }
       float most = st[0].x;
@@ -1096,7 +1167,8 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
     if (!there || (half & (every - 1)) != 0) continue;
     const float f = weight_of(sum);
     const int row = j.row + r;
-    const int64_t out = (int64_t)(j.first + row / a.group) * a.heads + j.head * a.group + row % a.group;
+    const int t = token_of(a, row);
+    const int64_t out = (int64_t)(j.first + t) * a.heads + (j.head - t) * a.group + row;
     tE pk;
 #pragma unroll
     for (int e = 0; e < E; ++e) pk[e] = (typename T::x1)(acc[e] * f);
@@ -1164,6 +1236,10 @@ extern "C" int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_
   a.parts = (float*)workspace, a.o = o, a.lse = lse;
   a.q_stride = q_stride;
   a.n_seqs = n_seqs, a.n_tokens = n_tokens, a.heads = c.heads, a.kv_heads = c.kv_heads, a.group = c.heads / c.kv_heads;
+  uint32_t k = 0;
+  while ((1 << k) < a.group) ++k;
+  a.group_shift = 29 + k;
+  a.group_magic = (uint32_t)((((uint64_t)1 << a.group_shift) + a.group - 1) / a.group);
   a.unit_shift = __builtin_ctz((unsigned)c.page) - 5;
   a.n_pages = c.n_pages, a.max_pages = c.max_pages, a.causal = c.causal;
   a.scale_log2 = plan->scale_log2;
