@@ -1104,8 +1104,8 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
   }
 }
 
-// Adds the parts of the tiles that are cut.  A workgroup takes a joint at a time, 32 lanes to a row; where there are fewer than 8
-// rows, 2, 4 or 8 times 32 lanes share the parts of one.
+// Adds the parts of the tiles that are cut.  A workgroup takes a joint at a time, 32 lanes to a row; of few rows 2, 4 or 8 times 32
+// lanes share the parts of one.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Args a) {
   constexpr int E = D / 32, DEEP = 8;              // channels of a lane; parts asked for at a time
@@ -1113,14 +1113,16 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
   typedef __attribute__((ext_vector_type(E))) typename T::x1 tE;
   __shared__ fE sums[8][32];
   __shared__ float2 totals[8];
-  const int half = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  // Of many rows, neighbouring lanes take neighbouring rows: their sums lie side by side.
+  constexpr bool MANY = ROWS >= RF2_PAGED_ROWS_MANY;
+  const int half = MANY ? (int)threadIdx.x & 7 : (int)threadIdx.x >> 5, lane = MANY ? (int)threadIdx.x >> 3 : (int)threadIdx.x & 31;
   // (the first joint is asked for beside their number: there is memory for it either way)
   const int count = *joints_count(a);
   Joint j = joints(a)[blockIdx.x];
   for (int task = (int)blockIdx.x; task < count; task += (int)gridDim.x) {
     if (task != (int)blockIdx.x) j = joints(a)[task];
     if (j.parts == 0) continue;
-    const int share = j.n_rows > 4 ? 0 : j.n_rows > 2 ? 1 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
+    const int share = MANY || j.n_rows > 4 ? 0 : j.n_rows > 2 ? 1 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
     const bool there = r < j.n_rows;
     fE acc = (fE)0.f;
     float top = -FLT_MAX, sum = 0.f;
