@@ -30,6 +30,7 @@ CASES = {
     "chunk": dict(new=[300], ctx=[77], heads=4, kv=2, d=128, page=64),
     "chunk_fp16": dict(new=[513], ctx=[1000], heads=8, kv=8, d=128, page=128, dtype=FP),
     "chunk_d64": dict(new=[257], ctx=[64], heads=12, kv=4, d=64, page=32),
+    "chunk_group_11": dict(new=[2900], ctx=[100], heads=11, kv=1, d=64, page=64),
     "chunk_long": dict(new=[130], ctx=[6000], heads=8, kv=8, d=128, page=64),
     "prompts": dict(new=[200, 1, 77, 640, 33], ctx=[0, 500, 31, 129, 2000], heads=8, kv=2, d=128, page=32),
     "prompts_d64": dict(new=[200, 1, 77, 640, 33], ctx=[0, 500, 31, 129, 2000], heads=16, kv=8, d=64, page=256, dtype=FP),
@@ -303,6 +304,46 @@ def test_streams_and_workspaces():
             plan.rf2_paged_attn(b.q, b.k_cache, b.v_cache, b.table, b.seq_len, b.cu, ws, o, None, st)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of different batches, the same workspace, replayed in turn beside eager calls: none keeps anything in it."""
+    batches = [Batch(seed=16, new=[1, 1, 1], ctx=[9000, 4000, 10], heads=8, kv=2, d=128, page=64),
+               Batch(seed=17, new=[300, 2], ctx=[2000, 700], heads=8, kv=2, d=128, page=64)]
+    plans = [b.plan() for b in batches]
+    wants = [b.run(p)[0] for b, p in zip(batches, plans)]
+    space = plans[0].alloc_workspace()
+    outs = [torch.zeros_like(w) for w in wants]
+
+    def call(i):
+        b = batches[i]
+        plans[i].rf2_paged_attn(b.q, b.k_cache, b.v_cache, b.table, b.seq_len, b.cu, space, outs[i])
+
+    graphs = []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            call(i)
+        graphs.append(graph)
+    for turn in (0, 1, 1, 0, "eager", 1, 0):
+        for o in outs:
+            o.zero_()
+        for i in ((0, 1) if turn == "eager" else (turn,)):
+            call(i) if turn == "eager" else graphs[i].replay()
+            assert torch.equal(outs[i], wants[i])
+
+
+def test_sequences_that_share_pages():
+    """A prompt's pages in the rows of several sequences: each reads them as its own."""
+    b = Batch(seed=18, new=[1, 1, 3, 1], ctx=[1000, 1040, 1100, 7], heads=8, kv=2, d=128, page=64)
+    table = b.table.clone()
+    for s in (1, 2):
+        table[s, :10] = table[0, :10]
+        b.k[s][:640], b.v[s][:640] = b.k[0][:640], b.v[0][:640]
+    b.table = table
+    o, lse = b.run(b.plan())
+    b.check(o, lse)
 
 
 def test_nothing_to_do():

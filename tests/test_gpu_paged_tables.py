@@ -160,6 +160,28 @@ def test_store(kind, kv, d, page, dtype):
     assert torch.equal(buf["v_cache"].cpu().view(torch.int16), v_want.view(torch.int16))
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_store_of_many_sequences(seed):
+    """Runs of neighbouring slots as appends leave them, of random lengths from random places of pages in random order; some are -1."""
+    rng = np.random.default_rng(seed)
+    page, kv, d, n_pages = int(rng.choice([32, 64, 128, 256])), int(rng.choice([1, 3, 8])), int(rng.choice([64, 128])), 40
+    order, slots = rng.permutation(n_pages), []
+    for p in order[:25]:
+        first, n = int(rng.integers(0, page)), int(rng.choice([1, 2, 7, 31, 32, 33, 300]))
+        slots += [int(p) * page + r for r in range(first, min(page, first + n))]
+        slots += [-1] * int(rng.choice([0, 0, 0, 1, 40]))
+    plan = rf2.PagedPlan(heads=kv, kv_heads=kv, head_dim=d, page=page, n_pages=n_pages, max_seqs=1, max_pages=1, max_tokens=len(slots))
+    buf = plan.alloc()
+    buf["k_cache"].fill_(3.0)
+    buf["v_cache"].fill_(4.0)
+    k_want, v_want = buf["k_cache"].cpu(), buf["v_cache"].cpu()
+    k, v = torch.randn(len(slots), 2 * kv, d, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).cuda().split(kv, 1)
+    plan.rf2_paged_store(k, v, ints(slots), buf["k_cache"], buf["v_cache"])
+    ref.put(k_want, v_want, slots, k.cpu(), v.cpu(), page)
+    assert torch.equal(buf["k_cache"].cpu().view(torch.int16), k_want.view(torch.int16))
+    assert torch.equal(buf["v_cache"].cpu().view(torch.int16), v_want.view(torch.int16))
+
+
 def test_store_of_the_same_slot_twice_leaves_one_of_the_two():
     plan = rf2.PagedPlan(heads=1, kv_heads=1, head_dim=64, page=32, n_pages=2, max_seqs=1, max_pages=1, max_tokens=64)
     buf = plan.alloc()
