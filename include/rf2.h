@@ -276,7 +276,8 @@ typedef struct {
   int32_t page;            /* tokens of a page, in {32, 64, 128, 256} */
   int32_t n_pages;         /* pages of the pool; n_pages * page <= 2^30 */
   int32_t max_seqs;        /* sequences of a call at most, <= 4096 */
-  int32_t max_pages;       /* pages of a sequence at most = row length of the block table; max_pages * page <= 2^24 */
+  int32_t max_pages;       /* pages of a sequence at most = row length of the block table; max_pages * page <= 2^24,
+                              max_seqs * max_pages <= 2^30 */
   int32_t max_tokens;      /* new tokens of a call at most, all sequences together, <= 2^20 */
   int32_t dtype;           /* RF2_DTYPE_*: q, k, v, o and both caches */
   int32_t causal;          /* 1: a token sees the tokens of its sequence up to itself; 0: all that are cached, its whole

@@ -20,6 +20,7 @@ int rf2_paged_plan_create(const rf2_paged_config* cfg, rf2_paged_plan** out) {
   if (c.heads > 512 || c.max_seqs > RF2_PAGED_MAX_SEQS || c.max_tokens > 1 << 20) return RF2_ERR_UNSUPPORTED;
   if ((int64_t)c.n_pages * c.page > (int64_t)1 << 30) return RF2_ERR_UNSUPPORTED;    // slots in int32
   if ((int64_t)c.max_pages * c.page > (int64_t)1 << 24) return RF2_ERR_UNSUPPORTED;  // 16 Mi tokens, as a layer has at most
+  if ((int64_t)c.max_seqs * c.max_pages > (int64_t)1 << 30) return RF2_ERR_UNSUPPORTED;    // entries of the table in int32
 
   rf2_paged_plan* p = new (std::nothrow) rf2_paged_plan();
   if (!p) return RF2_ERR_ALLOC;

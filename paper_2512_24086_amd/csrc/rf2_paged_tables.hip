@@ -200,7 +200,6 @@ __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
   }
   block_sums<NT>(across, before, rows, all64, all_rows, flags);
   int status = flags;
-  if (all64 > INT32_MAX) status |= RF2_PAGED_POOL_FULL;     // (more than any pool has)
   const int all = status ? 0 : (int)all64, n_rows = (int)all_rows;
   if (!status) {
     for (int s = s0; s < s1; ++s) {
@@ -214,24 +213,48 @@ __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
     if (threadIdx.x == 0) first[n_rows] = all;
   }
   __syncthreads();
-  // Entries of a round that begin at `at` for this wavefront.  Its place among the sequences only moves on.
+  // Entries of a round that begin at `at` for this wavefront.  Its place among the sequences only moves on.  Where the 64
+  // sequences from there on begin stands in its lanes, so that a step from one to the next is a step of the scalar unit.
   int place = 0;
   auto look = [&](int at, int (&entry)[DEEP]) __attribute__((always_inline)) {
+    int begins = 0, row = 0, held = 0;               // of sequence place + lane; of how many this is known
+    auto hold = [&]() __attribute__((always_inline)) {
+      begins = first[min(place + lane, n_rows)];
+      row = which[min(place + lane, max(n_rows - 1, 0))];
+      held = min(64, n_rows - place);
+    };
+    if (at < all) {
+      while (true) {                                 // (64 sequences' ends at a time)
+        const int next = place + 1 + lane;
+        const int passed = __popcll(__builtin_amdgcn_ballot_w64(next < n_rows && first[min(next, n_rows)] <= at));
+        place += passed;
+        if (passed < 64) break;
+      }
+      hold();
+    }
+    int k = 0;                                       // the sequence looked at is number place + k
 #pragma unroll
     for (int j = 0; j < DEEP; ++j) {
       const int from = at + 64 * j, i = from + lane;
       entry[j] = -1;
       if (from >= all) continue;
-      while (true) {                                 // (64 sequences' ends at a time)
-        const int next = place + 1 + lane;
-        const int passed = __popcll(__builtin_amdgcn_ballot_w64(next < n_rows && first[min(next, n_rows)] <= from));
-        place += passed;
-        if (passed < 64) break;
-      }
-      int s = place;
-      while (s + 1 < n_rows && first[s + 1] <= i) ++s;
-      if (i < all) entry[j] = a.table[(int64_t)which[s] * a.max_pages + (i - first[s])];
+      int64_t cell = 0;                              // of entry i in the table
+      bool more;
+      do {                                           // sequences that begin before the end of the 64 entries
+        const int begin = __builtin_amdgcn_readlane(begins, k), seq = __builtin_amdgcn_readlane(row, k);
+        if (i >= begin) cell = (int64_t)seq * a.max_pages + (i - begin);
+        int next = k + 1;
+        if (next == held && place + held < n_rows) {
+          place += k;                                // (the last one stays: entries of it may follow)
+          hold();
+          k = 0, next = 1;
+        }
+        more = next < held && __builtin_amdgcn_readlane(begins, next & 63) < from + 64;
+        if (more) k = next;
+      } while (more);
+      if (i < all) entry[j] = a.table[cell];
     }
+    place += k;
   };
   // How many pages stand before the wavefront's entries in the round, and how many there are in all.
   int turn = 0;

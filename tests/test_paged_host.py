@@ -23,7 +23,8 @@ def test_invalid_configurations(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(head_dim=96), dict(head_dim=0), dict(page=16), dict(page=48), dict(page=512), dict(heads=514), dict(max_seqs=4097),
-                                 dict(max_tokens=(1 << 20) + 1), dict(n_pages=(1 << 24) + 1), dict(max_pages=(1 << 18) + 1)], ids=str)
+                                 dict(max_tokens=(1 << 20) + 1), dict(n_pages=(1 << 24) + 1), dict(max_pages=(1 << 18) + 1),
+                                 dict(max_seqs=4096, max_pages=(1 << 18) + 1, page=32)], ids=str)
 def test_unsupported_configurations(bad):
     with pytest.raises(rf2.Rf2Error) as e:
         make(**bad)
