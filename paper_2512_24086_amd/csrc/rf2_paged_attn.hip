@@ -209,15 +209,17 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     // in units; START more for a part's first loads and its last stores, three times that where sums are written and joined.
     constexpr float START = 8.f;
     const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
-    const float per = 1.f / (float)mine;
-    float items = 0.f, cut = 0.f, longest = 0.f;
-    for (int i = 0; i < a.n_seqs; ++i) {
-      const float n = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)tiles), i));
-      const float u = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)units_of(s.len)), i));
-      const float c = ceilf(u * per);
-      items += n * c;
-      cut += c > 1.f ? n * c : 0.f;
-      longest = n > 0.f ? fmaxf(longest, fminf(u, (float)mine)) : longest;
+    const float per = 1.f / (float)mine, my_tiles = (float)tiles, my_units = (float)units_of(s.len);
+    const float longest = fminf(-wave_least(tiles > 0 ? -my_units : 0.f), (float)mine);
+    float items = 0.f, cut = 0.f;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 4) {       // (lanes without a sequence have no tiles)
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        const float n = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_tiles), i));
+        const float c = ceilf(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_units), i)) * per);
+        items = fmaf(n, c, items);
+        cut = fmaf(c > 1.f ? n : 0.f, c, cut);
+      }
     }
     const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
     float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + 3.f * cut / fmaxf(items, 1.f))) + (longest - mean);
