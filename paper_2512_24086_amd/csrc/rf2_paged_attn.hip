@@ -2,20 +2,27 @@
 //
 // Rows.  The query heads that share a K/V head are rows side by side: row r of a sequence and K/V head h is token r / G,
 // query head h G + r % G (G = heads / kv_heads), so a step of single tokens has G rows to a product and a chunk n G.  A
-// workgroup owns a tile of these rows.
+// workgroup owns a tile of these rows: 16 or 32 where a sequence has few (few_attn_kernel, bound by memory), 128 where it has
+// many (many_attn_kernel, bound by the matrix cores).
 //
 // Parts.  A tile's keys are cut into parts of `units` units of 32 keys, counted from key 0 for all tiles of a sequence; the
 // workgroups of one part of different tiles run at the same time and find each other's keys in the caches.  With
-//     W = sum over sequences of tiles * units(length),   units = max(least, ceil(W / aimed)),
+//     W = sum over sequences of tiles * units(length),   units >= max(least, W / aimed),
 // a sequence that is cut (c = ceil(units(length) / units) >= 2) has c < 2 units(length) / units parts to a tile, all of them
-// less than 2 W / units <= 2 aimed: the size of the workspace.  The lengths are in device memory, so every workgroup works
-// this out for itself and finds its own part; the grid is the most there can be.
+// less than 2 W / units <= 2 aimed: the size of the workspace.  Few rows take the least such number; for many, and up to 64
+// sequences, it is searched for (find_part).  The lengths are in device memory, so every workgroup works this out for itself
+// and finds its own part: 2 to 4 us with up to 16 sequences, 5 with 64.  (A kernel before that did it once would cost as much and
+// a launch.)  The grid is the most there can be; workgroups without a part leave.
 //
-// Products as in rf2_attn.hip: S^T = K Q^T, O^T = V^T P^T (v_mfma_f32_32x32x16), operands from the cache's tiles straight
-// into registers, P the accumulators of S^T.
+// Sums.  The sums of a tile that is cut go to the workspace in fp32; its first part lists its rows there (Joint), and a second
+// launch, join_kernel, adds what is listed in the order of the parts: no atomics, the same bits each time.
+//
+// Products: S^T = K Q^T, O^T = V^T P^T, operands from the cache's tiles straight into registers, 1 KiB an instruction; P is what
+// the accumulators of S^T hold, rounded: the cache's order of keys is theirs.
 //
 // Softmax: a probability is exp2(q.k c - m), c = scale log2(e), with a reference m per row that is moved only when the sum
-// of a unit's probabilities leaves the range that P's type carries (as in rf2_attn.hip).  Sums are fp32, of unrounded P.
+// of a unit's probabilities leaves the range that P's type carries: no maximum per unit, and O is hardly ever rescaled.  Sums are
+// fp32, of unrounded P.
 #include "rf2_paged.h"
 
 #include <cfloat>
@@ -204,9 +211,12 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
   int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
   if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
-    // Where tiles are long, how many of them and of their parts fill the chip's places (for at_once workgroups) counts.  Lane i holds what
-    // a launch takes with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more,
-    // in units; START more for a part's first loads and its last stores, three times that where sums are written and joined.
+    // How many parts there are and how they fill the chip's places (for at_once workgroups) counts.  Lane i holds what a launch takes
+    // with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more, in units; START
+    // more a round for first loads and last stores, three times that for each chip full of parts whose sums are written and joined.
+    // (As many parts as are aimed at, without a search: one prompt of 100 tokens behind 32,000 at 32 heads on 8 87 us, 74 with it; 16
+    // chunks of 32 behind 4,000 96 and 76; 16 sequences of which two have chunks, D = 64, 24.4 and 27.5: the search itself takes one.
+    // START 4: 12 prompts 90 us for 83.6; 16: the same.)
     constexpr float START = 8.f;
     const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
     const float per = 1.f / (float)mine, my_tiles = (float)tiles, my_units = (float)units_of(s.len);
@@ -221,8 +231,8 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
         cut = fmaf(c > 1.f ? n : 0.f, c, cut);
       }
     }
-    const float heads = (float)a.kv_heads, mean = work / fmaxf(items, 1.f);
-    float cost = ceilf(items * heads / (float)a.at_once) * (mean + START * (1.f + 3.f * cut / fmaxf(items, 1.f))) + (longest - mean);
+    const float share = (float)a.kv_heads / (float)a.at_once, mean = work / fmaxf(items, 1.f);
+    const float cost = ceilf(items * share) * (mean + START) + 3.f * START * cut * share + (longest - mean);
     const float best = wave_least(cost);
     const uint64_t those = __builtin_amdgcn_ballot_w64(cost <= best);
     units = __builtin_amdgcn_readlane(mine, those == 0 ? 63 : __builtin_ctzll(those));
@@ -428,7 +438,17 @@ __device__ __forceinline__ bf16x8 seen(int left) {
 __device__ __forceinline__ float weight_of(float l) { return l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l); }
 __device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(l)) * 0.6931471805599453f; }
 
-// Many rows: two wavefronts of 64 rows each (two tiles of 32) walk a part's keys.
+// Many rows: two wavefronts of 64 rows each (two tiles of 32) walk a part's keys (v_mfma_f32_32x32x16).  64 rows, for each of
+// K's and V's bytes from the caches serves two products, and what a wavefront holds (D = 128: O 128, Q 64, S and P of two units 96,
+// operands of two units 128 registers) just fits into the 512 of a SIMD.  One wavefront to a SIMD has to hide everything by itself:
+// a step does S of the next unit, O += V P of the one before and the softmax of the present one, operand by operand, a load into an
+// operand's registers right behind the products that read it, two steps ahead for K and one for V.  At D = 64 half a step apart is
+// enough and two wavefronts share a SIMD.
+//
+// Bound by the matrix cores, which hold the card at about 1.7 GHz here (power): 4,680 tokens over 32,760 keys, 40 heads, full, bf16,
+// D = 128: 2,480 us, 1,270 TFLOP/s, matrix cores busy in 70% of the cycles; a library product of 8192^3 reaches 1,192.  D = 64, where
+// there is as much softmax for half the products: 1,550 us, 1,010 TFLOP/s, 53%.  Five prompts (300 to 2,600 tokens, 32 heads on 8,
+// causal): 117 us, 890 TFLOP/s; there 512 workgroups run in fewer than three rounds, of which the last leaves 12% of the places empty.
 template <class T, int D>
 __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a) {
   constexpr int DS = D / 16, DT = D / 32, ROWS = RF2_PAGED_ROWS_MANY;
@@ -872,6 +892,8 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
 // of the second eight more, and a lane's eight probabilities are the eight keys of storage group lane / 16.
 //
 // Bound by memory: operands of two units are on their way (each is asked for as soon as the one two before has been read).
+// 64 single tokens over 0.79 GB of keys and values: 131 us, 6.0 TB/s; four over 0.58 GB, 20,000 to 110,000 keys each: 105 us, 5.6 TB/s
+// (a kernel that only reads reaches 6.5, one that copies 6.2).  One token over 200 keys takes 5.8 us, of which 0.1 are its bytes.
 template <class T, int D, int QT>
 __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kernel(Args a) {
   constexpr int KW = 4, CS = D / 32, CT = D / 16, ROWS = 16 * QT;
@@ -1106,7 +1128,7 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
   }
 }
 
-// Adds the parts of the tiles that are cut.  A workgroup takes a joint at a time, 32 lanes to a row; of few rows 2, 4 or 8 times 32
+// Adds the parts of the tiles that are cut: 4 to 7 us, with nothing listed too, most of it the launch.  A workgroup takes a joint at a time, 32 lanes to a row; of few rows 2, 4 or 8 times 32
 // lanes share the parts of one.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Args a) {
