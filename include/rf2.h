@@ -323,6 +323,8 @@ int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_token
 /*
  * Gives back the pages of the sequences s with done[s] != 0: the entries of the first ceil(seq_len[s] / page) columns of
  * their rows that are pages (others are holes) go on top of the stack, in order of s and column.  All or nothing.
+ * There are no reference counts: a page that stands in several rows (attention reads it through each) is given back once for each of
+ * them that is done, so a program that shares pages makes all but the last of those entries holes first.
  *   done       : [n_seqs] uint8                                                            (in)
  *   seq_len, block_table, n_free : as above                                                (in)
  *   free_pages : [n_pages] int32, written behind its first n_free entries                  (in, out)
@@ -345,6 +347,7 @@ int rf2_paged_release(const rf2_paged_plan* plan, int32_t n_seqs, const uint8_t*
  *             (P, head, r / 32, r % 32 / 16 * 2 + r % 8 / 4, c, r % 16 / 8 * 4 + r % 4): the operand order of
  *             rf2_permute's vp, each group of 16 keys in the order 0-3, 8-11, 4-7, 12-15   (out)
  *             Both are read by rf2_paged_attn as matrix-core operands, 1 KiB at a time.  What no slot names stays.
+ * ceil(n_tokens / 32) * kv_heads above 2^24 - 8 is RF2_ERR_UNSUPPORTED.
  * If two tokens have the same slot, each element of it is one of theirs.
  */
 int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k, int64_t k_stride, const void* v,

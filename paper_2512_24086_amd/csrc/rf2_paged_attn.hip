@@ -1216,8 +1216,8 @@ int launch(const rf2_paged_plan* plan, Args a, Kernel kernel, int threads, int l
   const int64_t rows = (int64_t)a.n_tokens * a.group, some = std::min(a.n_seqs, a.n_tokens);
   const int64_t tiles = std::min(rows / ROWS + some, (int64_t)a.n_tokens * ((a.group + ROWS - 1) / ROWS));
   const bool can_be_cut = (int64_t)c.max_pages * c.page > 32 * a.least;
+  // (2^20 tokens of 512 heads and 4,096 sequences are less than 2^30 threads)
   const int64_t grid = (tiles + (can_be_cut ? a.aimed : 0)) * c.kv_heads;
-  if (grid * threads >= (int64_t)1 << 32) return RF2_ERR_UNSUPPORTED;
   kernel<<<dim3((unsigned)grid), dim3(threads), 0, st>>>(a);
   RF2_LAUNCH_CHECK();
   if (can_be_cut) {
@@ -1232,7 +1232,9 @@ template <class T, int D>
 int dispatch(const rf2_paged_plan* plan, const Args& a, hipStream_t st) {
   // Up to 32 rows a sequence on average: four wavefronts share the keys of one or two tiles of 16.  More: two wavefronts of 64 rows.
   // (16 sequences of 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 62.1 as one of 128; 128 rows: 131 and 78.6.)
-  // No sequence is cut below 16 units (for single tokens of 2,000 keys 13.1 us, 16.2 with 32), and 8.
+  // (16 rows as a tile of 16 or one of 32: 64 single tokens 130.3 and 132.5 us, 16 chunks of 4 tokens behind 4,000 53.5 and 54.9.)
+  // No sequence is cut below 16 units (a single token of 2,000 keys 13.1 us, 16.2 with 32), and 8 (with 16 two chunks
+  // and 14 single tokens take 3% longer; with 4 as long).
   const int64_t rows = (int64_t)a.n_tokens * a.group;
   if (rows <= 16 * (int64_t)a.n_seqs) return launch<T, D, 16>(plan, a, few_attn_kernel<T, D, 1>, 256, 16, 512, st);
   if (rows <= 32 * (int64_t)a.n_seqs) return launch<T, D, 32>(plan, a, few_attn_kernel<T, D, 2>, 256, 16, 512, st);

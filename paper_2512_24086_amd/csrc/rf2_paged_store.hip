@@ -5,6 +5,10 @@
 // of a channel side by side (V).  V goes out 16 bytes a lane where the tokens fill the eight keys of a storage group (0-3 and
 // 8-11, or 4-7 and 12-15, of 16 slots), as those of a chunk do, eight bytes where they fill four keys in a row, else key by key.
 // A group belongs to the workgroup of its first token, which reads up to 11 tokens more for it.
+//
+// 4,680 tokens of 40 heads of 128 channels: 192 MB in 37 us, 5.2 TB/s (33 to 34 us the kernel by itself; a large copy reaches 6.2).  Windows
+// of 64 tokens take longer to fill a compute unit's LDS and gain nothing; stores that are not to be kept cost the lines that two
+// windows complete (44 us).  48 single tokens of 8 heads: 6.7 us, of which 0.1 are its bytes.
 #include "rf2_paged.h"
 
 namespace {
@@ -117,9 +121,10 @@ extern "C" int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, con
   if (k_stride % 8 != 0 || v_stride % 8 != 0) return RF2_ERR_INVALID_ARG;
   if (!rf2_aligned(k, 16) || !rf2_aligned(v, 16) || !rf2_aligned(k_cache, 16) || !rf2_aligned(v_cache, 16) || !rf2_aligned(slots, 4))
     return RF2_ERR_INVALID_ARG;
+  const unsigned windows = (unsigned)(n_tokens + TOKENS - 1) / TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
+  if (run >= 1u << 21) return RF2_ERR_UNSUPPORTED;         // (a grid has less than 2^32 threads)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;
-  const unsigned windows = (unsigned)(n_tokens + TOKENS - 1) / TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
   const auto launch = [&](auto kernel) {
     kernel<<<dim3(8 * run), dim3(256), 0, (hipStream_t)stream>>>((const uint16_t*)k, (const uint16_t*)v, k_stride, v_stride, slots, n_tokens,
                                                                (int64_t)c.n_pages * c.page, __builtin_ctz((unsigned)c.page), c.kv_heads,

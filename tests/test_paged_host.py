@@ -109,6 +109,12 @@ def test_arguments_are_checked_before_the_device(over, refuse):
             assert code == rf2.RF2_ERR_HIP, (name, code)        # (everything else is in order: there is no device)
 
 
+def test_more_rows_than_a_grid_has_room_for():
+    p = make(heads=512, kv_heads=512, max_tokens=1 << 20)
+    for n in (1 << 20, (1 << 20) - 31):
+        assert rf2.lib().rf2_paged_store(p._h, n, 0x10000, 512 * 64, 0x10000, 512 * 64, 0x10000, 0x10000, 0x10000, None) == rf2.RF2_ERR_UNSUPPORTED
+
+
 def test_without_a_device_nothing_computes():
     if torch.cuda.is_available():
         pytest.skip("there is a device")
