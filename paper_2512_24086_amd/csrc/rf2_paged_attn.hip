@@ -215,7 +215,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     // with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more, in units; START
     // more a round for first loads and last stores, three times that for each chip full of parts whose sums are written and joined.
     // (As many parts as are aimed at, without a search: one prompt of 100 tokens behind 32,000 at 32 heads on 8 87 us, 74 with it; 16
-    // chunks of 32 behind 4,000 96 and 76; 16 sequences of which two have chunks, D = 64, 24.4 and 27.5: the search itself takes one.
+    // chunks of 32 behind 4,000 96 and 76; 700 tokens beside 15 single ones, D = 64, 24.4 and 27.4: the search itself takes one.
     // START 4: 12 prompts 90 us for 83.6; 16: the same.)
     constexpr float START = 8.f;
     const int mine = max((int)fminf(work * 1.0001f * 64.f / ((float)a.aimed * (float)(lane + 1)), 1048576.f) + 1, a.least);
@@ -447,7 +447,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(
 //
 // Bound by the matrix cores, which hold the card at about 1.7 GHz here (power): 4,680 tokens over 32,760 keys, 40 heads, full, bf16,
 // D = 128: 2,480 us, 1,270 TFLOP/s, matrix cores busy in 70% of the cycles; a library product of 8192^3 reaches 1,192.  D = 64, where
-// there is as much softmax for half the products: 1,550 us, 1,010 TFLOP/s, 53%.  Five prompts (300 to 2,600 tokens, 32 heads on 8,
+// there is as much softmax for half the products: 1,550 us, 1,010 TFLOP/s, 53%.  Five prompts (361 to 2,397 tokens, 32 heads on 8,
 // causal): 117 us, 890 TFLOP/s; there 512 workgroups run in fewer than three rounds, of which the last leaves 12% of the places empty.
 template <class T, int D>
 __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a) {
@@ -892,7 +892,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
 // of the second eight more, and a lane's eight probabilities are the eight keys of storage group lane / 16.
 //
 // Bound by memory: operands of two units are on their way (each is asked for as soon as the one two before has been read).
-// 64 single tokens over 0.79 GB of keys and values: 131 us, 6.0 TB/s; four over 0.58 GB, 20,000 to 110,000 keys each: 105 us, 5.6 TB/s
+// 64 single tokens over 0.79 GB of keys and values: 131 us, 6.0 TB/s; four over 0.58 GB, 21,000 to 61,000 keys each: 105 us, 5.6 TB/s
 // (a kernel that only reads reaches 6.5, one that copies 6.2).  One token over 200 keys takes 5.8 us, of which 0.1 are its bytes.
 template <class T, int D, int QT>
 __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kernel(Args a) {
@@ -1233,8 +1233,8 @@ int dispatch(const rf2_paged_plan* plan, const Args& a, hipStream_t st) {
   // Up to 32 rows a sequence on average: four wavefronts share the keys of one or two tiles of 16.  More: two wavefronts of 64 rows.
   // (16 sequences of 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 62.1 as one of 128; 128 rows: 131 and 78.6.)
   // (16 rows as a tile of 16 or one of 32: 64 single tokens 130.3 and 132.5 us, 16 chunks of 4 tokens behind 4,000 53.5 and 54.9.)
-  // No sequence is cut below 16 units (a single token of 2,000 keys 13.1 us, 16.2 with 32), and 8 (with 16 two chunks
-  // and 14 single tokens take 3% longer; with 4 as long).
+  // No sequence is cut below 16 units (a single token of 2,000 keys 13.1 us, 16.2 with 32), and 8 (with 16 a chunk of 700
+  // tokens and 15 single ones take 3% longer; with 4 as long).
   const int64_t rows = (int64_t)a.n_tokens * a.group;
   if (rows <= 16 * (int64_t)a.n_seqs) return launch<T, D, 16>(plan, a, few_attn_kernel<T, D, 1>, 256, 16, 512, st);
   if (rows <= 32 * (int64_t)a.n_seqs) return launch<T, D, 32>(plan, a, few_attn_kernel<T, D, 2>, 256, 16, 512, st);

@@ -97,7 +97,7 @@ __device__ __forceinline__ void deal_slots(const AppendArgs& a, const Lengths& m
 }
 
 // One workgroup: sums, checks, lengths; with `slots` the slots too.  Every thread has a run of sequences.  Bound by its latency: 2.6 us for
-// 48 single tokens (a launch takes about 3).
+// 24 single tokens (a launch takes about 3).
 template <int NT>
 __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   __shared__ Lengths m;
@@ -179,8 +179,9 @@ struct ReleaseArgs {
   int n_seqs, page_shift, max_pages, n_pages;
 };
 
-// One workgroup; bound by the latency of its rounds: 65,000 entries of 256 sequences, a fifth of them holes, 19.7 us.  The columns of all sequences that give back stand in one row of `all` entries, of which a round takes
-// NT * DEEP, a wavefront 64 * DEEP side by side; what is a page among them goes to the next places of the stack.
+// One workgroup.  The columns of all sequences that give back stand in one row of `all` entries, of which a round takes
+// NT * DEEP, a wavefront 64 * DEEP side by side; what is a page among them goes to the next places of the stack.  Bound by what one
+// compute unit issues to find each entry's place: 29,000 entries of 264 sequences, a fifth of them holes, 19.7 us.
 template <int NT>
 __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
   constexpr int DEEP = 8, WAVES = NT / 64, OF_WAVE = 64 * DEEP;
@@ -330,7 +331,7 @@ extern "C" int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int3
   const AppendArgs a{seq_len, new_len, free_pages, n_free, block_table, seq_len_out, n_free_out, cu_new, slots, status,
                      n_seqs, n_tokens, page_shift(plan), plan->cfg.max_pages, plan->cfg.n_pages};
   // One workgroup deals this many slots in less than another launch takes (in a graph, 4,096 tokens 5.3 us, 7.2 in two launches; 8,192
-  // 7.3 and 6.9; 512 sequences of 24 14.1 and 8.4); fewer threads meet sooner (48 single tokens 2.9 us with 256, 3.7 with 1,024; 1,000
+  // 7.3 and 6.9; 512 sequences of 24 14.1 and 8.4); fewer threads meet sooner (24 single tokens 2.9 us with 256, 3.7 with 1,024; 1,000
   // of them 7.3 and 5.4).
   const bool together = n_tokens <= 4096, few = n_tokens <= 512 && n_seqs <= 512;
   if (few) append_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a, true);
@@ -355,8 +356,8 @@ extern "C" int rf2_paged_release(const rf2_paged_plan* plan, int32_t n_seqs, con
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   const ReleaseArgs a{done, seq_len, block_table, n_free, free_pages, seq_len_out, n_free_out, status, n_seqs, page_shift(plan),
                       plan->cfg.max_pages, plan->cfg.n_pages};
-  // Two rounds of the smaller workgroup at most (in a graph, 4 sequences of 32 give back in 4.0 us with 256 threads, 5.3 with 1,024; all of
-  // 64 with 4,600 pages in 9.7 and 7.0).
+  // Two rounds of the smaller workgroup at most (in a graph, 3 sequences of 32 give back in 4.0 us with 256 threads, 5.3 with 1,024; all of
+  // 64 with 4,500 pages in 9.7 and 7.0).
   if ((int64_t)n_seqs * plan->cfg.max_pages <= 4096) release_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a);
   else release_kernel<1024><<<dim3(1), dim3(1024), 0, (hipStream_t)stream>>>(a);
   RF2_LAUNCH_CHECK();
