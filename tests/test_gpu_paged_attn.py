@@ -20,10 +20,13 @@ CASES = {
     "group_3": dict(new=[1, 1, 1], ctx=[700, 5, 1300], heads=9, kv=3, d=128, page=64),
     "group_7": dict(new=[1, 2], ctx=[450, 81], heads=7, kv=1, d=64, page=64, dtype=FP),
     "group_40": dict(new=[1, 3], ctx=[600, 10], heads=40, kv=1, d=128, page=32),
+    "group_512": dict(new=[1, 2, 0, 1], ctx=[900, 33, 5, 0], heads=512, kv=1, d=64, page=32),
+    "mha_512": dict(new=[1, 3], ctx=[1500, 31], heads=512, kv=512, d=64, page=64, dtype=FP),
     "mha_24": dict(new=[1, 1], ctx=[99, 1001], heads=24, kv=24, d=64, page=256),
     # long caches: cut into parts, whole ones beside them
     "long": dict(new=[1], ctx=[20011], heads=8, kv=2, d=128, page=64),
     "long_fp16": dict(new=[1, 1, 1], ctx=[9000, 17, 3333], heads=16, kv=8, d=128, page=128, dtype=FP),
+    "million": dict(new=[1], ctx=[1000000], heads=2, kv=1, d=64, page=256),
     "long_d64": dict(new=[1, 1], ctx=[12345, 600], heads=4, kv=4, d=64, page=32),
     # chunks
     "chunk_small": dict(new=[5], ctx=[0], heads=2, kv=1, d=64, page=32),
@@ -286,6 +289,24 @@ def test_offsets_past_32_bits():
     b.k_cache, b.v_cache = k_cache, v_cache
     b.table = torch.where(b.table >= 0, b.table + shift, b.table)
     o, lse = b.run(b.plan(n_pages=n_pages))
+    b.check(o, lse)
+
+
+def test_more_columns_than_a_wavefront_lists_at_a_time():
+    """Parts of more than 512 pages (many rows) and of more than 256 to a wavefront (few), with holes near where a list ends."""
+    holes = [(0, p, -1) for p in (0, 255, 256, 511, 512, 513, 560)]
+    b = Batch(seed=19, new=[1024], ctx=[17000], heads=128, kv=1, d=64, page=32, holes=holes)
+    o, lse = b.run(b.plan(False))
+    b.check(o, lse, False)
+
+    n = 128
+    b = Batch(seed=20, new=[1], ctx=[35199], heads=8, kv=8, d=64, page=32, holes=[(0, p, -1) for p in (1, 255, 256, 274, 275, 276, 530, 531, 1099)])
+    b.new, b.len, b.rows = [1] * n, b.len * n, n
+    b.k, b.v, b.kept = b.k * n, b.v * n, b.kept * n                    # all sequences read the same pages
+    b.table, b.seq_len = b.table.repeat(n, 1).contiguous(), b.seq_len.repeat(n)
+    b.cu = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    b.q = torch.randn(n, 8, 64, generator=torch.Generator().manual_seed(20)).to(BF).cuda()
+    o, lse = b.run(b.plan())
     b.check(o, lse)
 
 
