@@ -96,14 +96,17 @@ __device__ __forceinline__ void deal_slots(const AppendArgs& a, const Lengths& m
   }
 }
 
-// One workgroup: sums, checks, lengths; with `slots` the slots too.  Every thread has a run of sequences.  Bound by its latency: 2.6 us for
-// 24 single tokens (a launch takes about 3).
+constexpr int SLOT_THREADS = 1024, SLOTS_OF_GROUP = 2 * SLOT_THREADS;
+
+// Sums, checks, lengths; with `slots` the slots too, by one workgroup or SLOTS_OF_GROUP by each: all do the sums, the first writes
+// what is not a slot.  Every thread has a run of sequences.  Bound by its latency: 2.6 us for 24 single tokens (a launch takes about 3).
 template <int NT>
 __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   __shared__ Lengths m;
   const int run = (a.n_seqs + NT - 1) / NT, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
   const int64_t cap = (int64_t)a.max_pages << a.page_shift;
   const int n_free = a.n_free[0];
+  const bool writes = blockIdx.x == 0;
   int bad = n_free < 0 || n_free > a.n_pages ? RF2_PAGED_BAD_LENGTH : 0;
   int64_t cu = 0, base = 0;
   for (int s = s0; s < s1; ++s) {
@@ -122,27 +125,30 @@ __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   const bool fine = status == 0;
   for (int s = s0; s < s1; ++s) {
     const int old = m.old[s], more = fine ? a.new_len[s] : 0;
-    m.cu[s] = a.cu_new[s] = fine ? (int)cu : 0;
+    m.cu[s] = fine ? (int)cu : 0;
     m.base[s] = (int)base;
-    a.seq_len_out[s] = old + more;
+    if (writes) a.cu_new[s] = m.cu[s], a.seq_len_out[s] = old + more;
     if (fine) {
       cu += more;
       base += pages_of((int64_t)old + more, a.page_shift) - pages_of(old, a.page_shift);
     }
   }
   if (threadIdx.x == 0) {
-    m.cu[a.n_seqs] = a.cu_new[a.n_seqs] = fine ? (int)all_tokens : 0;
-    a.n_free_out[0] = fine ? n_free - (int)all_pages : n_free;
-    a.status[0] = status;
+    m.cu[a.n_seqs] = fine ? (int)all_tokens : 0;
+    if (writes) {
+      a.cu_new[a.n_seqs] = m.cu[a.n_seqs];
+      a.n_free_out[0] = fine ? n_free - (int)all_pages : n_free;
+      a.status[0] = status;
+    }
   }
   if (!slots) return;
   __syncthreads();
-  deal_slots(a, m, n_free, fine, (int)threadIdx.x, a.n_tokens, NT);
+  const int first = (int)blockIdx.x * SLOTS_OF_GROUP;
+  deal_slots(a, m, n_free, fine, first + (int)threadIdx.x, gridDim.x == 1 ? a.n_tokens : min(first + SLOTS_OF_GROUP, a.n_tokens), NT);
 }
 
-constexpr int SLOT_THREADS = 1024, SLOTS_OF_GROUP = 2 * SLOT_THREADS;
-
-// Slots where there are many: every workgroup repeats the sums (from what append_kernel left, which may lie over its inputs).
+// Slots where there are many and outputs lie over inputs, so that these have to be read before: every workgroup repeats the sums, from
+// what append_kernel left.
 __global__ void __launch_bounds__(SLOT_THREADS) slots_kernel(AppendArgs a) {
   constexpr int NT = SLOT_THREADS;
   __shared__ Lengths m;
@@ -330,15 +336,16 @@ extern "C" int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int3
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   const AppendArgs a{seq_len, new_len, free_pages, n_free, block_table, seq_len_out, n_free_out, cu_new, slots, status,
                      n_seqs, n_tokens, page_shift(plan), plan->cfg.max_pages, plan->cfg.n_pages};
-  // One workgroup deals this many slots in less than another launch takes (in a graph, 4,096 tokens 5.3 us, 7.2 in two launches; 8,192
-  // 7.3 and 6.9; 512 sequences of 24 14.1 and 8.4); fewer threads meet sooner (24 single tokens 2.9 us with 256, 3.7 with 1,024; 1,000
-  // of them 7.3 and 5.4).
-  const bool together = n_tokens <= 4096, few = n_tokens <= 512 && n_seqs <= 512;
+  // Fewer threads meet sooner (in a graph, 24 single tokens 3.0 us with 256, 3.7 with 1,024; 1,000 of them 7.3 and 5.4).  More slots than a
+  // workgroup's go to several, each of which repeats the sums (81,936 tokens of 256 sequences 5.6 us, 8.4 in two launches), unless outputs
+  // lie over inputs: then one deals up to 4,096 (5.3 us, 7.2 in two launches; 8,192 7.3 and 6.9), and more are left to a second launch.
+  const bool few = n_tokens <= 512 && n_seqs <= 512, over = seq_len_out == seq_len || n_free_out == n_free, two = over && n_tokens > 4096;
+  const unsigned groups = std::max(1, (n_tokens + SLOTS_OF_GROUP - 1) / SLOTS_OF_GROUP);
   if (few) append_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a, true);
-  else append_kernel<1024><<<dim3(1), dim3(1024), 0, (hipStream_t)stream>>>(a, together);
+  else append_kernel<SLOT_THREADS><<<dim3(over ? 1 : groups), dim3(SLOT_THREADS), 0, (hipStream_t)stream>>>(a, !two);
   RF2_LAUNCH_CHECK();
-  if (!together) {
-    slots_kernel<<<dim3((n_tokens + SLOTS_OF_GROUP - 1) / SLOTS_OF_GROUP), dim3(SLOT_THREADS), 0, (hipStream_t)stream>>>(a);
+  if (two) {
+    slots_kernel<<<dim3(groups), dim3(SLOT_THREADS), 0, (hipStream_t)stream>>>(a);
     RF2_LAUNCH_CHECK();
   }
   return RF2_OK;
