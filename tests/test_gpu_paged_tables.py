@@ -42,7 +42,8 @@ class State:
         plan = self.plan(n_tokens)
         want = ref.append(self.lens, new, self.free, n_free, self.table, n_tokens, self.page, self.n_pages)
         table, lens, top = torch.from_numpy(self.table).cuda(), ints(self.lens), ints([n_free])
-        lens_out, top_out = (lens, top) if in_place else (ints([-9] * len(self.lens)), ints([-9]))
+        lens_out = lens if in_place in (True, "lengths") else ints([-9] * len(self.lens))
+        top_out = top if in_place in (True, "count") else ints([-9])
         cu, slots, status = ints([-9] * (len(self.lens) + 1)), ints([-9] * n_tokens), ints([-9])
         free = torch.from_numpy(self.free).cuda()
         plan.rf2_paged_append(lens, ints(new), free, top, table, lens_out, top_out, cu, slots, status)
@@ -54,7 +55,7 @@ class State:
         return want
 
 
-@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("in_place", [False, True, "lengths", "count"])
 @pytest.mark.parametrize("page", [32, 64, 256])
 @pytest.mark.parametrize("lens, new, pad", [
     ([0], [1], 0), ([31], [1], 0), ([32], [1], 3), ([5, 0, 64, 63], [1, 1, 1, 1], 0), ([0, 0, 0], [0, 0, 0], 4), ([], [], 5),
@@ -71,7 +72,8 @@ def test_append(lens, new, pad, page, in_place):
 def test_append_many_sequences(n_seqs, most):
     rng = np.random.default_rng(n_seqs)
     lens, new = rng.integers(0, 100, n_seqs).tolist(), rng.integers(0, most, n_seqs).tolist()
-    State(lens, 32, 12000, 12, seed=1).append(new, sum(new) + 11)
+    for in_place in (False, True):
+        State(lens, 32, 12000, 12, seed=1).append(new, sum(new) + 11, in_place)
 
 
 @pytest.mark.parametrize("n_tokens_less, n_free, lens, new, row", [
