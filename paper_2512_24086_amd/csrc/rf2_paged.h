@@ -25,9 +25,15 @@ inline int rf2_paged_parts_per_head(int kv_heads) { return std::max(1, RF2_PAGED
 // Bytes of the partial results of a launch: sequences that are cut have fewer than twice as many parts as are aimed at, each of
 // `rows` rows of head_dim sums and two numbers more, and at most as many tiles, with 32 bytes for every 8 rows
 // (rf2_paged_attn.hip).
-inline int64_t rf2_paged_workspace(const rf2_paged_config& c) {
+inline int64_t rf2_paged_parts_bytes(const rf2_paged_config& c) {
   const int64_t aimed = (int64_t)rf2_paged_parts_per_head(c.kv_heads) * c.kv_heads;
   return 2 * aimed * RF2_PAGED_ROWS_MANY * (c.head_dim + 2) * 4 + 32 * (aimed * RF2_PAGED_JOINTS + 1);
+}
+
+// Launches of more sequences than this add up their shares first: 16 bytes each, and 16 more.
+constexpr int RF2_PAGED_SURVEY = 256;
+inline int64_t rf2_paged_workspace(const rf2_paged_config& c) {
+  return rf2_paged_parts_bytes(c) + (c.max_seqs > RF2_PAGED_SURVEY ? 16 * ((int64_t)c.max_seqs + 1) : 0);
 }
 
 inline bool rf2_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }

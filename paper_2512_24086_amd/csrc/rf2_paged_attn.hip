@@ -11,14 +11,15 @@
 // a sequence that is cut (c = ceil(units(length) / units) >= 2) has c < 2 units(length) / units parts to a tile, all of them
 // less than 2 W / units <= 2 aimed: the size of the workspace.  Few rows take the least such number; for many, and up to 64
 // sequences, it is searched for (find_part).  The lengths are in device memory, so every workgroup works this out for itself
-// and finds its own part: 2 to 4 us with up to 16 sequences, 5 with 64.  (A kernel before that did it once would cost as much and
-// a launch.)  The grid is the most there can be; workgroups without a part leave.
+// and finds its own part: 2 to 4 us with up to 16 sequences, 5 with 64.  Above 256 sequences a launch before adds up what they have in
+// common (survey_kernel).  The grid is the most there can be; workgroups without a part leave.
 //
 // Sums.  The sums of a tile that is cut go to the workspace in fp32; its first part lists its rows there (Joint), and a second
 // launch, join_kernel, adds what is listed in the order of the parts: no atomics, the same bits each time.
 //
 // Products: S^T = K Q^T, O^T = V^T P^T, operands from the cache's tiles straight into registers, 1 KiB an instruction; P is what
-// the accumulators of S^T hold, rounded: the cache's order of keys is theirs.
+// the accumulators of S^T hold: the cache's order of keys is theirs.  P is rounded to the type of V, half a step as V's own values
+// are, for products of fp32 run at a sixteenth of the rate; O once, when it is whole.
 //
 // Softmax: a probability is exp2(q.k c - m), c = scale log2(e), with a reference m per row that is moved only when the sum
 // of a unit's probabilities leaves the range that P's type carries: no maximum per unit, and O is hardly ever rescaled.  Sums are
@@ -88,6 +89,7 @@ struct Args {
   const void *q, *k_cache, *v_cache;
   const int32_t *table, *seq_len, *cu_new;
   float* parts;
+  int4* survey;                           // see survey_kernel; nullptr: there is none
   void* o;
   float* lse;
   int64_t q_stride;
@@ -187,15 +189,60 @@ __device__ __forceinline__ int part_at(int r, int ch) {
 template <int ROWS>
 constexpr int JOINT = ROWS < RF2_PAGED_ROWS_MANY ? 2 : 8;
 
+// A sequence's share of the parts, and what the ones before it have (of one K/V head).
+struct Share {
+  unsigned items, places, joints, chunks;
+};
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const Args& a, const Seq& s) { return (int)((unsigned)(s.n_new * a.group + ROWS - 1) / (unsigned)ROWS); }
+template <int ROWS>
+__device__ __forceinline__ unsigned joints_of(const Args& a, const Seq& s) { return (unsigned)(s.n_new * a.group + JOINT<ROWS> - 1) / JOINT<ROWS>; }
+
+// Units of a part, of so many units of all tiles.  (Rounded up by more than the sums are off; no sequence has more than 2^19 units.)
+__device__ __forceinline__ int parts_of(const Args& a, float work) { return max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least); }
+
+// Part number `mine` of the launch's (on this XCD, where K/V heads are dealt to them), which is one of sequence `seq`.
+template <int ROWS>
+__device__ __forceinline__ bool settle(const Args& a, unsigned block, unsigned mine, unsigned heads, int seq, const Seq& s, const Share& before, Part& w) {
+  w.seq = seq;
+  w.s = s;
+  w.tiles = tiles_of<ROWS>(a, s);
+  const unsigned n = before.chunks, each = w.tiles * n;
+  w.units = (int)((unsigned)(units_of(s.len) + n - 1) / n);          // (all parts alike, but for the last)
+  const unsigned rest = mine - before.items * heads, hh = rest / each, x = rest % each;
+  w.head = (int)(heads < (unsigned)a.kv_heads ? hh * 8 + (block & 7) : hh);
+  w.chunk = (int)(x / (unsigned)w.tiles);
+  w.tile = w.tiles - 1 - (int)(x % (unsigned)w.tiles);               // (under a causal mask the last tile is the longest: it goes first)
+  w.place = n > 1 ? (int)((before.places * a.kv_heads + w.head * each) + x) : -1;
+  w.joint = (int)(before.joints * a.kv_heads + w.head * (n > 1 ? joints_of<ROWS>(a, s) : 0)) + w.tile * (ROWS / JOINT<ROWS>);
+  return w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / JOINT<ROWS> <= a.most_joints;
+}
+
 // Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.
 template <int ROWS>
 __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w) {
   const int lane = (int)threadIdx.x & 63;
+  // Workgroups with equal number % 8 share an XCD and its L2.  Where the K/V heads can be dealt to the XCDs evenly, they are.
+  const bool dealt = a.kv_heads % 8 == 0;
+  const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
+  if (a.survey) {
+    // The last sequence with no more than `at` items before it, of 64 at equal distances and then of those from there on.
+    const int n = a.survey[0].y, step = (n + 63) >> 6;
+    const auto last = [&](int i, int end) __attribute__((always_inline)) {
+      return __popcll(__builtin_amdgcn_ballot_w64(i < end && (unsigned)a.survey[1 + min(i, a.n_seqs - 1)].x <= at)) - 1;
+    };
+    if (n == 0) return false;
+    const int from = uniform(last(lane * step, n)) * step, seq = from + uniform(last(from + lane, min(from + step, n)));
+    const int4 r = a.survey[1 + seq];
+    const Seq s = seq_of(a, seq);
+    if (at >= (unsigned)r.x + tiles_of<ROWS>(a, s) * (unsigned)r.w) return false;
+    return settle<ROWS>(a, block, mine, heads, seq, s, {(unsigned)r.x, (unsigned)r.y, (unsigned)r.z, (unsigned)r.w}, w);
+  }
   Seq s{0, 0, 0};
   int tiles = 0;
   const auto look = [&](int at) __attribute__((always_inline)) {
     s = at < a.n_seqs ? seq_of(a, at) : Seq{0, 0, 0};
-    tiles = (int)((unsigned)(s.n_new * a.group + ROWS - 1) / (unsigned)ROWS);
+    tiles = tiles_of<ROWS>(a, s);
   };
   float work = 0.f, tokens = 0.f;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
@@ -208,8 +255,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   // Rows that overlap, which no table of this library has, can be more than the grid and the workspace are made for: nothing is done.
   // (Sums up to 2^24 are exact, n_tokens is at most 2^20.)
   const int n_seqs = uniform(tokens <= (float)a.n_tokens) ? a.n_seqs : 0;
-  // (rounded up by more than the sums are off; no sequence has more than 2^19 units)
-  int units = max((int)fminf(work * 1.0001f / (float)a.aimed, 1048576.f) + 1, a.least);
+  int units = parts_of(a, work);
   if (ROWS == RF2_PAGED_ROWS_MANY && a.n_seqs <= 64) {
     // How many parts there are and how they fill the chip's places (for at_once workgroups) counts.  Lane i holds what a launch takes
     // with i + 1 64ths of the parts that are aimed at: rounds of parts of mean length, and what the longest has more, in units; START
@@ -237,32 +283,20 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     const uint64_t those = __builtin_amdgcn_ballot_w64(cost <= best);
     units = __builtin_amdgcn_readlane(mine, those == 0 ? 63 : __builtin_ctzll(those));
   }
-  // Workgroups with equal number % 8 share an XCD and its L2.  Where the K/V heads can be dealt to the XCDs evenly, they are.
-  const bool dealt = a.kv_heads % 8 == 0;
-  const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
   unsigned before = 0, places = 0, joined = 0;       // of the sequences before, one head's
   bool found = false;
   for (int s0 = 0; s0 < n_seqs; s0 += 64) {
     if (a.n_seqs > 64) look(s0 + lane);
     const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units;
-    const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, joint = chunks > 1 ? (unsigned)(s.n_new * a.group + JOINT<ROWS> - 1) / JOINT<ROWS> : 0;
+    const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, joint = chunks > 1 ? joints_of<ROWS>(a, s) : 0;
     const unsigned sum = before + wave_sums(items), cut_sum = places + wave_sums(cut), joint_sum = joined + wave_sums(joint);
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum <= at);
     if (!found && past != ~0ull) {                   // (a lane's sum only grows: the first lane that is beyond)
       const int l = __builtin_ctzll(~past);
       const auto pick = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, l); };
-      w.seq = s0 + l;
-      w.s = {pick(s.first), pick(s.n_new), pick(s.len)};
-      w.tiles = pick(tiles);
-      const unsigned n = (unsigned)pick((int)chunks), each = w.tiles * n;
-      w.units = (int)((unsigned)(units_of(w.s.len) + n - 1) / n);          // (all parts alike, but for the last)
-      const unsigned rest = mine - (unsigned)pick((int)(sum - items)) * heads, hh = rest / each, x = rest % each;
-      w.head = (int)(dealt ? hh * 8 + (block & 7) : hh);
-      w.chunk = (int)(x / (unsigned)w.tiles);
-      w.tile = w.tiles - 1 - (int)(x % (unsigned)w.tiles);                 // (under a causal mask the last tile is the longest: it goes first)
-      w.place = n > 1 ? (int)(((unsigned)pick((int)(cut_sum - cut)) * a.kv_heads + w.head * each) + x) : -1;
-      w.joint = (int)((unsigned)pick((int)(joint_sum - joint)) * a.kv_heads + w.head * (unsigned)pick((int)joint)) + w.tile * (ROWS / JOINT<ROWS>);
-      found = w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / JOINT<ROWS> <= a.most_joints;
+      found = settle<ROWS>(a, block, mine, heads, s0 + l, {pick(s.first), pick(s.n_new), pick(s.len)},
+                           {(unsigned)pick((int)(sum - items)), (unsigned)pick((int)(cut_sum - cut)), (unsigned)pick((int)(joint_sum - joint)),
+                            (unsigned)pick((int)chunks)}, w);
       if (block != 0) return found;
     }
     before = (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
@@ -271,6 +305,57 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   }
   if (block == 0 && threadIdx.x == 0) *joints_count(a) = (int)min(joined * (unsigned)a.kv_heads, (unsigned)a.most_joints);
   return found;
+}
+
+// Where a launch has many sequences, what every workgroup would add up is added up once: entry 1 + s is sequence s's Share, entry 0 the
+// units of a part and how many sequences there are (none, where rows overlap).  Every thread has a run of sequences.
+template <int ROWS>
+__global__ void __launch_bounds__(1024) survey_kernel(Args a) {
+  __shared__ float sums[2][16];
+  __shared__ uint32_t ends[3][16];
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int run = (a.n_seqs + 1023) >> 10, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
+  float work = 0.f, tokens = 0.f;
+  for (int i = s0; i < s1; ++i) {
+    const Seq s = seq_of(a, i);
+    work += (float)tiles_of<ROWS>(a, s) * (float)units_of(s.len);
+    tokens += (float)s.n_new;
+  }
+  work = wave_total(work);
+  tokens = wave_total(tokens);
+  if (lane == 0) sums[0][wave] = work, sums[1][wave] = tokens;
+  __syncthreads();
+  work = tokens = 0.f;
+  for (int i = 0; i < 16; ++i) work += sums[0][i], tokens += sums[1][i];
+  const bool fine = tokens <= (float)a.n_tokens;
+  const int units = parts_of(a, work);
+  Share mine{0, 0, 0, 0};
+  const auto add = [&](const Seq& s) {
+    const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units, items = tiles_of<ROWS>(a, s) * chunks;
+    mine.items += items;
+    if (chunks > 1) mine.places += items, mine.joints += joints_of<ROWS>(a, s);
+    return chunks;
+  };
+  for (int i = s0; i < s1; ++i) add(seq_of(a, i));
+  const uint32_t all[3] = {wave_sums(mine.items), wave_sums(mine.places), wave_sums(mine.joints)};
+  if (lane == 63)
+    for (int k = 0; k < 3; ++k) ends[k][wave] = all[k];
+  __syncthreads();
+  mine = {all[0] - mine.items, all[1] - mine.places, all[2] - mine.joints, 0};
+  uint32_t joined = 0;
+  for (int i = 0; i < 16; ++i) {
+    if (i < wave) mine.items += ends[0][i], mine.places += ends[1][i], mine.joints += ends[2][i];
+    joined += ends[2][i];
+  }
+  for (int i = s0; i < s1; ++i) {
+    const Share before = mine;
+    const unsigned chunks = add(seq_of(a, i));
+    a.survey[1 + i] = make_int4((int)before.items, (int)before.places, (int)before.joints, (int)chunks);
+  }
+  if (threadIdx.x == 0) {
+    a.survey[0] = make_int4(units, fine ? a.n_seqs : 0, 0, 0);
+    *joints_count(a) = fine ? (int)min(joined * (unsigned)a.kv_heads, (unsigned)a.most_joints) : 0;
+  }
 }
 
 // Keys that row r of a sequence sees.
@@ -1218,6 +1303,13 @@ int launch(const rf2_paged_plan* plan, Args a, Kernel kernel, int threads, int l
   const bool can_be_cut = (int64_t)c.max_pages * c.page > 32 * a.least;
   // (2^20 tokens of 512 heads and 4,096 sequences are less than 2^30 threads)
   const int64_t grid = (tiles + (can_be_cut ? a.aimed : 0)) * c.kv_heads;
+  // With a launch for the sums 4,096 sequences of 200 keys take 694 us, 2,040 without; 1,024 of 500 343 and 404; 512 of 700 233 and 245; 256 of
+  // 1,000 170 and 171; 128 of them 88.4 and 87.4.
+  a.survey = a.n_seqs > RF2_PAGED_SURVEY ? (int4*)((char*)a.parts + rf2_paged_parts_bytes(c)) : nullptr;
+  if (a.survey) {
+    survey_kernel<ROWS><<<dim3(1), dim3(1024), 0, st>>>(a);
+    RF2_LAUNCH_CHECK();
+  }
   kernel<<<dim3((unsigned)grid), dim3(threads), 0, st>>>(a);
   RF2_LAUNCH_CHECK();
   if (can_be_cut) {

@@ -44,6 +44,10 @@ CASES = {
     # more sequences than a wavefront has lanes
     "many_seqs": dict(new=[1] * 150, ctx=[(37 * i) % 301 for i in range(150)], heads=4, kv=2, d=64, page=32),
     "many_mixed": dict(new=[(i % 7 == 3) * 40 + i % 3 for i in range(100)], ctx=[(91 * i) % 500 for i in range(100)], heads=4, kv=1, d=128, page=64),
+    "more_seqs": dict(new=[i % 3 for i in range(700)], ctx=[(91 * i) % 700 for i in range(700)], heads=4, kv=2, d=64, page=32),
+    "more_seqs_long": dict(new=[1] * 300, ctx=[(977 * i) % 60 + 9000 * (i % 150 == 7) for i in range(300)], heads=8, kv=8, d=128, page=64, dtype=FP),
+    "more_mixed": dict(new=[(i % 7 == 3) * 140 + i % 3 for i in range(300)], ctx=[(91 * i) % 900 for i in range(300)], heads=8, kv=2, d=128, page=64, pad=5),
+    "more_chunks": dict(new=[20 + i % 9 for i in range(270)], ctx=[(i * 131) % 300 for i in range(270)], heads=3, kv=3, d=64, page=64),
     # single tokens of long sequences beside chunks
     "mixed": dict(new=[1, 300, 1, 1, 2, 90, 1, 0, 1, 5, 1, 1], ctx=[3000, 700, 20, 9000, 5, 0, 1, 60, 4100, 333, 2500, 31], heads=8, kv=2, d=128, page=64, pad=3),
     "mixed_d64": dict(new=[1, 1, 260, 1, 1, 1, 130, 1, 1], ctx=[5000, 2100, 900, 64, 63, 0, 2000, 3000, 1500], heads=4, kv=4, d=64, page=32, dtype=FP),
@@ -184,7 +188,7 @@ def test_lengths_out_of_range_are_clamped():
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("n", [3, 70])
+@pytest.mark.parametrize("n", [3, 70, 300])
 def test_rows_that_overlap_are_refused_by_the_kernel(n):
     """cu_new goes up and down, so that the sequences' rows are together more than there are."""
     b = Batch(seed=16, new=[30] + [0] * n, ctx=[2000] + [1000] * n, heads=8, kv=4, d=64, page=32)
@@ -269,7 +273,7 @@ def test_tokens_behind_that_are_not_finite_stay_unseen(shape, dtype):
             at += n
 
 
-@pytest.mark.parametrize("n", [1, 63, 64, 65, 200, 1024])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 200, 256, 257, 1024, 1025, 4096])
 def test_numbers_of_sequences(n):
     b = Batch(seed=12, new=[1] * n, ctx=[(i * 53) % 90 for i in range(n)], heads=2, kv=1, d=64, page=32)
     o, lse = b.run(b.plan())

@@ -39,12 +39,14 @@ def test_a_type_that_is_none_of_the_two():
     assert rf2.lib().rf2_paged_plan_create(C.byref(cfg), C.byref(h)) == rf2.RF2_ERR_INVALID_ARG and not h
 
 
-@pytest.mark.parametrize("over", [dict(), dict(head_dim=128, page=32), dict(heads=40, kv_heads=40), dict(heads=512, kv_heads=512), dict(heads=3, kv_heads=1)], ids=str)
+@pytest.mark.parametrize("over", [dict(), dict(head_dim=128, page=32), dict(heads=40, kv_heads=40), dict(heads=512, kv_heads=512), dict(heads=3, kv_heads=1), dict(max_seqs=256),
+                                  dict(max_seqs=257), dict(max_seqs=4096)], ids=str)
 def test_sizes(over):
     p = make(**over)
     c = p.cfg
     assert p.info.cache_elements == c.n_pages * c.kv_heads * c.page * c.head_dim
-    assert 0 < p.info.workspace_bytes <= 1024 * (2 * 128 * (c.head_dim + 2) * 4 + 16 * 32) + 32
+    survey = 16 * (c.max_seqs + 1) if c.max_seqs > 256 else 0
+    assert survey < p.info.workspace_bytes <= 1024 * (2 * 128 * (c.head_dim + 2) * 4 + 16 * 32) + 32 + survey
     buf = p.alloc("cpu")
     assert buf["k_cache"].numel() == buf["v_cache"].numel() == p.info.cache_elements
     assert buf["free_pages"].tolist() == list(range(c.n_pages - 1, -1, -1)) and buf["n_free"].item() == c.n_pages

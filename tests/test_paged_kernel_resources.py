@@ -14,7 +14,7 @@ def resources(source, tmp_path):
     return re.findall(r"Function Name: (\S+).*?ScratchSize \[bytes/lane\]: (\d+).*?Occupancy \[waves/SIMD\]: (\d+).*?VGPRs Spill: (\d+)", out.stderr, re.S)
 
 
-@pytest.mark.parametrize("source, instances", [("rf2_paged_attn.hip", 24), ("rf2_paged_store.hip", 2), ("rf2_paged_tables.hip", 5)])
+@pytest.mark.parametrize("source, instances", [("rf2_paged_attn.hip", 27), ("rf2_paged_store.hip", 2), ("rf2_paged_tables.hip", 5)])
 def test_no_instance_uses_scratch_memory(source, instances, tmp_path):
     found = resources(source, tmp_path)
     assert len(found) == instances
