@@ -225,10 +225,10 @@ __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
   // sequences from there on begin stands in its lanes, so that a step from one to the next is a step of the scalar unit.
   int place = 0;
   auto look = [&](int at, int (&entry)[DEEP]) __attribute__((always_inline)) {
-    int begins = 0, row = 0, held = 0;               // of sequence place + lane; of how many this is known
+    int begins = 0, cells = 0, held = 0;             // of sequence place + lane, what an entry is from its cell; of how many this is known
     auto hold = [&]() __attribute__((always_inline)) {
       begins = first[min(place + lane, n_rows)];
-      row = which[min(place + lane, max(n_rows - 1, 0))];
+      cells = which[min(place + lane, max(n_rows - 1, 0))] * a.max_pages - begins;      // (a table has at most 2^30 cells)
       held = min(64, n_rows - place);
     };
     if (at < all) {
@@ -246,11 +246,11 @@ __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
       const int from = at + 64 * j, i = from + lane;
       entry[j] = -1;
       if (from >= all) continue;
-      int64_t cell = 0;                              // of entry i in the table
+      int cell = 0;                                  // of entry i in the table
       bool more;
       do {                                           // sequences that begin before the end of the 64 entries
-        const int begin = __builtin_amdgcn_readlane(begins, k), seq = __builtin_amdgcn_readlane(row, k);
-        if (i >= begin) cell = (int64_t)seq * a.max_pages + (i - begin);
+        const int begin = __builtin_amdgcn_readlane(begins, k), to = __builtin_amdgcn_readlane(cells, k);
+        cell = i >= begin ? i + to : cell;
         int next = k + 1;
         if (next == held && place + held < n_rows) {
           place += k;                                // (the last one stays: entries of it may follow)
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
       for (int j = 0; j < DEEP; ++j) {
         const bool page = (unsigned)entry[j] < (unsigned)a.n_pages;
         const uint64_t pages = __builtin_amdgcn_ballot_w64(page);
-        if (page) a.free_pages[to + __popcll(pages & ((1ull << lane) - 1))] = entry[j];
+        if (page) a.free_pages[__builtin_amdgcn_mbcnt_hi((uint32_t)(pages >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)pages, (uint32_t)to))] = entry[j];
         to += __popcll(pages);
         entry[j] = next[j];
       }
