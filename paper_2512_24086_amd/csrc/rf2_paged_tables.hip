@@ -99,7 +99,7 @@ __device__ __forceinline__ void deal_slots(const AppendArgs& a, const Lengths& m
 constexpr int SLOT_THREADS = 1024, SLOTS_OF_GROUP = 2 * SLOT_THREADS;
 
 // Sums, checks, lengths; with `slots` the slots too, by one workgroup or SLOTS_OF_GROUP by each: all do the sums, the first writes
-// what is not a slot.  Every thread has a run of sequences.  Bound by its latency: 2.6 us for 24 single tokens (a launch takes about 3).
+// what is not a slot.  Every thread has a run of sequences.  Bound by its latency: 2.8 us for 24 single tokens (a launch takes about 3).
 template <int NT>
 __global__ void __launch_bounds__(NT) append_kernel(AppendArgs a, bool slots) {
   __shared__ Lengths m;
@@ -187,7 +187,7 @@ struct ReleaseArgs {
 
 // One workgroup.  The columns of all sequences that give back stand in one row of `all` entries, of which a round takes
 // NT * DEEP, a wavefront 64 * DEEP side by side; what is a page among them goes to the next places of the stack.  Bound by what one
-// compute unit issues to find each entry's place: 29,000 entries of 264 sequences, a fifth of them holes, 19.7 us.
+// compute unit issues to find each entry's place: 29,000 entries of 264 sequences, a fifth of them holes, 18.3 us.
 template <int NT>
 __global__ void __launch_bounds__(NT) release_kernel(ReleaseArgs a) {
   constexpr int DEEP = 8, WAVES = NT / 64, OF_WAVE = 64 * DEEP;
@@ -363,8 +363,8 @@ extern "C" int rf2_paged_release(const rf2_paged_plan* plan, int32_t n_seqs, con
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   const ReleaseArgs a{done, seq_len, block_table, n_free, free_pages, seq_len_out, n_free_out, status, n_seqs, page_shift(plan),
                       plan->cfg.max_pages, plan->cfg.n_pages};
-  // Two rounds of the smaller workgroup at most (in a graph, 3 sequences of 32 give back in 4.0 us with 256 threads, 5.3 with 1,024; all of
-  // 64 with 4,500 pages in 9.7 and 7.0).
+  // Two rounds of the smaller workgroup at most (in a graph, 3 sequences of 32 give back in 4.1 us with 256 threads, 5.4 with 1,024; all of
+  // 64 with 4,300 pages in 9.1 and 6.7).
   if ((int64_t)n_seqs * plan->cfg.max_pages <= 4096) release_kernel<256><<<dim3(1), dim3(256), 0, (hipStream_t)stream>>>(a);
   else release_kernel<1024><<<dim3(1), dim3(1024), 0, (hipStream_t)stream>>>(a);
   RF2_LAUNCH_CHECK();
