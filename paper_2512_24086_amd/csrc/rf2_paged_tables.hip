@@ -4,22 +4,11 @@
 // cu_s of new_r and base_s of need_r over r < s say which rows and which entries of the stack are its own, so pages are
 // dealt without atomics and the same call always gives the same tables.
 #include "rf2_paged.h"
+#include "rf2_paged_wave.h"
 
 namespace {
 
-// Inclusive sums over the lanes of a wavefront, in the vector unit (rows of 16 lanes, then their last ones carried on).
-__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
-#define RF2_ADD(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, true)
-  RF2_ADD(0x111, 0xf);            // row_shr:1, 2, 4, 8
-  RF2_ADD(0x112, 0xf);
-  RF2_ADD(0x114, 0xf);
-  RF2_ADD(0x118, 0xf);
-  RF2_ADD(0x142, 0xa);            // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
-  RF2_ADD(0x143, 0xc);
-#undef RF2_ADD
-  return x;
-}
-// The same for values of up to 2^40 (20 bits at a time: no part overflows).
+// wave_sums for values of up to 2^40 (20 bits at a time: no part overflows).
 __device__ __forceinline__ int64_t wave_sums64(int64_t x) {
   return ((int64_t)wave_sums((uint32_t)(x >> 20)) << 20) + wave_sums((uint32_t)x & 0xfffffu);
 }
