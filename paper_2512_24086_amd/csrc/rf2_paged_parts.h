@@ -152,14 +152,15 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
     units = __builtin_amdgcn_readlane(mine, those == 0 ? 63 : __builtin_ctzll(those));
   }
   unsigned before = 0, places = 0, joined = 0;       // of the sequences before, one head's
-  bool found = false;
+  bool found = false, looked = false;                // (looked: the part's sequence is behind us; workgroup 0 goes on for the sums)
   for (int s0 = 0; s0 < n_seqs; s0 += 64) {
     if (a.n_seqs > 64) look(s0 + lane);
     const unsigned chunks = (unsigned)(units_of(s.len) + units - 1) / (unsigned)units;
     const unsigned items = tiles * chunks, cut = chunks > 1 ? items : 0, joint = chunks > 1 ? joints_of<ROWS>(a, s) : 0;
     const unsigned sum = before + wave_sums(items), cut_sum = places + wave_sums(cut), joint_sum = joined + wave_sums(joint);
     const uint64_t past = __builtin_amdgcn_ballot_w64(sum <= at);
-    if (!found && past != ~0ull) {                   // (a lane's sum only grows: the first lane that is beyond)
+    if (!looked && past != ~0ull) {                  // (a lane's sum only grows: the first lane that is beyond)
+      looked = true;
       const int l = __builtin_ctzll(~past);
       const auto pick = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, l); };
       found = settle<ROWS>(a, block, mine, heads, s0 + l, {pick(s.first), pick(s.n_new), pick(s.len)},

@@ -89,3 +89,18 @@ CASES = {
 def test_every_tile_is_taken_once(name, parts):
     case = dict(CASES[name])
     check(case["heads"], case["kv"], case["new"], case["ctx"], *parts(**case))
+
+
+@pytest.mark.parametrize("new", [[5000] + [1] * 64, [5000] + [1] * 63 + [2] * 66, [6000, 0, 3] + [0] * 100, [5000] + [1] * 255, [1100] + [0, 1] * 2047 + [0]],
+                         ids=lambda new: f"{len(new)}_sequences")
+def test_what_a_workgroup_finds_is_a_part(new, parts):
+    """A prompt of more than 1,024 tiles before other sequences: no workgroup finds a head, a tile or a part that there is not, workgroup 0
+    among them, which looks through all sequences."""
+    rows, found, listed, most_joints, places = parts(32, 1, new, [0] * len(new))
+    seq, head, tile, chunk, tiles, units, place, joint = found[found[:, 0] == 1][:, 1:].T
+    held = np.array([-(-n * 32 // rows) for n in new])
+    assert (held[seq] > 0).all() and (tiles == held[seq]).all()
+    assert (head == 0).all() and (tile >= 0).all() and (tile < tiles).all() and (chunk >= 0).all()
+    keys = np.maximum(-(-np.array(new) // 32), 1)
+    assert (chunk * units < keys[seq]).all()
+    assert (place < places).all() and ((place < 0) | (joint + rows // (2 if rows < 128 else 8) <= most_joints)).all()
