@@ -81,9 +81,14 @@ __device__ __forceinline__ bool settle(const Args& a, unsigned block, unsigned m
   w.head = (int)(heads < (unsigned)a.kv_heads ? hh * 8 + (block & 7) : hh);
   w.chunk = (int)(x / (unsigned)w.tiles);
   w.tile = w.tiles - 1 - (int)(x % (unsigned)w.tiles);               // (under a causal mask the last tile is the longest: it goes first)
-  w.place = n > 1 ? (int)((before.places * a.kv_heads + w.head * each) + x) : -1;
-  w.joint = (int)(before.joints * a.kv_heads + w.head * (n > 1 ? joints_of<ROWS>(a, s) : 0)) + w.tile * (ROWS / JOINT<ROWS>);
-  return w.head < a.kv_heads && w.place < a.places && w.joint + ROWS / JOINT<ROWS> <= a.most_joints;
+  w.place = w.joint = -1;
+  // Only what is cut has places in the workspace, less of them than there are; tiles that are whole can be any number.
+  if (n > 1) {
+    w.place = (int)((before.places * a.kv_heads + w.head * each) + x);
+    w.joint = (int)(before.joints * a.kv_heads + w.head * joints_of<ROWS>(a, s)) + w.tile * (ROWS / JOINT<ROWS>);
+    if (w.place >= a.places || w.joint + ROWS / JOINT<ROWS> > a.most_joints) return false;
+  }
+  return w.head < a.kv_heads;
 }
 
 // Finds part number `block` of the launch.  ROWS: of a tile.  Every wavefront does it for itself, 64 sequences at a time.

@@ -81,6 +81,14 @@ CASES = {
     "frames": dict(heads=5, kv=5, new=[4680], ctx=[28080], d=128),
     "hundred": dict(heads=4, kv=1, new=[(i % 7 == 3) * 40 + i % 3 for i in range(100)], ctx=[(91 * i) % 500 for i in range(100)], d=128),
     "three_hundred": dict(heads=8, kv=8, new=[1] * 300, ctx=[(977 * i) % 60 + 9000 * (i % 150 == 7) for i in range(300)]),
+    # more than 1,024 tiles that are not cut: of one sequence, behind one that is cut, of few rows
+    "long_prompt": dict(heads=32, kv=8, new=[40000], ctx=[0]),
+    "long_prompt_by_a_tile": dict(heads=32, kv=1, new=[4097], ctx=[0]),
+    "long_prompt_40_heads": dict(heads=40, kv=40, new=[129000], ctx=[0], d=128),
+    "cut_before_long": dict(heads=32, kv=8, new=[3200, 7360], ctx=[100000, 0], d=128),
+    "long_before_many": dict(heads=32, kv=1, new=[5000] + [1] * 64, ctx=[0] * 65),
+    "long_few_rows": dict(heads=16, kv=1, new=[2200] + [0, 1] * 900 + [0] * 2295, ctx=[0] * 4096),
+    "long_32_rows": dict(heads=32, kv=1, new=[1100] + [0, 1] * 1400 + [0] * 1295, ctx=[0] * 4096),
     "thousand_chunks": dict(heads=3, kv=3, new=[20 + i % 9 for i in range(1000)], ctx=[(i * 131) % 300 for i in range(1000)]),
 }
 
@@ -104,3 +112,16 @@ def test_what_a_workgroup_finds_is_a_part(new, parts):
     keys = np.maximum(-(-np.array(new) // 32), 1)
     assert (chunk * units < keys[seq]).all()
     assert (place < places).all() and ((place < 0) | (joint + rows // (2 if rows < 128 else 8) <= most_joints)).all()
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_batches_at_random(seed, parts):
+    rng = np.random.default_rng(seed)
+    for _ in range(4):
+        kv, group, n = int(rng.choice([1, 2, 3, 5, 8, 16, 40])), int(rng.choice([1, 2, 4, 7, 12])), int(rng.choice([1, 2, 8, 40, 64, 65, 130, 257, 400]))
+        longest, most = int(np.exp(rng.uniform(2, 11))), int(rng.choice([1, 4, 30, 200])) if n > 8 else int(rng.choice([1, 30, 2000]))
+        new = np.where(rng.random(n) < 0.3, 0, rng.integers(1, most + 1, n))
+        new[rng.integers(n)] = 1 if rng.random() < 0.6 else 20000 // (group * kv)
+        case = dict(heads=kv * group, kv=kv, new=new.tolist(), ctx=rng.integers(0, longest, n).tolist(), pad=int(rng.choice([0, 0, 77])),
+                    d=int(rng.choice([64, 128])), page=int(rng.choice([32, 256])))
+        check(case["heads"], case["kv"], case["new"], case["ctx"], *parts(**case))
