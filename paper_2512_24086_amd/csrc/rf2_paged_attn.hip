@@ -208,7 +208,7 @@ __device__ __forceinline__ x8 clear_behind(x8 v, int left) {
   return __builtin_bit_cast(x8, x);
 }
 
-// Values of V that are not finite, in units that some rows of a tile see more of than others: 0 times such a value is no 0, so they
+// Values of V that are not finite, in units of which some row of a tile does not see all tokens: 0 times such a value is no 0, so they
 // are taken out of V, and rows that see them get them by products of their own: the largest bf16 number where a value is +infinity
 // or not a number, times the same where a row sees the key, is +infinity in fp32 and 0 elsewhere; the negative one likewise.
 // (Two halves of a register at a time: an exponent of all ones carries into the sign's place.)
@@ -359,8 +359,9 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
   x8 kr[2][NQ], vr[2][NP];
   float last[2] = {};                      // sums of the latest unit, still to be added to l
   constexpr int NONE = 1 << 25;            // a unit that no sequence has
-  // V of unit u, of which rows do not all see the same, without values that are not finite (see take_out).
-  const bool rows_differ = uniform(limit_of(a, w.s, sp.row0) != limit_of(a, w.s, min(sp.row0 + 64, sp.n_rows) - 1));
+  // V of unit u, of which some row does not see all, without values that are not finite (see take_out).  The first row sees least; where all
+  // rows are of one token (many heads share a K/V head), others can stand behind it.
+  const bool unseen = uniform(limit_of(a, w.s, sp.row0) < w.s.len);
   auto guard = [&](x8 (&v)[NP], int u) __attribute__((always_inline)) {
     uint32_t any = 0;
 #pragma unroll
@@ -462,7 +463,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
           last[q] = probabilities(q, Scur[q], Pcur[q]);
         }
       if (u_next >= sp.free_units) mask(Snext[0], 0, u_next), mask(Snext[1], 1, u_next);
-      if (rows_differ && u >= sp.free_units && u != NONE) guard(vr[1 - B], u);
+      if (unseen && u >= sp.free_units && u != NONE) guard(vr[1 - B], u);
     }
   };
   // Units x0 to x1 - 1 of the list (behind unit `lead` of page `lead_page`, where there is one).
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
           for (int i = 0; i < 16; ++i) o[q][dt][i] *= alpha;
         last[q] = probabilities(q, S[q], P[q]);
       };
-      if (rows_differ && us[0] >= sp.free_units) guard(vr[0], us[0]);
+      if (unseen && us[0] >= sp.free_units) guard(vr[0], us[0]);
       redo(0);
       // Half of a step for tile Q: S of the next unit and O += V P of the present one, in turn, around the softmax arithmetic of the
       // other tile X (the present unit of tile 1 in the first half, the next one of tile 0 in the second).  In the second half the
@@ -630,7 +631,7 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rs <= __builtin_bit_cast(float, bound))) != 0ull, 0)) {
           if (__builtin_amdgcn_ballot_w64(!(rs <= T::RANGE)) != 0ull) redo(X);
           if (u_next >= sp.free_units) mask(S[Q], Q, u_next);
-          if (Q == 1 && rows_differ && u_next >= sp.free_units && u_next != NONE) guard(vr[1 - ODD], u_next);
+          if (Q == 1 && unseen && u_next >= sp.free_units && u_next != NONE) guard(vr[1 - ODD], u_next);
         }
       };
       constexpr std::integral_constant<int, 0> zero{};
@@ -739,7 +740,7 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
 #pragma unroll
     for (int cs = 0; cs < CS; ++cs) qf[q][cs] = *reinterpret_cast<const x8*>(from + 32 * cs);
   }
-  const bool rows_differ = uniform(limit_of(a, w.s, sp.row0) != limit_of(a, w.s, min(sp.row0 + ROWS, sp.n_rows) - 1));
+  const bool unseen = uniform(limit_of(a, w.s, sp.row0) < w.s.len);   // some row does not see all tokens (the first sees least)
   f32x4 o[QT][CT];
   float m[QT], l[QT];
 #pragma unroll
@@ -853,11 +854,11 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) vr[B][ct] = clear_behind(vr[B][ct], w.s.len - 32 * u - key0);
       uint32_t any = 0;
-      if (rows_differ && u >= sp.free_units)
+      if (unseen && u >= sp.free_units)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) any |= any_not_finite<T>(vr[B][ct]);
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0ull, 0)) {
-        // values of V that are not finite, where rows differ in what they see (see take_out); one operand after the other
+        // values of V that are not finite, where a row does not see all (see take_out); one operand after the other
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           __builtin_amdgcn_sched_barrier(0);

@@ -1,0 +1,49 @@
+"""Values of V that are not finite: where a tile's rows all belong to one token, and in the first units that a row sees."""
+import pytest
+import torch
+
+from tests.paged_ref import Batch
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.bfloat16, torch.float16]
+INF, NAN = float("inf"), float("nan")
+
+
+def set_v(b, s, pos, ch, x):
+    """Channel ch of V of token pos of sequence s, all K/V heads."""
+    page, r = int(b.table[s, pos // b.page]), pos % b.page
+    b.v_cache[page, :, r // 32, r % 32 // 16 * 2 + r % 8 // 4, ch, r % 16 // 8 * 4 + r % 4] = x
+
+
+def bits(x):
+    return x.contiguous().view(torch.int16)
+
+
+# rows of a token that fill whole tiles of 16, of 32 and of a wavefront's 64: the rows of a tile then all see the same keys, and the tokens
+# behind stand in the same unit of 32 keys
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads, new, ctx", [(16, [2, 0], [40, 0]), (16, [4, 0, 0, 0], [0, 9, 0, 3]), (32, [2, 0], [100, 5]), (40, [3, 0, 0, 0], [70, 0, 0, 0]),
+                                             (64, [7], [40]), (64, [30, 2], [900, 0]), (128, [9], [0]), (100, [11], [33]), (512, [5], [3])], ids=str)
+def test_one_token_to_a_tile(heads, new, ctx, d, dtype):
+    b = Batch(seed=30, new=new, ctx=ctx, heads=heads, kv=1, d=d, page=64, dtype=dtype)
+    plan = b.plan()
+    n, last = new[0], ctx[0] + new[0] - 1
+    values = [(0, INF), (1, -INF), (2, NAN), (d - 1, NAN)]
+    for first in {1, n // 2, n - 1}:                       # tokens from this one on
+        spots = range(ctx[0] + first, last + 1)
+        for ch, _ in values:
+            for pos in spots:
+                set_v(b, 0, pos, ch, 0.0)
+        clean, _ = b.run(plan)
+        for ch, x in values:
+            for pos in spots:
+                set_v(b, 0, pos, ch, x)
+        o, _ = b.run(plan)
+        for ch, _ in values:
+            for pos in spots:
+                set_v(b, 0, pos, ch, 0.0)
+        assert torch.equal(bits(o[:first]), bits(clean[:first])), first
+        assert torch.equal(bits(o[first:, :, 3:d - 1]), bits(clean[first:, :, 3:d - 1])), first
+        seen = o[first:n].float()
+        assert (seen[:, :, 0] == INF).all() and (seen[:, :, 1] == -INF).all() and torch.isnan(seen[:, :, [2, d - 1]]).all(), first
