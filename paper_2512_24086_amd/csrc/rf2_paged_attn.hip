@@ -337,7 +337,9 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
     for (int i = 1; i < 16; ++i) top = fmaxf(top, S[i]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.scale_log2 - T::HEAD, -FLT_MAX);
-    const float to = fmaxf(m[q], top), alpha = __builtin_amdgcn_exp2f(m[q] - to);
+    // (a row without a key so far has no sums but, at d = 64, infinities that the guard below gave it ahead of their unit: 0 times them
+    // would not be a number)
+    const float to = fmaxf(m[q], top), alpha = m[q] == -FLT_MAX ? 1.f : __builtin_amdgcn_exp2f(m[q] - to);
     m[q] = to;
     return alpha;
   };

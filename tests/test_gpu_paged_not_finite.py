@@ -47,3 +47,31 @@ def test_one_token_to_a_tile(heads, new, ctx, d, dtype):
         assert torch.equal(bits(o[first:, :, 3:d - 1]), bits(clean[first:, :, 3:d - 1])), first
         seen = o[first:n].float()
         assert (seen[:, :, 0] == INF).all() and (seen[:, :, 1] == -INF).all() and torch.isnan(seen[:, :, [2, d - 1]]).all(), first
+
+
+# a chunk whose partial last unit stands in the same wavefront's list as the unit with the values, which comes right behind it
+@pytest.mark.parametrize("dtype", TYPES, ids=["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new, ctx, heads, kv", [([60], [5], 1, 1), ([70], [16], 1, 1), ([61], [0], 2, 1), ([45, 50], [3, 20], 4, 2), ([40], [60], 1, 1),
+                                                 ([130], [7], 3, 1)], ids=str)
+def test_an_infinite_value_reaches_every_row_that_sees_it(new, ctx, heads, kv, d, dtype):
+    b = Batch(seed=31, new=new, ctx=ctx, heads=heads, kv=kv, d=d, page=64, dtype=dtype)
+    plan = b.plan()
+    for t in (0, 5, 33):                                   # a token of the chunks
+        at = 0
+        for s, n in enumerate(new):
+            for ch in (0, 1):
+                set_v(b, s, ctx[s] + t, ch, 0.0)
+        clean, _ = b.run(plan)
+        for s, n in enumerate(new):
+            set_v(b, s, ctx[s] + t, 0, INF)
+            set_v(b, s, ctx[s] + t, 1, -INF)
+        o, _ = b.run(plan)
+        for s, n in enumerate(new):
+            got, want = o[at:at + n], clean[at:at + n]
+            assert torch.equal(bits(got[:t]), bits(want[:t])), (t, s)
+            assert torch.equal(bits(got[:, :, 2:]), bits(want[:, :, 2:])), (t, s)
+            assert (got[t:, :, 0].float() == INF).all() and (got[t:, :, 1].float() == -INF).all(), (t, s)
+            for ch in (0, 1):
+                set_v(b, s, ctx[s] + t, ch, b.v[s][ctx[s] + t, 0, ch].item())
+            at += n
