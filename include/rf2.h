@@ -282,7 +282,7 @@ typedef struct {
   int32_t dtype;           /* RF2_DTYPE_*: q, k, v, o and both caches */
   int32_t causal;          /* 1: a token sees the tokens of its sequence up to itself; 0: all that are cached, its whole
                               chunk among them (new frames of a video) */
-  float scale;             /* factor of q.k; 0 = 1/sqrt(head_dim); finite, >= 0 */
+  float scale;             /* factor of q.k; 0 = 1/sqrt(head_dim); >= 0, finite, divided by ln 2 too */
 } rf2_paged_config;
 
 typedef struct {

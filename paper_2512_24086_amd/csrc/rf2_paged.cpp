@@ -22,11 +22,14 @@ int rf2_paged_plan_create(const rf2_paged_config* cfg, rf2_paged_plan** out) {
   if ((int64_t)c.max_pages * c.page > (int64_t)1 << 24) return RF2_ERR_UNSUPPORTED;  // 16 Mi tokens, as a layer has at most
   if ((int64_t)c.max_seqs * c.max_pages > (int64_t)1 << 30) return RF2_ERR_UNSUPPORTED;    // entries of the table in int32
 
+  const double scale = c.scale > 0.0f ? (double)c.scale : 1.0 / std::sqrt((double)c.head_dim);
+  const float scale_log2 = (float)(scale * 1.4426950408889634);
+  if (!std::isfinite(scale_log2)) return RF2_ERR_INVALID_ARG;      // (infinity times a logit of 0 is not a number)
+
   rf2_paged_plan* p = new (std::nothrow) rf2_paged_plan();
   if (!p) return RF2_ERR_ALLOC;
   p->cfg = c;
-  const double scale = c.scale > 0.0f ? (double)c.scale : 1.0 / std::sqrt((double)c.head_dim);
-  p->scale_log2 = (float)(scale * 1.4426950408889634);
+  p->scale_log2 = scale_log2;
   p->info.cache_elements = (int64_t)c.n_pages * c.kv_heads * c.page * c.head_dim;
   p->info.workspace_bytes = rf2_paged_workspace(c);
   int n_dev = 0;

@@ -31,6 +31,16 @@ def test_unsupported_configurations(bad):
     assert e.value.code == rf2.RF2_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("scale, fine", [(2.0 ** 127, True), (2.3e38, True), (2.4e38, False), (3.4e38, False)])
+def test_a_scale_is_finite_in_the_exponent_of_two_as_well(scale, fine):
+    if fine:
+        make(scale=scale).close()
+        return
+    with pytest.raises(rf2.Rf2Error) as e:
+        make(scale=scale)
+    assert e.value.code == rf2.RF2_ERR_INVALID_ARG
+
+
 def test_a_type_that_is_none_of_the_two():
     with pytest.raises(ValueError):
         make(dtype=torch.float32)
