@@ -957,8 +957,8 @@ __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kern
   }
 }
 
-// Adds the parts of the tiles that are cut: 4 to 7 us, with nothing listed too, most of it the launch.  A workgroup takes a joint at a time, 32 lanes to a row; of few rows 2, 4 or 8 times 32
-// lanes share the parts of one.
+// Adds the parts of the tiles that are cut: 4 to 7 us, with nothing listed too, most of it the launch.  A workgroup takes a joint at a
+// time: 8 rows with 32 lanes each, or, of few rows, two whose parts 4 times 32 lanes share, or one with 8 times.
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Args a) {
   constexpr int E = D / 32, DEEP = 8;              // channels of a lane; parts asked for at a time
@@ -975,7 +975,7 @@ __global__ void __launch_bounds__(256) join_kernel(Args a) {
   for (int task = (int)blockIdx.x; task < count; task += (int)gridDim.x) {
     if (task != (int)blockIdx.x) j = joints(a)[task];
     if (j.parts == 0) continue;
-    const int share = MANY || j.n_rows > 4 ? 0 : j.n_rows > 2 ? 1 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
+    const int share = MANY ? 0 : j.n_rows > 1 ? 2 : 3, every = 1 << share, r = half >> share;
     const bool there = r < j.n_rows;
     fE acc = (fE)0.f;
     float top = -FLT_MAX, sum = 0.f;

@@ -100,7 +100,7 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   const unsigned heads = dealt ? a.kv_heads / 8 : a.kv_heads, mine = dealt ? block >> 3 : block, at = mine / heads;
   if (a.survey) {
     // The last sequence with no more than `at` items before it, of 64 at equal distances and then of those from there on.
-    const int n = a.survey[0].y, step = (n + 63) >> 6;
+    const int n = a.survey[0].x, step = (n + 63) >> 6;
     const auto last = [&](int i, int end) __attribute__((always_inline)) {
       return __popcll(__builtin_amdgcn_ballot_w64(i < end && (unsigned)a.survey[1 + min(i, a.n_seqs - 1)].x <= at)) - 1;
     };
@@ -181,8 +181,8 @@ __device__ __forceinline__ bool find_part(const Args& a, unsigned block, Part& w
   return found;
 }
 
-// Where a launch has many sequences, what every workgroup would add up is added up once: entry 1 + s is sequence s's Share, entry 0 the
-// units of a part and how many sequences there are (none, where rows overlap).  Every thread has a run of sequences.
+// Where a launch has many sequences, what every workgroup would add up is added up once: entry 1 + s is sequence s's Share, entry 0 how many
+// sequences there are (none, where rows overlap).  Every thread has a run of sequences.
 template <int ROWS>
 __global__ void __launch_bounds__(1024) survey_kernel(Args a) {
   __shared__ float sums[2][16];
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(1024) survey_kernel(Args a) {
     a.survey[1 + i] = make_int4((int)before.items, (int)before.places, (int)before.joints, (int)chunks);
   }
   if (threadIdx.x == 0) {
-    a.survey[0] = make_int4(units, fine ? a.n_seqs : 0, 0, 0);
+    a.survey[0] = make_int4(fine ? a.n_seqs : 0, 0, 0, 0);
     *joints_count(a) = fine ? (int)min(joined * (unsigned)a.kv_heads, (unsigned)a.most_joints) : 0;
   }
 }
