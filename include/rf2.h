@@ -324,7 +324,8 @@ int rf2_paged_append(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_token
  * Gives back the pages of the sequences s with done[s] != 0: the entries of the first ceil(seq_len[s] / page) columns of
  * their rows that are pages (others are holes) go on top of the stack, in order of s and column.  All or nothing.
  * There are no reference counts: a page that stands in several rows (attention reads it through each) is given back once for each of
- * them that is done, so a program that shares pages makes all but the last of those entries holes first.
+ * them that is done, so a program that shares pages makes all but the last of those entries holes first.  One that evicts single pages
+ * of a sequence that goes on makes their entries holes and puts the pages on the stack itself, between calls.
  *   done       : [n_seqs] uint8                                                            (in)
  *   seq_len, block_table, n_free : as above                                                (in)
  *   free_pages : [n_pages] int32, written behind its first n_free entries                  (in, out)
@@ -371,6 +372,12 @@ int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k,
  * Rows from cu_new[n_seqs] on are neither read nor written.  What a token does not see does not reach it: the cache behind a
  * sequence's last token, and tokens of the chunk behind its own, may hold anything, infinities and NaN included.  The same
  * call gives the same bits each time; in a batch of other sequences a token's result may differ by fp32 rounding.
+ * O is summed in fp32 before it is divided by the probabilities' sum, of up to 2^61: values of V up to 2^67 in size (all of fp16, 1.4e20
+ * in bf16) are summed for any lengths and logits, larger ones may come out infinite where the mean is not.
+ * The kernels are chosen from n_tokens and n_seqs, padding included, for the lengths are in device memory: up to 32 query rows (tokens
+ * times heads / kv_heads) to a sequence on average go to one that reads the cache as fast as it can, more to one for the matrix cores.
+ * So a graph for steps of single tokens is better captured with room for those alone: 64 of them, 32 heads on 8, over 0.79 GB take
+ * 131 us with room for 64 tokens, 133 for 264, 169 for 564 or 8,064.
  */
 int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens, const void* q, int64_t q_stride,
                    const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* seq_len,

@@ -1,8 +1,8 @@
-"""Values of V that are not finite: where a tile's rows all belong to one token, and in the first units that a row sees."""
+"""Values of V that are not finite, where a tile's rows all belong to one token and in the first units that a row sees; large ones."""
 import pytest
 import torch
 
-from tests.paged_ref import Batch
+from tests.paged_ref import Batch, attention, put_many
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float16]
@@ -75,3 +75,32 @@ def test_an_infinite_value_reaches_every_row_that_sees_it(new, ctx, heads, kv, d
             for ch in (0, 1):
                 set_v(b, s, ctx[s] + t, ch, b.v[s][ctx[s] + t, 0, ch].item())
             at += n
+
+
+@pytest.mark.parametrize("dtype, size", [(torch.bfloat16, 2.0 ** 64), (torch.float16, 2.0 ** 13)], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [[1, 1], [70, 3]], ids=["few", "many"])
+def test_large_values_stay_finite(new, d, dtype, size):
+    """V of up to 2^67 in bf16 (nearly all of fp16), behind logits that grow by 38 octaves, so that references lag."""
+    b = Batch(seed=32, new=new, ctx=[640, 300], heads=2, kv=1, d=d, page=32, dtype=dtype)
+    b.q.zero_()
+    b.q[:, :, 0] = 1.0
+    for s in (0, 1):
+        b.k[s] = torch.zeros(b.len[s], 1, d)
+        b.k[s][:, 0, 0] = torch.linspace(0, 38 * 0.6931 * d ** 0.5, b.len[s])
+        b.k[s] = b.k[s].to(dtype)
+        b.v[s] = (b.v[s].double().clamp(-7.9, 7.9) * size).to(dtype)
+        pos = torch.arange(b.len[s])
+        slots = b.table[s].cpu()[pos // 32].long() * 32 + pos % 32
+        k_cache, v_cache = b.k_cache.cpu(), b.v_cache.cpu()
+        put_many(k_cache, v_cache, slots, b.k[s], b.v[s], 32)
+        b.k_cache.copy_(k_cache)
+        b.v_cache.copy_(v_cache)
+    o, lse = b.run(b.plan())
+    at = 0
+    for s, n in enumerate(new):
+        want, want_lse, tol, lse_tol = attention(b.q[at:at + n], b.k[s].cuda(), b.v[s].cuda(), b.kept[s].cuda(), n, True, d ** -0.5, torch.finfo(dtype).eps / 2)
+        # (logits up to 27 in place of 8: 2^-18 of a probability more, twice)
+        assert ((o[at:at + n].double() - want).abs() <= tol + 2.0 ** -17 * b.v[s].abs().max().item()).all()
+        assert ((lse[at:at + n].double() - want_lse).abs() <= lse_tol + 2.0 ** -17).all()
+        at += n
