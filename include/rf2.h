@@ -366,7 +366,7 @@ int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k,
  *                 are more than n_tokens (they overlap) nothing is computed.               (in)
  *   workspace   : rf2_paged_info.workspace_bytes, written and read by this call alone: calls that may run at the same time
  *                 need one each                                                            (scratch)
- *   o           : [n_tokens, heads, head_dim]; a token that sees no key gets zeros         (out)
+ *   o           : [n_tokens, heads, head_dim]; a token that sees no key gets zeros; overlaps nothing else (out)
  *   lse         : optional [n_tokens, heads] fp32, natural-log sum-exp of the scaled logits, -inf where there is no key;
  *                 may be NULL                                                              (out)
  * Rows from cu_new[n_seqs] on are neither read nor written.  What a token does not see does not reach it: the cache behind a

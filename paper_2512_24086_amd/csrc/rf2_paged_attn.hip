@@ -272,9 +272,9 @@ __device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(
 // enough and two wavefronts share a SIMD.
 //
 // Bound by the matrix cores, which hold the card at about 1.7 GHz here (power): 4,680 tokens over 32,760 keys, 40 heads, full, bf16,
-// D = 128: 2,480 us, 1,270 TFLOP/s, matrix cores busy in 70% of the cycles; a library product of 8192^3 reaches 1,192.  D = 64, where
-// there is as much softmax for half the products: 1,550 us, 1,010 TFLOP/s, 53%.  Five prompts (361 to 2,397 tokens, 32 heads on 8,
-// causal): 117 us, 890 TFLOP/s; there 512 workgroups run in fewer than three rounds, of which the last leaves 12% of the places empty.
+// D = 128: 2,480 to 2,630 us by the card, 1,270 to 1,195 TFLOP/s, matrix cores busy in 70% of the cycles; a library product of 8192^3
+// reaches 1,192.  D = 64, where there is as much softmax for half the products: 1,550 to 1,630 us, 1,010 to 960 TFLOP/s, 53%.  Five prompts (361 to 2,397 tokens, 32 heads on 8,
+// causal): 117 to 122 us, 890 to 850 TFLOP/s; there 512 workgroups run in fewer than three rounds, of which the last leaves 12% of the places empty.
 template <class T, int D>
 __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a) {
   constexpr int DS = D / 16, DT = D / 32, ROWS = RF2_PAGED_ROWS_MANY;
@@ -722,7 +722,8 @@ __global__ void __launch_bounds__(128, D == 128 ? 1 : 2) many_attn_kernel(Args a
 //
 // Bound by memory: operands of two units are on their way (each is asked for as soon as the one two before has been read).
 // 64 single tokens over 0.79 GB of keys and values: 131 us, 6.0 TB/s; four over 0.58 GB, 21,000 to 61,000 keys each: 105 us, 5.6 TB/s
-// (a kernel that only reads reaches 6.5, one that copies 6.2).  One token over 200 keys takes 5.8 us, of which 0.1 are its bytes.
+// (a kernel that only reads reaches 6.5, one that copies 6.2); 64 at 64 channels over 0.39 GB: 70 us, 5.6 TB/s.  One token over 200 keys
+// takes 5.8 us, of which 0.1 are its bytes.
 template <class T, int D, int QT>
 __global__ void __launch_bounds__(256, D == 64 && QT == 1 ? 3 : 2) few_attn_kernel(Args a) {
   constexpr int KW = 4, CS = D / 32, CT = D / 16, ROWS = 16 * QT;

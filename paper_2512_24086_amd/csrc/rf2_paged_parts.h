@@ -53,7 +53,7 @@ struct Joint {
 };
 __device__ __forceinline__ int* joints_count(const Args& a) { return (int*)a.parts; }
 __device__ __forceinline__ Joint* joints(const Args& a) { return (Joint*)a.parts + 1; }
-// Rows of a joint: a workgroup of join_kernel has 32 lanes for each, and more where there are few rows and many parts.
+// Rows of a joint: a workgroup of join_kernel has 32 lanes for each, 128 or 256 where there are few rows.
 template <int ROWS>
 constexpr int JOINT = ROWS < RF2_PAGED_ROWS_MANY ? 2 : 8;
 
@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(1024) survey_kernel(Args a) {
 // Rows of a launch's tiles (host).  Up to 32 rows a sequence on average: four wavefronts share the keys of one or two tiles of 16.  More: two wavefronts of 64 rows.
 // (16 sequences of 4,000 keys, 8 K/V heads, 48 rows each: 83.7 us as two tiles of 32, 62.1 as one of 128; 128 rows: 131 and 78.6.)
 // (16 rows as a tile of 16 or one of 32: 64 single tokens 130.3 and 132.5 us, 16 chunks of 4 tokens behind 4,000 53.5 and 54.9.)
+// Rows of padding count, for the lengths are not known here: 64 single tokens among 8,064 rows take 169 us.
 inline int tile_rows(const Args& a) {
   const int64_t rows = (int64_t)a.n_tokens * a.group;
   return rows <= 16 * (int64_t)a.n_seqs ? 16 : rows <= 32 * (int64_t)a.n_seqs ? 32 : RF2_PAGED_ROWS_MANY;

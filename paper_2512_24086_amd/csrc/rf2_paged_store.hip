@@ -8,7 +8,8 @@
 //
 // 4,680 tokens of 40 heads of 128 channels: 192 MB in 37 us, 5.2 TB/s (33 to 34 us the kernel by itself; a large copy reaches 6.2).  Windows
 // of 64 tokens take longer to fill a compute unit's LDS and gain nothing; stores that are not to be kept cost the lines that two
-// windows complete (44 us).  48 single tokens of 8 heads: 6.7 us, of which 0.1 are its bytes.
+// windows complete (44 us).  48 single tokens of 8 heads: 6.7 us, of which 0.1 are its bytes: in each of 16
+// workgroups V's lone keys go out two at a time, one pair behind the other.
 #include "rf2_paged.h"
 
 namespace {
