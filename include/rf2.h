@@ -258,7 +258,8 @@ int rf2_unpermute(const rf2_plan* plan, const void* op, void* o, void* stream);
  */
 enum {
   RF2_DTYPE_BF16 = 0,
-  RF2_DTYPE_F16 = 1 /* IEEE binary16 */
+  RF2_DTYPE_F16 = 1, /* IEEE binary16 */
+  RF2_DTYPE_F32 = 2  /* weights of norms alone */
 };
 
 /* What rf2_paged_append and rf2_paged_release leave in `status` (sums of): 0, done, or nothing has been changed. */
@@ -382,6 +383,91 @@ int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, const void* k,
 int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens, const void* q, int64_t q_stride,
                    const void* k_cache, const void* v_cache, const int32_t* block_table, const int32_t* seq_len,
                    const int32_t* cu_new, void* workspace, void* o, float* lse, void* stream);
+
+/* ---- Norms and rotary positions of Q and K ------------------------------------------------------------------------
+ *
+ * What models do to Q and K before attention: a norm of each head's row of d channels, and its rotation by the position of its token,
+ * which may have several axes (time, height and width of a video, height and width of an image, one for text).  By itself, with its
+ * gradients (rf2_rope_apply, rf2_rope_backward), and within the two calls that read Q and K next anyway (rf2_permute_rope,
+ * rf2_paged_store_rope).
+ *
+ * Row x of a head of token n, weights w:
+ *     norm       y_c = x_c w_c / sqrt(sum_c x_c^2 / d + eps)       (RF2_NORM_NONE: y = x, and w is NULL)
+ *     rotation   z_u = y_u cos p - y_v sin p,  z_v = y_v cos p + y_u sin p,   p = pos[n][axis of the pair] * its frequency
+ * where pair i of the d/2 has the channels (u, v) = (2i, 2i + 1) (RF2_ROPE_PAIRS) or (i, i + d/2) (RF2_ROPE_HALVES).  The first
+ * axis_dim[0] / 2 pairs turn with axis 0, the next axis_dim[1] / 2 with axis 1, and so on; the j-th pair of axis a has the frequency
+ * theta^(-2j / axis_dim[a]), or the pairs' frequencies come from a table.  Pairs behind the last axis do not turn.
+ *
+ * All in 32 bits (angles in 64, so that far positions keep theirs), rounded to dtype once.  Rows of any finite numbers are
+ * normalised; what is not finite makes its pair not a number, or with a norm its row (an infinity: its pair, and the rest of the row 0).
+ * Positions are int32 in device memory, any value, [n_tokens][axes].  Conventions as above.
+ */
+enum { RF2_NORM_NONE = 0, RF2_NORM_RMS = 1 };
+enum { RF2_ROPE_PAIRS = 0, RF2_ROPE_HALVES = 1 };
+
+typedef struct {
+  int32_t heads, kv_heads;  /* of Q, of K; at most 65,535 */
+  int32_t head_dim;         /* d, in {64, 128} */
+  int32_t dtype;            /* RF2_DTYPE_BF16 or RF2_DTYPE_F16: rows */
+  int32_t weight_dtype;     /* weights: dtype, or RF2_DTYPE_F32 */
+  int32_t norm;             /* RF2_NORM_* */
+  float eps;                /* of the norm, 1e-30 to 1 */
+  int32_t pairing;          /* RF2_ROPE_PAIRS, RF2_ROPE_HALVES */
+  int32_t axes;             /* of a position, 0 to 4; 0: no rotation (a norm there must be then, and pos is not read) */
+  int32_t axis_dim[4];      /* channels of each axis, even, head_dim together at most */
+  double theta;             /* base of the frequencies, > 0; not read where there is a table */
+} rf2_rope_config;
+
+typedef struct {
+  int64_t workspace_bytes; /* what rf2_rope_backward needs at `workspace` (0 without a norm) */
+} rf2_rope_info;
+
+typedef struct rf2_rope_plan rf2_rope_plan; /* opaque */
+
+/* inv_freq_host: NULL, or the frequencies of the pairs that turn, in radians per position, at most 65,536 in size.  The plan belongs to the
+ * device that is current (without any: host-only, like rf2_plan_create). */
+int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host, rf2_rope_plan** out);
+int rf2_rope_plan_destroy(rf2_rope_plan* plan);
+int rf2_rope_plan_info(const rf2_rope_plan* plan, rf2_rope_info* out);
+
+/* Rows of d channels side by side, aligned to 16 bytes: row of head h of token n of element b of the batch at
+ * at + b * batch + n * token + h * head, in elements.  Strides are multiples of 8, 0 or more; rows that are written share no memory
+ * (of any two axes the one with the larger stride steps over all of the other). */
+typedef struct {
+  const void* at;
+  int64_t batch, token, head;
+} rf2_rows;
+
+typedef struct {
+  rf2_rows q, k, q_out, k_out;               /* q and k: in; q_out, k_out: out (written through `at`) */
+} rf2_rope_tensors;
+typedef struct {
+  rf2_rows q, k, dq_out, dk_out, dq, dk;     /* dq, dk: out */
+} rf2_rope_gradients;
+
+/*
+ * Rows of Q and K normalised and rotated, in one launch.
+ *   rows      : [batch, n_tokens, heads or kv_heads, d]; `at` of q and q_out, or of k and k_out, may be NULL: left out.  An output may be its
+ *               input (the same address and strides) and shares no memory with anything else    (host struct)
+ *   pos       : [n_tokens][axes] int32, pos_batch elements from one element of the batch to the next (0: all have the same) (in)
+ *   wq, wk    : [d] of weight_dtype, aligned to 16 bytes                                       (in)
+ * batch = 0 and n_tokens = 0 are allowed; batch * n_tokens above 2^24 is RF2_ERR_UNSUPPORTED.
+ */
+int rf2_rope_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rope_tensors* rows, const int32_t* pos,
+                   int64_t pos_batch, const void* wq, const void* wk, void* stream);
+
+/*
+ * Its gradients: dq and dk from the gradients dq_out and dk_out of its outputs and its inputs q and k, and those of the weights, summed over
+ * all rows of all heads.
+ *   rows      : as above; dq may be dq_out or q (the same address and strides), dk dk_out or k.  Without a norm q and k are not read and
+ *               their `at` is of no account                                                     (host struct)
+ *   dwq, dwk  : [d] fp32, written over; NULL without a norm                                    (out)
+ *   workspace : rf2_rope_info.workspace_bytes, written and read by this call alone: calls that may run at the same time need one each;
+ *               may be NULL without a norm                                                     (scratch)
+ * The same call gives the same bits each time.
+ */
+int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rope_gradients* rows, const int32_t* pos,
+                      int64_t pos_batch, const void* wq, const void* wk, float* dwq, float* dwk, void* workspace, void* stream);
 
 /*
  * Measurement aid, not part of the layer: the ceilings of the device the calling thread is on, so

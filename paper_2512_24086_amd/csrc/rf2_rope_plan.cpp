@@ -1,0 +1,79 @@
+// Host side of the norms and rotations of Q and K: configuration checks, frequencies, sizes.
+#include "rf2_rope.h"
+
+#include <cmath>
+#include <new>
+
+extern "C" {
+
+int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host, rf2_rope_plan** out) {
+  if (!cfg || !out) return RF2_ERR_INVALID_ARG;
+  *out = nullptr;
+  const rf2_rope_config& c = *cfg;
+  if (c.heads < 1 || c.kv_heads < 1) return RF2_ERR_INVALID_ARG;
+  if (c.dtype != RF2_DTYPE_BF16 && c.dtype != RF2_DTYPE_F16) return RF2_ERR_INVALID_ARG;
+  if (c.weight_dtype != c.dtype && c.weight_dtype != RF2_DTYPE_F32) return RF2_ERR_INVALID_ARG;
+  if (c.norm != RF2_NORM_NONE && c.norm != RF2_NORM_RMS) return RF2_ERR_INVALID_ARG;
+  if (c.norm == RF2_NORM_RMS && !(c.eps >= 1e-30f && c.eps <= 1.0f)) return RF2_ERR_INVALID_ARG;  // also rejects NaN
+  if (c.pairing != RF2_ROPE_PAIRS && c.pairing != RF2_ROPE_HALVES) return RF2_ERR_INVALID_ARG;
+  if (c.axes < 0 || c.axes > 4 || (c.axes == 0 && c.norm == RF2_NORM_NONE)) return RF2_ERR_INVALID_ARG;
+  if (c.head_dim != 64 && c.head_dim != 128) return RF2_ERR_UNSUPPORTED;
+  if (c.heads > 65535 || c.kv_heads > 65535) return RF2_ERR_UNSUPPORTED;
+  int64_t dims = 0;
+  for (int a = 0; a < c.axes; ++a) {
+    if (c.axis_dim[a] < 0 || c.axis_dim[a] % 2 != 0) return RF2_ERR_INVALID_ARG;
+    dims += c.axis_dim[a];
+  }
+  if (dims > c.head_dim) return RF2_ERR_INVALID_ARG;
+  if (c.axes > 0 && !inv_freq_host && !(c.theta > 0.0 && std::isfinite(c.theta))) return RF2_ERR_INVALID_ARG;
+
+  // turns per position of each pair; pairs behind the last axis do not turn
+  constexpr double TWO_PI = 6.283185307179586476925286766559;
+  rf2_rope_pair pairs[128] = {};
+  int i = 0;
+  for (int a = 0; a < c.axes; ++a)
+    for (int j = 0; j < c.axis_dim[a] / 2; ++j, ++i) {
+      const double f = inv_freq_host ? inv_freq_host[i] : std::pow(c.theta, -2.0 * j / c.axis_dim[a]);
+      if (!(std::fabs(f) <= 65536.0)) return RF2_ERR_INVALID_ARG;
+      pairs[i] = {f / TWO_PI, a, 0};
+      pairs[64 + i] = {-f / TWO_PI, a, 0};
+    }
+
+  rf2_rope_plan* p = new (std::nothrow) rf2_rope_plan();
+  if (!p) return RF2_ERR_ALLOC;
+  p->cfg = c;
+  p->d_pairs = nullptr;
+  p->info.workspace_bytes = c.norm == RF2_NORM_RMS ? rf2_rope_workspace(c.head_dim) : 0;
+  int n_dev = 0;
+  if (hipGetDeviceCount(&n_dev) != hipSuccess || n_dev == 0) {
+    (void)hipGetLastError();
+    p->device = -1;
+    *out = p;
+    return RF2_OK;
+  }
+  hipError_t e = hipGetDevice(&p->device);
+  if (e == hipSuccess) e = hipMalloc((void**)&p->d_pairs, sizeof pairs);
+  if (e == hipSuccess) e = hipMemcpy(p->d_pairs, pairs, sizeof pairs, hipMemcpyHostToDevice);
+  if (e != hipSuccess) {
+    const int rc = e == hipErrorOutOfMemory ? ((void)hipGetLastError(), (int)RF2_ERR_ALLOC) : rf2_note_hip_error(e);
+    rf2_rope_plan_destroy(p);
+    return rc;
+  }
+  *out = p;
+  return RF2_OK;
+}
+
+int rf2_rope_plan_destroy(rf2_rope_plan* plan) {
+  if (!plan) return RF2_OK;
+  if (plan->d_pairs) (void)hipFree(plan->d_pairs);
+  delete plan;
+  return RF2_OK;
+}
+
+int rf2_rope_plan_info(const rf2_rope_plan* plan, rf2_rope_info* out) {
+  if (!plan || !out) return RF2_ERR_INVALID_ARG;
+  *out = plan->info;
+  return RF2_OK;
+}
+
+}  // extern "C"

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -18,7 +19,9 @@ RF2_ERR_INVALID_ARG, RF2_ERR_UNSUPPORTED, RF2_ERR_ALLOC, RF2_ERR_HIP, RF2_ERR_TO
 RF2_BUDGET_GLOBAL, RF2_BUDGET_ROW_INCL_SINK, RF2_BUDGET_ROW_PLUS_SINK = 0, 1, 2
 RF2_LAYOUT_BHND, RF2_LAYOUT_BNHD = 0, 1
 RF2_SELECT_TOPN, RF2_SELECT_CDF = 0, 1
-RF2_DTYPE_BF16, RF2_DTYPE_F16 = 0, 1
+RF2_DTYPE_BF16, RF2_DTYPE_F16, RF2_DTYPE_F32 = 0, 1, 2
+RF2_NORM_NONE, RF2_NORM_RMS = 0, 1
+RF2_ROPE_PAIRS, RF2_ROPE_HALVES = 0, 1
 RF2_PAGED_BAD_LENGTH, RF2_PAGED_SEQ_FULL, RF2_PAGED_TOKENS_FULL, RF2_PAGED_POOL_FULL = 1, 2, 4, 8
 
 
@@ -48,6 +51,15 @@ class rf2_paged_info(C.Structure):
     _fields_ = [("cache_elements", C.c_int64), ("workspace_bytes", C.c_int64)]
 
 
+class rf2_rope_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "kv_heads", "head_dim", "dtype", "weight_dtype", "norm")] + \
+               [("eps", C.c_float), ("pairing", C.c_int32), ("axes", C.c_int32), ("axis_dim", C.c_int32 * 4), ("theta", C.c_double)]
+
+
+class rf2_rope_info(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_int64)]
+
+
 # symbol -> (restype, argtypes); also the list of exports the tests check
 SIGNATURES = {
     "rf2_plan_create": (C.c_int, [C.POINTER(rf2_config), C.POINTER(C.c_void_p)]),
@@ -66,6 +78,11 @@ SIGNATURES = {
     "rf2_paged_release": (C.c_int, [C.c_void_p, C.c_int32] + [C.c_void_p] * 9),
     "rf2_paged_store": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 4),
     "rf2_paged_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64] + [C.c_void_p] * 9),
+    "rf2_rope_plan_create": (C.c_int, [C.POINTER(rf2_rope_config), C.c_void_p, C.POINTER(C.c_void_p)]),
+    "rf2_rope_plan_destroy": (C.c_int, [C.c_void_p]),
+    "rf2_rope_plan_info": (C.c_int, [C.c_void_p, C.POINTER(rf2_rope_info)]),
+    "rf2_rope_apply": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 3),
+    "rf2_rope_backward": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 6),
     "rf2_measure_peaks": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_void_p]),
     "rf2_measure_sustained_mfma": (C.c_int, [C.c_double, C.POINTER(C.c_double), C.c_void_p]),
     "rf2_probe_xcd_mapping": (C.c_int, [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_void_p]),
@@ -383,3 +400,135 @@ class PagedPlan:
             _arg(o, "o", self.dtype, n_tokens * c.heads * c.head_dim, dev),
             None if lse is None else _arg(lse, "lse", torch.float32, n_tokens * c.heads, dev), self._stream(stream)),
             "rf2_paged_attn")
+
+
+# an rf2_rows of C: the address of the first row, and how far elements of the batch, tokens and heads are apart
+_two_rows_twice, _two_rows_thrice = struct.Struct("=" + "Qqqq" * 4), struct.Struct("=" + "Qqqq" * 6)
+_NO_ROWS = (0, 0, 0, 0)
+
+
+class RopePlan:
+    """Owner of an rf2_rope_plan*: norms of the rows of Q's and K's heads and their rotation by positions of several axes.
+
+    `layout` says how the tensors handed over are indexed: [batch, tokens, heads, head_dim] (RF2_LAYOUT_BNHD) or
+    [batch, heads, tokens, head_dim] (RF2_LAYOUT_BHND), with or without the batch; their rows may lie anywhere (parts of a joint
+    projection, views), channels side by side.  pos is [tokens, axes] or [batch, tokens, axes], int32.  A plan's rotation may also ride on
+    `Plan.rf2_permute_rope` and `PagedPlan.rf2_paged_store_rope`.
+    """
+
+    def __init__(self, *, heads, kv_heads, head_dim, axis_dims, theta=10000.0, inv_freq=None, pairing=RF2_ROPE_PAIRS, norm=RF2_NORM_RMS,
+                 eps=1e-6, dtype=torch.bfloat16, weight_dtype=None, layout=RF2_LAYOUT_BNHD):
+        codes = {torch.bfloat16: RF2_DTYPE_BF16, torch.float16: RF2_DTYPE_F16, torch.float32: RF2_DTYPE_F32}
+        weight_dtype = dtype if weight_dtype is None or norm == RF2_NORM_NONE else weight_dtype
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"dtype: expected torch.bfloat16 or torch.float16, got {dtype}")
+        if weight_dtype not in codes:
+            raise ValueError(f"weight_dtype: expected {dtype} or torch.float32, got {weight_dtype}")
+        if layout not in (RF2_LAYOUT_BHND, RF2_LAYOUT_BNHD):
+            raise ValueError(f"layout: expected RF2_LAYOUT_BHND or RF2_LAYOUT_BNHD, got {layout}")
+        axis_dims = [int(x) for x in axis_dims]
+        if len(axis_dims) > 4:
+            raise ValueError(f"axis_dims: expected at most 4, got {len(axis_dims)}")
+        table = None
+        if inv_freq is not None:
+            inv_freq = [float(x) for x in inv_freq]
+            if len(inv_freq) != sum(axis_dims) // 2:
+                raise ValueError(f"inv_freq: expected {sum(axis_dims) // 2} frequencies, one for each pair, got {len(inv_freq)}")
+            table = (C.c_double * max(1, len(inv_freq)))(*inv_freq)
+        self.dtype, self.weight_dtype, self.layout = dtype, weight_dtype, layout
+        self.cfg = rf2_rope_config(heads, kv_heads, head_dim, codes[dtype], codes[weight_dtype], norm, float(eps), pairing, len(axis_dims),
+                                   (C.c_int32 * 4)(*axis_dims), float(theta))
+        self._h = C.c_void_p(0)
+        _check(lib().rf2_rope_plan_create(C.byref(self.cfg), table, C.byref(self._h)), "rf2_rope_plan_create")
+        self.info = rf2_rope_info()
+        _check(lib().rf2_rope_plan_info(self._h, C.byref(self.info)), "rf2_rope_plan_info")
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+
+    def close(self):
+        if self._h:
+            lib().rf2_rope_plan_destroy(self._h)
+            self._h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def alloc_workspace(self, device="cuda"):
+        return torch.empty(self.info.workspace_bytes, dtype=torch.uint8, device=device)
+
+    # -- arguments -----------------------------------------------------------------------------
+    def _rows(self, t, what, heads, batch, tokens):
+        """(address, strides of the batch, a token, a head) of a tensor of rows; batch and tokens as another one has them, or None."""
+        shape, stride, n = t.shape, t.stride(), t.dim()
+        token, head = (n - 3, n - 2) if self.layout == RF2_LAYOUT_BNHD else (n - 2, n - 3)
+        if (n not in (3, 4) or t.dtype is not self.dtype or t.get_device() != self.device or shape[head] != heads
+                or shape[-1] != self.cfg.head_dim or stride[-1] != 1 or (tokens is not None and (shape[token] != tokens or
+                                                                                                 (shape[0] if n == 4 else 1) != batch))):
+            order = "tokens, heads" if self.layout == RF2_LAYOUT_BNHD else "heads, tokens"
+            raise ValueError(f"{what}: expected [batch, {order}, head_dim] of {self.dtype} on device {self.device} with {heads} heads of "
+                             f"{self.cfg.head_dim} channels side by side, batch and tokens as the others have, got {tuple(shape)} of {t.dtype} on "
+                             f"{t.device}, strides {stride}")
+        # (the stride of an axis of one says nothing)
+        return (t.data_ptr(), stride[0] if n == 4 and shape[0] > 1 else 0, stride[token] if shape[token] > 1 else 0,
+                stride[head] if heads > 1 else 0)
+
+    def _sides(self, q, k, more):
+        """The rows of q's tensors and k's, (q, k, q, k, ...), and batch and tokens."""
+        one = q[0] if q[0] is not None else k[0]
+        if one is None:
+            raise ValueError("q and k: expected one at least")
+        n = one.dim()
+        batch, tokens = one.shape[0] if n == 4 else 1, one.shape[n - 3 if self.layout == RF2_LAYOUT_BNHD else n - 2] if n >= 3 else 0
+        rows = []
+        for i, name in enumerate(more):
+            for t, side, heads in ((q[i], "q", self.cfg.heads), (k[i], "k", self.cfg.kv_heads)):
+                if (t is None) != ((q if side == "q" else k)[0] is None):
+                    raise ValueError(f"{name.format(side)}: expected with the other tensors of {side}, or without them")
+                rows += _NO_ROWS if t is None else self._rows(t, name.format(side), heads, batch, tokens)
+        return rows, batch, tokens
+
+    def _pos(self, pos, batch, tokens):
+        axes = self.cfg.axes
+        if axes == 0:
+            return None, 0
+        if (pos is None or pos.dtype is not torch.int32 or pos.get_device() != self.device or not pos.is_contiguous()
+                or tuple(pos.shape) not in ((tokens, axes), (batch, tokens, axes))):
+            raise ValueError(f"pos: expected contiguous {(tokens, axes)} or {(batch, tokens, axes)} of torch.int32 on device {self.device}, got "
+                             + ("none" if pos is None else f"{tuple(pos.shape)} of {pos.dtype} on {pos.device}, strides {pos.stride()}"))
+        return pos.data_ptr(), tokens * axes if pos.dim() == 3 else 0
+
+    def _weight(self, w, what, there=True):
+        if (w is None) == (self.cfg.norm == RF2_NORM_RMS and there):
+            raise ValueError(f"{what}: expected " + ("weights of the norm" if w is None else "none: there is no norm, or no rows that have it"))
+        return None if w is None else _arg(w, what, self.weight_dtype, self.cfg.head_dim, self.device)
+
+    def _stream(self, stream):
+        return _raw_stream(self.device) if stream is None else stream.cuda_stream
+
+    # -- the calls -----------------------------------------------------------------------------
+    def rf2_rope_apply(self, q, k, pos, q_out, k_out, wq=None, wk=None, stream=None):
+        """q_out and k_out from q and k (either of them may be None, with its output).  q_out may be q, k_out k."""
+        rows, batch, tokens = self._sides((q, q_out), (k, k_out), ("{}", "{}_out"))
+        at, step = self._pos(pos, batch, tokens)
+        _check(lib().rf2_rope_apply(self._h, batch, tokens, _two_rows_twice.pack(*rows), at, step, self._weight(wq, "wq", q is not None),
+                                    self._weight(wk, "wk", k is not None), self._stream(stream)), "rf2_rope_apply")
+
+    def rf2_rope_backward(self, q, k, pos, dq_out, dk_out, dq, dk, wq=None, wk=None, dwq=None, dwk=None, workspace=None, stream=None):
+        """dq, dk, dwq, dwk from q, k and the gradients of q_out and k_out.  Without a norm q and k are not read and may be None."""
+        norm = self.cfg.norm == RF2_NORM_RMS
+        if not norm:
+            q, k = dq_out, dk_out
+        rows, batch, tokens = self._sides((q, dq_out, dq), (k, dk_out, dk), ("{}", "d{}_out", "d{}"))
+        at, step = self._pos(pos, batch, tokens)
+        f32, d = torch.float32, self.cfg.head_dim
+        for name, dw, side in (("dwq", dwq, q), ("dwk", dwk, k)):
+            if (dw is None) == (norm and side is not None):
+                raise ValueError(f"{name}: expected " + (f"{d} elements of {f32}" if dw is None else "none: there is no norm, or no rows that have it"))
+        _check(lib().rf2_rope_backward(
+            self._h, batch, tokens, _two_rows_thrice.pack(*rows), at, step, self._weight(wq, "wq", q is not None),
+            self._weight(wk, "wk", k is not None), None if dwq is None else _arg(dwq, "dwq", f32, d, self.device),
+            None if dwk is None else _arg(dwk, "dwk", f32, d, self.device),
+            None if not norm or workspace is None else _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, self.device),
+            self._stream(stream)), "rf2_rope_backward")
