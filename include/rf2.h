@@ -11,10 +11,12 @@
  *                         selection, plus the first-frame sink of Sec. 3.4
  *   rf2_block_sparse_attn Sec. 3.1, eqs. (1)-(4) with the block skip rule
  *   rf2_unpermute         inverse of the Sec. 3.3 permutation
- *   (rf2_block_sparse_attn_unpermuted does the last two in one kernel.)
+ *   (rf2_block_sparse_attn_unpermuted does the last two in one kernel, rf2_permute_rope the first one for rows that are yet to be
+ *   normalised and rotated by their positions.)
  *
  * Beside it, for models that generate chunk after chunk (new frames, or tokens, that attend to everything generated
- * before): a paged cache of keys and values and the attention of new tokens over it, rf2_paged_* below.
+ * before): a paged cache of keys and values and the attention of new tokens over it, rf2_paged_* below; and what comes before either of
+ * them, norms and rotary positions of Q and K with their gradients, rf2_rope_*.
  *
  * Conventions
  *   - Every function returns an int: RF2_OK (0) or a negative RF2_ERR_* code.
@@ -468,6 +470,39 @@ int rf2_rope_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, c
  */
 int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rope_gradients* rows, const int32_t* pos,
                       int64_t pos_batch, const void* wq, const void* wk, float* dwq, float* dwk, void* workspace, void* stream);
+
+/*
+ * rf2_permute with Q and K normalised and rotated on the way: the layer's first call for a model's raw projections.  The same bytes are
+ * read and written, and the pass over Q and K before it is saved.
+ *   rope      : a plan for dtype bf16, of the layer's head_dim and heads (kv_heads the same), on its device
+ *   pos       : [N][axes] int32 by token, as q, k and v lie (text tokens behind the grid's), pos_batch elements from one element of the
+ *               batch to the next (0: all have the same)                                       (in)
+ *   wq, wk    : weights of the norms; of the grid's tokens alone where there are others for the text (in)
+ *   wq_text, wk_text : weights of the norms of the text tokens; both NULL: as wq and wk         (in)
+ *   qbar, kbar: means of the rows before they are rounded to bf16, where rf2_permute's are means of rounded rows: the two differ by a
+ *               fraction of a step of bf16                                                     (out)
+ * All other arguments as for rf2_permute; they are aligned to 16 bytes, pos, qbar and kbar to 4.  qp and kp are what rf2_rope_apply followed by
+ * rf2_permute leave there.
+ */
+int rf2_permute_rope(const rf2_plan* plan, const rf2_rope_plan* rope, const void* q, const void* k, const void* v, const int32_t* pos,
+                     int64_t pos_batch, const void* wq, const void* wk, const void* wq_text, const void* wk_text, void* qp, void* kp, void* vp,
+                     float* qbar, float* kbar, void* stream);
+
+/*
+ * rf2_paged_store for raw projections: the new tokens' Q is normalised and rotated into q_out (what rf2_paged_attn reads), their K too and
+ * into the cache, V goes into the cache as it is.  One launch.
+ *   rope      : a plan of the cache's heads, kv_heads, head_dim and dtype, on its device
+ *   q         : [n_tokens, heads, head_dim], rows q_stride elements apart                      (in)
+ *   pos       : [n_tokens][axes] int32                                                         (in)
+ *   n_live    : NULL, or one int32 in device memory: tokens from it on are padding, whose rows of q_out stay as they are
+ *               (cu_new + n_seqs of rf2_paged_append; slots already says so for the cache)     (in)
+ *   q_out     : [n_tokens, heads, head_dim], rows q_out_stride elements apart; may be q with its stride, else shares no memory with anything (out)
+ * All other arguments as for rf2_paged_store; strides are at least a row, multiples of 8, and at most 2^36.  Cache and q_out are what
+ * rf2_rope_apply followed by rf2_paged_store leave there.  ceil(n_tokens / 32) * kv_heads above 2^23 - 8 is RF2_ERR_UNSUPPORTED.
+ */
+int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_plan* rope, int32_t n_tokens, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride, const int32_t* pos, const void* wq, const void* wk, const int32_t* slots,
+                         const int32_t* n_live, void* k_cache, void* v_cache, void* q_out, int64_t q_out_stride, void* stream);
 
 /*
  * Measurement aid, not part of the layer: the ceilings of the device the calling thread is on, so

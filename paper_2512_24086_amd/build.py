@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librf2.so")
 SOURCES = ["rf2_plan.cpp", "rf2_permute.hip", "rf2_mask.hip", "rf2_attn.hip", "rf2_probe.hip",
            "rf2_paged.cpp", "rf2_paged_tables.hip", "rf2_paged_store.hip", "rf2_paged_attn.hip",
-           "rf2_rope_plan.cpp", "rf2_rope.hip"]
+           "rf2_rope_plan.cpp", "rf2_rope.hip", "rf2_permute_rope.hip", "rf2_paged_store_rope.hip"]
 # Packed-fp32 VALU forms are switched off on purpose (they have misbehaved on the target machines).
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

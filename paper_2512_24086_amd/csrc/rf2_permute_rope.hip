@@ -1,0 +1,207 @@
+// Window permutation and block means of a layer, Q and K normalised and rotated on the way (gfx950).
+//
+// HBM bound, like the permutation by itself: the same bytes are read and written, and a pass over Q and K before it is saved.  A workgroup takes
+// a block of rows through four heads: cosines and sines belong to a token, and the loads of the heads' rows are on their way
+// together.  A wavefront holds eight rows, d / 8 lanes to a row (d = 64) or in two sets of four (d = 128).
+#include "rf2_permute_rows.h"
+#include "rf2_rope.h"
+
+namespace {
+
+struct PermuteRopeArgs {
+  PermuteArgs p;
+  RopeArgs rope;
+  const int32_t* pos;
+  int64_t pos_batch;
+  const void *w[2], *w_text[2];      // of Q and K; of the tokens behind the grid's
+  int video;                         // tokens of the grid
+  int norm;
+  uint32_t groups;                   // of heads
+};
+
+constexpr int HEADS = 4;
+
+template <bool KEEP>
+__device__ __forceinline__ rope_u32x4 ld_row(const u16* p) {
+  if constexpr (KEEP) return *reinterpret_cast<const rope_u32x4*>(p);
+  else return __builtin_nontemporal_load(reinterpret_cast<const rope_u32x4*>(p));
+}
+template <bool KEEP>
+__device__ __forceinline__ void st_row(u16* p, const rope_u32x4& v) {
+  if constexpr (KEEP) *reinterpret_cast<rope_u32x4*>(p) = v;
+  else __builtin_nontemporal_store(v, reinterpret_cast<rope_u32x4*>(p));
+}
+
+template <int D>
+using mean_sums = float[4][HEADS][D];
+
+// Rows of a block of Q (row by row) or K (operand parts, see rf2.h), HEADS heads from h0 on.
+template <int D, bool IS_K, bool HALVES, bool NORM, int KEEP>
+__device__ __forceinline__ void rope_block(const PermuteRopeArgs& a, int rows, int n_blocks, int last_valid, int blk, int b, int h0, mean_sums<D>& sums) {
+  constexpr int CH = D / 8, SETS = CH / 8;                  // sets of rows of a wavefront
+  const PermuteArgs& p = a.p;
+  const u16* const x = reinterpret_cast<const u16*>(IS_K ? p.k : p.q) + (int64_t)b * p.st.batch * D;
+  u16* const xp = reinterpret_cast<u16*>(IS_K ? p.kp : p.qp);
+  float* const mean = IS_K ? p.kbar : p.qbar;
+  const int heads = min(HEADS, p.heads - h0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
+  const int half = rows / 2;
+  float sum[HEADS][8] = {};
+  for (int r0 = 8 * wave; r0 < rows; r0 += 32) {
+    int n[SETS];
+    rope_u32x4 v[SETS][HEADS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) n[s] = p.perm[blk * rows + r0 + 4 * s + g];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i) {
+        v[s][i] = rope_u32x4{0, 0, 0, 0};
+        if (i < heads && n[s] >= 0) v[s][i] = ld_row<KEEP == 2>(x + ((h0 + i) * p.st.head + (int64_t)n[s] * p.st.token) * D + 8 * c);
+      }
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      const int at = max(n[s], 0);
+      const void* const w = NORM && at >= a.video && a.w_text[IS_K] ? a.w_text[IS_K] : a.w[IS_K];
+      float A[8], B[8];
+      rope_factors<RopeBf16, D, HALVES, NORM>(a.rope, a.pos + b * a.pos_batch + (int64_t)at * a.rope.axes, w, c, A, B);
+      if (n[s] < 0)                                          // rows behind the last are 0, not -0
+#pragma unroll
+        for (int e = 0; e < 8; ++e) A[e] = B[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i) {
+        float y[8];
+        RopeBf16::unpack(v[s][i], y);
+        rope_row<D, HALVES, NORM>(a.rope, A, B, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[i][e] += y[e];
+        v[s][i] = RopeBf16::pack(y);
+      }
+    }
+    if constexpr (IS_K && SETS == 2) {
+      // The first set's upper chunks against the second's lower ones: a store then covers eight rows of eight chunks, whole lines of 128 bytes.
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t first = v[0][i][e], second = v[1][i][e];
+          v[0][i][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)first, (int)second, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
+          v[1][i][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)second, (int)first, 0x128, 0xf, 0x3, false);      // and into lanes 0-7
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+      if (i < heads) {
+        u16* const to = xp + ((int64_t)(b * p.heads + h0 + i) * n_blocks + blk) * rows * D;
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+          int r = r0 + 4 * s + g, chunk = c;
+          if (IS_K && SETS == 2) r = r0 + 4 * (c / 8) + g, chunk = 8 * s + c % 8;
+          const int k_slot = ((r % half) / 32 * CH + chunk) * 64 + r / half * 32 + r % 32;
+          st_row<KEEP >= 1>(to + (IS_K ? k_slot : r * CH + chunk) * 8, v[s][i]);
+        }
+      }
+  }
+  if (mean == nullptr) return;
+  // the wavefront's rows are added lane by lane, the wavefronts' sums in LDS: a fixed order
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (D == 64) sum[i][e] += __shfl_xor(sum[i][e], 8);
+      sum[i][e] += __shfl_xor(sum[i][e], 16);
+      sum[i][e] += __shfl_xor(sum[i][e], 32);
+      if (lane < CH) sums[wave][i][8 * c + e] = sum[i][e];
+    }
+  __syncthreads();
+  const int count = blk == n_blocks - 1 ? last_valid : rows;
+  for (int i = threadIdx.x; i < heads * D; i += 256) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s += sums[w][i / D][i % D];
+    mean[((int64_t)(b * p.heads + h0 + i / D) * n_blocks + blk) * D + i % D] = s / (float)count;
+  }
+}
+
+// First the Q blocks, then the K blocks, then V's parts, as in the permutation by itself.
+template <int D, int BK, bool HALVES, int KEEP>
+__global__ void __launch_bounds__(256) permute_rope_kernel(PermuteRopeArgs a, int q_rows) {
+  __shared__ __attribute__((aligned(16))) union { mean_sums<D> sums; v_rows<D> tile; } lds;
+  const PermuteArgs& p = a.p;
+  uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+  if (id < p.q_wgs) {
+    const uint32_t blk = id % p.n_q, at = id / p.n_q, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
+    if (a.norm) rope_block<D, false, HALVES, true, KEEP>(a, q_rows, p.n_q, p.last_q, blk, b, h0, lds.sums);
+    else rope_block<D, false, HALVES, false, KEEP>(a, q_rows, p.n_q, p.last_q, blk, b, h0, lds.sums);
+    return;
+  }
+  id -= p.q_wgs;
+  if (id < p.k_wgs) {
+    const uint32_t blk = id % p.n_k, at = id / p.n_k, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
+    if (a.norm) rope_block<D, true, HALVES, true, KEEP>(a, BK, p.n_k, p.last_k, blk, b, h0, lds.sums);
+    else rope_block<D, true, HALVES, false, KEEP>(a, BK, p.n_k, p.last_k, blk, b, h0, lds.sums);
+    return;
+  }
+  id -= p.k_wgs;
+  const uint32_t parts = p.n_k * (BK / 64);
+  if (id < p.v_wgs) permute_vtile_part<D, BK, KEEP>(p.v, p.vp, p.perm, p.n_k, p.heads, p.st, id % parts, id / parts, lds.tile);
+}
+
+template <int D, int BK>
+int launch(const rf2_plan* plan, PermuteRopeArgs a, bool halves, uint32_t q_wgs, uint32_t k_wgs, uint32_t v_wgs, hipStream_t st) {
+  const uint32_t n = q_wgs + k_wgs + v_wgs, rows = (n + 65535u) / 65536u;
+  a.p.q_wgs = q_wgs, a.p.k_wgs = k_wgs, a.p.v_wgs = v_wgs;
+  const dim3 grid((n + rows - 1) / rows, rows);
+  const int64_t bytes = (3 * plan->info.N + plan->info.N_pad + 2 * plan->info.N_pad_k) * (int64_t)a.p.bh * D * 2;
+  const auto with = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, plan->cfg.block); };
+  if (halves) {
+    if (bytes <= KEEP_ALL) with(permute_rope_kernel<D, BK, true, 2>);
+    else if (bytes <= KEEP_STORES) with(permute_rope_kernel<D, BK, true, 1>);
+    else with(permute_rope_kernel<D, BK, true, 0>);
+  } else {
+    if (bytes <= KEEP_ALL) with(permute_rope_kernel<D, BK, false, 2>);
+    else if (bytes <= KEEP_STORES) with(permute_rope_kernel<D, BK, false, 1>);
+    else with(permute_rope_kernel<D, BK, false, 0>);
+  }
+  RF2_LAUNCH_CHECK();
+  return RF2_OK;
+}
+
+template <int D, int BK>
+int permute_rope(const rf2_plan* plan, const PermuteRopeArgs& a, bool halves, hipStream_t st) {
+  const uint32_t both = (uint32_t)plan->cfg.batch * a.groups, q = a.p.n_q * both, k = a.p.n_k * both, v = a.p.n_k * a.p.bh * (BK / 64);
+  if (!tensors_overlap(plan, a.p)) return launch<D, BK>(plan, a, halves, q, k, v, st);
+  if (const int rc = launch<D, BK>(plan, a, halves, q, 0, 0, st)) return rc;
+  if (const int rc = launch<D, BK>(plan, a, halves, 0, k, 0, st)) return rc;
+  return launch<D, BK>(plan, a, halves, 0, 0, v, st);
+}
+
+}  // namespace
+
+extern "C" int rf2_permute_rope(const rf2_plan* plan, const rf2_rope_plan* rope, const void* q, const void* k, const void* v, const int32_t* pos,
+                                int64_t pos_batch, const void* wq, const void* wk, const void* wq_text, const void* wk_text, void* qp, void* kp,
+                                void* vp, float* qbar, float* kbar, void* stream) {
+  if (!plan || !rope || !q || !k || !v || !qp || !kp || !vp || pos_batch < 0 || pos_batch > (int64_t)1 << 32) return RF2_ERR_INVALID_ARG;
+  if ((qbar == nullptr) != (kbar == nullptr)) return RF2_ERR_INVALID_ARG;
+  const rf2_rope_config& r = rope->cfg;
+  if (r.heads != plan->cfg.heads || r.kv_heads != plan->cfg.heads || r.head_dim != plan->cfg.head_dim || r.dtype != RF2_DTYPE_BF16 ||
+      rope->device != plan->device)
+    return RF2_ERR_INVALID_ARG;
+  if (!rf2_rope_pos_fits(rope, pos) || !rf2_rope_weight_fits(rope, wq) || !rf2_rope_weight_fits(rope, wk)) return RF2_ERR_INVALID_ARG;
+  if ((wq_text == nullptr) != (wk_text == nullptr)) return RF2_ERR_INVALID_ARG;
+  if (wq_text && (!rf2_rope_weight_fits(rope, wq_text) || !rf2_rope_weight_fits(rope, wk_text))) return RF2_ERR_INVALID_ARG;
+  for (const void* t : {q, k, v, (const void*)qp, (const void*)kp, (const void*)vp})
+    if (!rf2_rope_aligned(t, 16)) return RF2_ERR_INVALID_ARG;
+  if (!rf2_rope_aligned(qbar, 4) || !rf2_rope_aligned(kbar, 4)) return RF2_ERR_INVALID_ARG;
+  if (const int rc = rf2_check_device(plan)) return rc;
+  const rf2_info& in = plan->info;
+  const PermuteRopeArgs a{{(const uint4*)q, (const uint4*)k, (const uint4*)v, (uint4*)qp, (uint4*)kp, (uint4*)vp, qbar, kbar, plan->d_perm,
+                           (uint32_t)in.n_blocks, (uint32_t)in.n_blocks_k, (uint32_t)(plan->cfg.batch * plan->cfg.heads), 0, 0, 0,
+                           in.last_block_valid, in.last_block_valid_k, plan->cfg.heads, rf2_qkv_strides(plan)},
+                          rope_args(rope), pos, pos_batch, {wq, wk}, {wq_text, wk_text}, (int)(in.N - plan->cfg.text_tokens),
+                          r.norm == RF2_NORM_RMS, (uint32_t)((plan->cfg.heads + HEADS - 1) / HEADS)};
+  const bool halves = r.pairing == RF2_ROPE_HALVES;
+  hipStream_t st = (hipStream_t)stream;
+  if (plan->cfg.head_dim == 128) return in.block_k == 128 ? permute_rope<128, 128>(plan, a, halves, st) : permute_rope<128, 64>(plan, a, halves, st);
+  return in.block_k == 128 ? permute_rope<64, 128>(plan, a, halves, st) : permute_rope<64, 64>(plan, a, halves, st);
+}

@@ -1,5 +1,8 @@
 // Norms of heads' rows and rotation by positions: the plan, and what the kernels that do it share (not installed).
 #pragma once
+#include <algorithm>
+#include <type_traits>
+
 #include "rf2_internal.h"
 
 // A pair of channels: turns per unit of its axis' position.
@@ -121,6 +124,7 @@ __device__ __forceinline__ void rope_partners(const float (&x)[8], float (&y)[8]
 // where rounding to 32 bits alone is 1.5e-8).
 template <int D, bool HALVES>
 __device__ __forceinline__ void rope_angles(const RopeArgs& a, const int32_t* __restrict__ pos, int c, float (&cs)[8], float (&sn)[8]) {
+#pragma clang fp contract(off)                  // (the kernels that share this are to give the same bits)
   constexpr int N = HALVES ? 8 : 4;
   int p[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -208,6 +212,134 @@ __device__ __forceinline__ void rope_row(const RopeArgs& a, const float (&A)[8],
   rope_partners<D, HALVES>(x, y);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = fmaf(y[e], B[e], x[e] * A[e]);
+}
+
+// Rows of a tensor, in elements.
+struct RopeRows {
+  const uint16_t* at;
+  int64_t batch, token, head;
+};
+
+// Rows of Q or of K, in and out, and how wavefronts share them.
+struct RopeSide {
+  RopeRows x, z;                 // in, out
+  const void* w;
+  int heads, heads_log2;     // heads; log2 of the rows of a wavefront that are neighbouring heads
+  int steps, groups;         // of heads a wavefront goes through, and wavefronts that share a token's heads
+  uint32_t workgroups;
+};
+
+// Tokens and their positions.
+struct RopeTokens {
+  const int32_t* pos;
+  int64_t pos_batch;
+  uint32_t tokens, total;    // of an element of the batch, of all
+};
+template <bool KEEP>
+__device__ __forceinline__ rope_u32x4 rope_load(const uint16_t* p) {
+  if constexpr (KEEP) return *reinterpret_cast<const rope_u32x4*>(p);
+  else return __builtin_nontemporal_load(reinterpret_cast<const rope_u32x4*>(p));
+}
+template <bool KEEP>
+__device__ __forceinline__ void rope_store(uint16_t* p, const rope_u32x4& v) {
+  if constexpr (KEEP) *reinterpret_cast<rope_u32x4*>(p) = v;
+  else __builtin_nontemporal_store(v, reinterpret_cast<rope_u32x4*>(p));
+}
+
+// Token m of all, as an element of the batch and a token of it.
+struct RopeToken {
+  uint32_t b, n;
+};
+__device__ __forceinline__ RopeToken rope_token(uint32_t m, uint32_t tokens, uint32_t total) {
+  if (tokens == total) return {0, m};
+  const uint32_t b = m / tokens;
+  return {b, m - b * tokens};
+}
+
+// What a workgroup of 256 threads does of a side: 4 * (64 / (d / 8)) rows at a time.
+template <class T, int D, bool HALVES, bool NORM, bool KEEP>
+__device__ __forceinline__ void rope_apply_rows(const RopeArgs& a, const RopeTokens& t, const RopeSide& s, uint32_t id) {
+  constexpr int CH = D / 8, R = 64 / CH, U = 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
+  const int by_head = 1 << s.heads_log2, by_token = R >> s.heads_log2;
+  const uint32_t tile = id / (uint32_t)s.groups, group = id - tile * (uint32_t)s.groups;
+  const uint32_t m = (tile * 4 + wave) * by_token + (g >> s.heads_log2);
+  if (m >= t.total) return;
+  const RopeToken token = rope_token(m, t.tokens, t.total);
+  int h = group * s.steps * by_head + (g & (by_head - 1));
+  const int end = min(s.heads, (int)(group + 1) * s.steps * by_head);
+  const uint16_t* from = s.x.at + token.b * s.x.batch + token.n * s.x.token + h * s.x.head + 8 * c;
+  uint16_t* to = const_cast<uint16_t*>(s.z.at) + token.b * s.z.batch + token.n * s.z.token + h * s.z.head + 8 * c;
+  const int64_t from_step = s.x.head * by_head, to_step = s.z.head * by_head;
+  float A[8], B[8];
+  bool first = true;
+  while (h < end) {
+    rope_u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h + u * by_head < end) v[u] = rope_load<KEEP>(from + u * from_step);
+    if (first) {
+      rope_factors<T, D, HALVES, NORM>(a, t.pos + token.b * t.pos_batch + (int64_t)token.n * a.axes, s.w, c, A, B);
+      first = false;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (h + u * by_head < end) {
+        float x[8];
+        T::unpack(v[u], x);
+        rope_row<D, HALVES, NORM>(a, A, B, x);
+        rope_store<KEEP>(to + u * to_step, T::pack(x));
+      }
+    h += U * by_head;
+    from += U * from_step;
+    to += U * to_step;
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------
+
+inline RopeRows rope_rows(const rf2_rows& r) { return {(const uint16_t*)r.at, r.batch, r.token, r.head}; }
+
+// How many rows of a wavefront are neighbouring heads of a token (log2): all where heads lie side by side and there are as many.
+inline int rope_heads_log2(const rf2_rows& r, int heads, int rows) {
+  if (r.head >= r.token) return 0;
+  int log2 = 0;
+  while (2 << log2 <= rows && 2 << log2 <= heads) ++log2;
+  return log2;
+}
+
+// How the wavefronts of a launch share rows: `wavefronts` of tokens, `groups` of heads for each.
+struct RopeShare {
+  int heads_log2, steps, groups;
+  uint32_t tiles;            // of four wavefronts' tokens
+};
+inline RopeShare rope_share(const rf2_rows& x, int heads, int head_dim, uint32_t tokens) {
+  const int rows = 512 / head_dim, log2 = rope_heads_log2(x, heads, rows), by_head = 1 << log2, all_steps = (heads + by_head - 1) / by_head;
+  const int64_t wavefronts = ((int64_t)tokens * by_head + rows - 1) / rows;
+  const int steps = (int)std::min<int64_t>(all_steps, std::max<int64_t>(1, wavefronts * all_steps / 8192));
+  return {log2, steps, (all_steps + steps - 1) / steps, (uint32_t)((wavefronts + 3) / 4)};
+}
+inline RopeSide rope_side(const rf2_rows& x, const rf2_rows& z, const void* w, int heads, int head_dim, uint32_t tokens) {
+  const RopeShare s = rope_share(x, heads, head_dim, tokens);
+  return {rope_rows(x), rope_rows(z), w, heads, s.heads_log2, s.steps, s.groups, x.at ? s.tiles * (uint32_t)s.groups : 0};
+}
+
+constexpr int64_t ROPE_KEEP = (int64_t)160 << 20;
+
+template <class F>
+int rope_for_types(const rf2_rope_config& c, F f) {
+  const auto pairing = [&](auto type, auto d) {
+    if (c.pairing == RF2_ROPE_HALVES) f(type, d, std::true_type());
+    else f(type, d, std::false_type());
+  };
+  const auto dim = [&](auto type) {
+    if (c.head_dim == 128) pairing(type, std::integral_constant<int, 128>());
+    else pairing(type, std::integral_constant<int, 64>());
+  };
+  if (c.dtype == RF2_DTYPE_F16) dim(RopeF16());
+  else dim(RopeBf16());
+  RF2_LAUNCH_CHECK();
+  return RF2_OK;
 }
 
 }  // namespace

@@ -3,101 +3,26 @@
 // HBM bound: each row is read once and written once.  d / 8 neighbouring lanes hold a row, 16 bytes each.  Cosines and sines belong to a
 // token, not to a head: a wavefront takes a few tokens, works their angles out once and goes through the heads, 64 / (d / 8) rows at a
 // time.  Those are consecutive tokens of a head where tokens lie side by side, consecutive heads of a token where heads do.
-#include <algorithm>
-#include <type_traits>
-
 #include "rf2_rope.h"
 
 namespace {
 
-struct Rows {
-  const uint16_t* at;
-  int64_t batch, token, head;
-};
-
-struct Side {
-  Rows x, z;                 // in, out
-  const void* w;
-  int heads, heads_log2;     // heads; log2 of the rows of a wavefront that are neighbouring heads
-  int steps, groups;         // of heads a wavefront goes through, and wavefronts that share a token's heads
-  uint32_t workgroups;
-};
-
 struct ApplyArgs {
   RopeArgs rope;
-  const int32_t* pos;
-  int64_t pos_batch;
-  uint32_t tokens, total;    // of an element of the batch, of all
-  Side side[2];
+  RopeTokens tokens;
+  RopeSide side[2];
 };
-
-template <bool KEEP>
-__device__ __forceinline__ rope_u32x4 load(const uint16_t* p) {
-  if constexpr (KEEP) return *reinterpret_cast<const rope_u32x4*>(p);
-  else return __builtin_nontemporal_load(reinterpret_cast<const rope_u32x4*>(p));
-}
-template <bool KEEP>
-__device__ __forceinline__ void store(uint16_t* p, const rope_u32x4& v) {
-  if constexpr (KEEP) *reinterpret_cast<rope_u32x4*>(p) = v;
-  else __builtin_nontemporal_store(v, reinterpret_cast<rope_u32x4*>(p));
-}
-
-// Token m of all, as an element of the batch and a token of it.
-struct Token {
-  uint32_t b, n;
-};
-__device__ __forceinline__ Token token_of(uint32_t m, uint32_t tokens, uint32_t total) {
-  if (tokens == total) return {0, m};
-  const uint32_t b = m / tokens;
-  return {b, m - b * tokens};
-}
 
 template <class T, int D, bool HALVES, bool NORM, bool KEEP>
 __global__ void __launch_bounds__(256) apply_kernel(ApplyArgs a) {
-  constexpr int CH = D / 8, R = 64 / CH, U = 4;
   const bool second = blockIdx.x >= a.side[0].workgroups;
-  const Side& s = a.side[second ? 1 : 0];
-  const uint32_t id = blockIdx.x - (second ? a.side[0].workgroups : 0);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
-  const int by_head = 1 << s.heads_log2, by_token = R >> s.heads_log2;
-  const uint32_t tile = id / (uint32_t)s.groups, group = id - tile * (uint32_t)s.groups;
-  const uint32_t m = (tile * 4 + wave) * by_token + (g >> s.heads_log2);
-  if (m >= a.total) return;
-  const Token t = token_of(m, a.tokens, a.total);
-  int h = group * s.steps * by_head + (g & (by_head - 1));
-  const int end = min(s.heads, (int)(group + 1) * s.steps * by_head);
-  const uint16_t* from = s.x.at + t.b * s.x.batch + t.n * s.x.token + h * s.x.head + 8 * c;
-  uint16_t* to = const_cast<uint16_t*>(s.z.at) + t.b * s.z.batch + t.n * s.z.token + h * s.z.head + 8 * c;
-  const int64_t from_step = s.x.head * by_head, to_step = s.z.head * by_head;
-  float A[8], B[8];
-  bool first = true;
-  while (h < end) {
-    rope_u32x4 v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (h + u * by_head < end) v[u] = load<KEEP>(from + u * from_step);
-    if (first) {
-      rope_factors<T, D, HALVES, NORM>(a.rope, a.pos + t.b * a.pos_batch + (int64_t)t.n * a.rope.axes, s.w, c, A, B);
-      first = false;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (h + u * by_head < end) {
-        float x[8];
-        T::unpack(v[u], x);
-        rope_row<D, HALVES, NORM>(a.rope, A, B, x);
-        store<KEEP>(to + u * to_step, T::pack(x));
-      }
-    h += U * by_head;
-    from += U * from_step;
-    to += U * to_step;
-  }
+  rope_apply_rows<T, D, HALVES, NORM, KEEP>(a.rope, a.tokens, a.side[second ? 1 : 0], blockIdx.x - (second ? a.side[0].workgroups : 0));
 }
 
 // ---- gradients --------------------------------------------------------------------------------------------------
 
 struct BackSide {
-  Rows x, dz, dx;
+  RopeRows x, dz, dx;
   const void* w;
   float* sums;               // of the workgroups, [workgroups][d]; the gradient itself where there is one workgroup
   int heads, heads_log2, steps, groups;
@@ -105,9 +30,7 @@ struct BackSide {
 };
 struct BackArgs {
   RopeArgs rope;
-  const int32_t* pos;
-  int64_t pos_batch;
-  uint32_t tokens, total;
+  RopeTokens tokens;
   BackSide side[2];
 };
 
@@ -129,20 +52,20 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
     const uint32_t tile = unit / (uint32_t)s.groups, group = unit - tile * (uint32_t)s.groups;
     const uint32_t m = (tile * 4 + wave) * by_token + (g >> s.heads_log2);
     int h = group * s.steps * by_head + (g & (by_head - 1));
-    const int end = m < a.total ? min(s.heads, (int)(group + 1) * s.steps * by_head) : 0;
-    const Token t = token_of(min(m, a.total - 1), a.tokens, a.total);
+    const int end = m < a.tokens.total ? min(s.heads, (int)(group + 1) * s.steps * by_head) : 0;
+    const RopeToken t = rope_token(min(m, a.tokens.total - 1), a.tokens.tokens, a.tokens.total);
     const uint16_t* x_at = s.x.at + t.b * s.x.batch + t.n * s.x.token + h * s.x.head + 8 * c;
     const uint16_t* dz_at = s.dz.at + t.b * s.dz.batch + t.n * s.dz.token + h * s.dz.head + 8 * c;
     uint16_t* dx_at = const_cast<uint16_t*>(s.dx.at) + t.b * s.dx.batch + t.n * s.dx.token + h * s.dx.head + 8 * c;
     float cs[8], sn[8], sum[8] = {};
-    rope_angles<D, HALVES>(a.rope, a.pos + t.b * a.pos_batch + (int64_t)t.n * a.rope.axes, c, cs, sn);
+    rope_angles<D, HALVES>(a.rope, a.tokens.pos + t.b * a.tokens.pos_batch + (int64_t)t.n * a.rope.axes, c, cs, sn);
     while (h < end) {
       rope_u32x4 vx[U], vz[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (h + u * by_head < end) {
-          vx[u] = load<KEEP>(x_at + u * by_head * s.x.head);
-          vz[u] = load<KEEP>(dz_at + u * by_head * s.dz.head);
+          vx[u] = rope_load<KEEP>(x_at + u * by_head * s.x.head);
+          vz[u] = rope_load<KEEP>(dz_at + u * by_head * s.dz.head);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -163,7 +86,7 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
           m = rope_row_sum<D>(m) * (1.f / D);
 #pragma unroll
           for (int e = 0; e < 8; ++e) z[e] = r * fmaf(-x[e], m, z[e]);
-          store<KEEP>(dx_at + u * by_head * s.dx.head, T::pack(z));
+          rope_store<KEEP>(dx_at + u * by_head * s.dx.head, T::pack(z));
         }
       h += U * by_head;
       x_at += U * by_head * s.x.head;
@@ -232,34 +155,6 @@ bool in_range(const rf2_rows& r, int32_t batch, int32_t tokens, int32_t heads) {
   return r.batch <= most / batch && r.token <= most / tokens && r.head <= most / heads;
 }
 
-Rows rows_of(const rf2_rows& r) { return {(const uint16_t*)r.at, r.batch, r.token, r.head}; }
-
-// How many rows of a wavefront are neighbouring heads of a token (log2): all where heads lie side by side and there are as many.
-int heads_log2(const rf2_rows& r, int heads, int rows) {
-  if (r.head >= r.token) return 0;
-  int log2 = 0;
-  while (2 << log2 <= rows && 2 << log2 <= heads) ++log2;
-  return log2;
-}
-
-constexpr int64_t KEEP = (int64_t)160 << 20;
-
-template <class F>
-int for_types(const rf2_rope_config& c, F f) {
-  const auto pairing = [&](auto type, auto d) {
-    if (c.pairing == RF2_ROPE_HALVES) f(type, d, std::true_type());
-    else f(type, d, std::false_type());
-  };
-  const auto dim = [&](auto type) {
-    if (c.head_dim == 128) pairing(type, std::integral_constant<int, 128>());
-    else pairing(type, std::integral_constant<int, 64>());
-  };
-  if (c.dtype == RF2_DTYPE_F16) dim(RopeF16());
-  else dim(RopeBf16());
-  RF2_LAUNCH_CHECK();
-  return RF2_OK;
-}
-
 template <bool B>
 using flag = std::integral_constant<bool, B>;
 
@@ -286,31 +181,21 @@ int check_tokens(int32_t batch, int32_t n_tokens, int64_t pos_batch) {
 int launch_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rows& q, const rf2_rows& k, const int32_t* pos, int64_t pos_batch,
                  const void* wq, const void* wk, const rf2_rows& q_out, const rf2_rows& k_out, bool norm, bool inverse, hipStream_t st) {
   const rf2_rope_config& c = plan->cfg;
-  const int rows = 512 / c.head_dim;
-  ApplyArgs a{rope_args(plan, inverse), pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens, {}};
+  ApplyArgs a{rope_args(plan, inverse), {pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens}, {}};
   int64_t bytes = 0;
   for (int i = 0; i < 2; ++i) {
     const rf2_rows& x = i == 0 ? q : k;
-    Side& s = a.side[i];
-    s.x = rows_of(x);
-    s.z = rows_of(i == 0 ? q_out : k_out);
-    s.w = i == 0 ? wq : wk;
-    s.heads = i == 0 ? c.heads : c.kv_heads;
-    s.heads_log2 = heads_log2(x, s.heads, rows);
-    const int by_head = 1 << s.heads_log2, all_steps = (s.heads + by_head - 1) / by_head;
-    const int64_t wavefronts = ((int64_t)a.total * by_head + rows - 1) / rows;
-    s.steps = (int)std::min<int64_t>(all_steps, std::max<int64_t>(1, wavefronts * all_steps / 8192));
-    s.groups = (all_steps + s.steps - 1) / s.steps;
-    s.workgroups = x.at ? (uint32_t)((wavefronts + 3) / 4) * (uint32_t)s.groups : 0;
-    if (x.at) bytes += (int64_t)a.total * s.heads * c.head_dim * 4;
+    const int heads = i == 0 ? c.heads : c.kv_heads;
+    a.side[i] = rope_side(x, i == 0 ? q_out : k_out, i == 0 ? wq : wk, heads, c.head_dim, a.tokens.total);
+    if (x.at) bytes += (int64_t)a.tokens.total * heads * c.head_dim * 4;
   }
   const dim3 grid(a.side[0].workgroups + a.side[1].workgroups);
-  return for_types(c, [&](auto type, auto d, auto halves) {
+  return rope_for_types(c, [&](auto type, auto d, auto halves) {
     const auto launch = [&](auto with_norm, auto keep) {
       apply_kernel<decltype(type), d(), halves(), with_norm(), keep()><<<grid, 256, 0, st>>>(a);
     };
     const auto with = [&](auto keep) { norm ? launch(flag<true>(), keep) : launch(flag<false>(), keep); };
-    bytes <= KEEP ? with(flag<true>()) : with(flag<false>());
+    bytes <= ROPE_KEEP ? with(flag<true>()) : with(flag<false>());
   });
 }
 
@@ -356,34 +241,29 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     return launch_apply(plan, batch, n_tokens, rows->dq_out, rows->dk_out, pos, pos_batch, nullptr, nullptr, rows->dq, rows->dk, false, true, st);
   }
 
-  const int per_wave = 512 / c.head_dim;
-  BackArgs a{rope_args(plan, false), pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens, {}};
+  BackArgs a{rope_args(plan, false), {pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens}, {}};
   JoinArgs join{};
   int64_t bytes = 0;
   for (int i = 0; i < 2; ++i) {
     if (!have[i]) continue;
     BackSide& s = a.side[i];
-    s.x = rows_of(i == 0 ? rows->q : rows->k);
-    s.dz = rows_of(i == 0 ? rows->dq_out : rows->dk_out);
-    s.dx = rows_of(i == 0 ? rows->dq : rows->dk);
+    s.x = rope_rows(i == 0 ? rows->q : rows->k);
+    s.dz = rope_rows(i == 0 ? rows->dq_out : rows->dk_out);
+    s.dx = rope_rows(i == 0 ? rows->dq : rows->dk);
     s.w = i == 0 ? wq : wk;
     s.heads = i == 0 ? c.heads : c.kv_heads;
-    s.heads_log2 = heads_log2(i == 0 ? rows->q : rows->k, s.heads, per_wave);
-    const int by_head = 1 << s.heads_log2, all_steps = (s.heads + by_head - 1) / by_head;
-    const int64_t wavefronts = ((int64_t)a.total * by_head + per_wave - 1) / per_wave;
-    s.steps = (int)std::min<int64_t>(all_steps, std::max<int64_t>(1, wavefronts * all_steps / 8192));
-    s.groups = (all_steps + s.steps - 1) / s.steps;
-    s.tiles = (uint32_t)((wavefronts + 3) / 4);
+    const RopeShare share = rope_share(i == 0 ? rows->q : rows->k, s.heads, c.head_dim, a.tokens.total);
+    s.heads_log2 = share.heads_log2, s.steps = share.steps, s.groups = share.groups, s.tiles = share.tiles;
     s.workgroups = nothing ? 0 : (uint32_t)std::min<int64_t>(RF2_ROPE_PARTS, (int64_t)s.tiles * s.groups);
     float* const sums = (float*)workspace + (size_t)i * RF2_ROPE_PARTS * c.head_dim;
     s.sums = s.workgroups == 1 ? dw[i] : sums;
     if (s.workgroups != 1) join.sums[i] = sums, join.dw[i] = dw[i], join.lines[i] = s.workgroups;
-    bytes += (int64_t)a.total * s.heads * c.head_dim * 6;
+    bytes += (int64_t)a.tokens.total * s.heads * c.head_dim * 6;
   }
   const dim3 grid(a.side[0].workgroups + a.side[1].workgroups);
   if (!nothing) {
-    const int rc = for_types(c, [&](auto type, auto d, auto halves) {
-      if (bytes <= KEEP) backward_kernel<decltype(type), d(), halves(), true><<<grid, 256, 0, st>>>(a);
+    const int rc = rope_for_types(c, [&](auto type, auto d, auto halves) {
+      if (bytes <= ROPE_KEEP) backward_kernel<decltype(type), d(), halves(), true><<<grid, 256, 0, st>>>(a);
       else backward_kernel<decltype(type), d(), halves(), false><<<grid, 256, 0, st>>>(a);
     });
     if (rc) return rc;

@@ -83,6 +83,8 @@ SIGNATURES = {
     "rf2_rope_plan_info": (C.c_int, [C.c_void_p, C.POINTER(rf2_rope_info)]),
     "rf2_rope_apply": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 3),
     "rf2_rope_backward": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64] + [C.c_void_p] * 6),
+    "rf2_permute_rope": (C.c_int, [C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 10),
+    "rf2_paged_store_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p, C.c_int64] * 3 + [C.c_void_p] * 8 + [C.c_int64, C.c_void_p]),
     "rf2_measure_peaks": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_void_p]),
     "rf2_measure_sustained_mfma": (C.c_int, [C.c_double, C.POINTER(C.c_double), C.c_void_p]),
     "rf2_probe_xcd_mapping": (C.c_int, [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_void_p]),
@@ -225,6 +227,19 @@ class Plan:
         _check(lib().rf2_permute(self._h, _ptr(q), _ptr(k), _ptr(v), _ptr(qp), _ptr(kp), _ptr(vp), _ptr(qbar),
                                  _ptr(kbar), _stream(stream)), "rf2_permute")
 
+    def rf2_permute_rope(self, rope, q, k, v, pos, qp, kp, vp, qbar=None, kbar=None, wq=None, wk=None, wq_text=None, wk_text=None, stream=None):
+        """rf2_permute of q and k normalised and rotated by a RopePlan; pos is [N, axes] or [batch, N, axes], text tokens behind the grid's."""
+        c, i, dev, bf, f32 = self.cfg, self.info, rope.device, torch.bfloat16, torch.float32
+        at, step = rope._pos(pos, c.batch, i.N)
+        row = c.batch * c.heads * c.head_dim
+        _check(lib().rf2_permute_rope(
+            self._h, rope._h, _arg(q, "q", bf, row * i.N, dev), _arg(k, "k", bf, row * i.N, dev), _arg(v, "v", bf, row * i.N, dev), at, step,
+            rope._weight(wq, "wq"), rope._weight(wk, "wk"), None if wq_text is None else rope._weight(wq_text, "wq_text"),
+            None if wk_text is None else rope._weight(wk_text, "wk_text"), _arg(qp, "qp", bf, row * i.N_pad, dev),
+            _arg(kp, "kp", bf, row * i.N_pad_k, dev), _arg(vp, "vp", bf, row * i.N_pad_k, dev),
+            None if qbar is None else _arg(qbar, "qbar", f32, row * i.n_blocks, dev),
+            None if kbar is None else _arg(kbar, "kbar", f32, row * i.n_blocks_k, dev), _stream(stream)), "rf2_permute_rope")
+
     def rf2_predict_mask(self, qbar, kbar, blk_idx, blk_cnt, mask_dense=None, scores=None, workspace=None,
                          stream=None):
         _check(lib().rf2_predict_mask(self._h, _ptr(qbar), _ptr(kbar), _ptr(blk_idx), _ptr(blk_cnt),
@@ -243,10 +258,14 @@ class Plan:
     def rf2_unpermute(self, op, o, stream=None):
         _check(lib().rf2_unpermute(self._h, _ptr(op), _ptr(o), _stream(stream)), "rf2_unpermute")
 
-    def layer_fused(self, q, k, v, buf, stream=None):
-        """The whole layer with the inverse permutation fused into the attention epilogue; returns buf['o']."""
+    def layer_fused(self, q, k, v, buf, stream=None, rope=None, pos=None, weights=()):
+        """The whole layer with the inverse permutation fused into the attention epilogue; returns buf['o'].  With a RopePlan, and pos and
+        weights (wq, wk, wq_text, wk_text: as many as there are) as rf2_permute_rope takes them, q and k are raw projections."""
         stream = torch.cuda.current_stream() if stream is None else stream
-        self.rf2_permute(q, k, v, buf["qp"], buf["kp"], buf["vp"], buf["qbar"], buf["kbar"], stream)
+        if rope is None:
+            self.rf2_permute(q, k, v, buf["qp"], buf["kp"], buf["vp"], buf["qbar"], buf["kbar"], stream)
+        else:
+            self.rf2_permute_rope(rope, q, k, v, pos, buf["qp"], buf["kp"], buf["vp"], buf["qbar"], buf["kbar"], *weights, stream=stream)
         self.rf2_predict_mask(buf["qbar"], buf["kbar"], buf["blk_idx"], buf["blk_cnt"], buf.get("mask_dense"),
                               buf.get("scores"), None, stream)
         self.rf2_block_sparse_attn_unpermuted(buf["qp"], buf["kp"], buf["vp"], buf["blk_idx"], buf["blk_cnt"],
@@ -387,6 +406,22 @@ class PagedPlan:
             self._h, n_tokens, *_rows(k, "k", self.dtype, shape, dev), *_rows(v, "v", self.dtype, shape, dev),
             _arg(slots, "slots", torch.int32, n_tokens, dev), _arg(k_cache, "k_cache", self.dtype, size, dev),
             _arg(v_cache, "v_cache", self.dtype, size, dev), self._stream(stream)), "rf2_paged_store")
+
+    def rf2_paged_store_rope(self, rope, q, k, v, pos, slots, k_cache, v_cache, q_out, wq=None, wk=None, cu_new=None, stream=None):
+        """rf2_paged_store of k normalised and rotated by a RopePlan, and q the same into q_out (which may be q); with cu_new, rows of q_out
+        behind the last new token stay as they are."""
+        c, dev, size = self.cfg, self.device, self.info.cache_elements
+        n_tokens = slots.numel()
+        shape, q_shape = (n_tokens, c.kv_heads, c.head_dim), (n_tokens, c.heads, c.head_dim)
+        if cu_new is not None and cu_new.numel() < 1:
+            raise ValueError("cu_new: expected one element at least")
+        _check(lib().rf2_paged_store_rope(
+            self._h, rope._h, n_tokens, *_rows(q, "q", self.dtype, q_shape, dev), *_rows(k, "k", self.dtype, shape, dev),
+            *_rows(v, "v", self.dtype, shape, dev), rope._pos(pos, 1, n_tokens)[0], rope._weight(wq, "wq"), rope._weight(wk, "wk"),
+            _arg(slots, "slots", torch.int32, n_tokens, dev),
+            None if cu_new is None else _arg(cu_new, "cu_new", torch.int32, cu_new.numel(), dev) + 4 * (cu_new.numel() - 1),
+            _arg(k_cache, "k_cache", self.dtype, size, dev), _arg(v_cache, "v_cache", self.dtype, size, dev),
+            *_rows(q_out, "q_out", self.dtype, q_shape, dev), self._stream(stream)), "rf2_paged_store_rope")
 
     def rf2_paged_attn(self, q, k_cache, v_cache, block_table, seq_len, cu_new, workspace, o, lse=None, stream=None):
         c, dev, size, i32 = self.cfg, self.device, self.info.cache_elements, torch.int32
