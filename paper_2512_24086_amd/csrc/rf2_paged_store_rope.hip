@@ -74,12 +74,12 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
   if (run >= 1u << 20) return RF2_ERR_UNSUPPORTED;           // (a grid has less than 2^32 threads, half of them for Q)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;
-  const RopeSide side = rope_side({q, 0, n_tokens > 1 ? q_stride : q_row, c.head_dim}, {q_out, 0, n_tokens > 1 ? q_out_stride : q_row, c.head_dim}, wq, c.heads,
-                                  c.head_dim, (uint32_t)n_tokens);
+  const rf2_rows q_rows{q, 0, n_tokens > 1 ? q_stride : q_row, c.head_dim}, out_rows{q_out, 0, n_tokens > 1 ? q_out_stride : q_row, c.head_dim};
+  const RopeSide side{rope_rows(q_rows), rope_rows(out_rows), wq, rope_share(q_rows, c.heads, r, (uint32_t)n_tokens)};
   const StoreRopeArgs a{(const uint16_t*)k, (const uint16_t*)v, k_stride, v_stride, slots, n_tokens, __builtin_ctz((unsigned)c.page), c.kv_heads,
                         (int64_t)c.n_pages * c.page, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
                         r.norm == RF2_NORM_RMS, n_live, side};
-  const dim3 grid(8 * run + side.workgroups);
+  const dim3 grid(8 * run + rope_workgroups(side.share));
   const bool keep = (int64_t)n_tokens * q_row * 4 <= ROPE_KEEP;
   hipStream_t st = (hipStream_t)stream;
   return rope_for_types(r, [&](auto type, auto d, auto halves) {

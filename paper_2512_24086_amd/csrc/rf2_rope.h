@@ -5,17 +5,17 @@
 
 #include "rf2_internal.h"
 
-// A pair of channels: turns per unit of its axis' position.
-struct rf2_rope_pair {
-  double turns;
-  int32_t axis, unused;
+// Of each pair of channels, turns per unit of its axis' position, and the axis: a lane reads those of its pairs in a few wide loads.
+struct rf2_rope_table {
+  double turns[64];
+  uint8_t axis[64];
 };
 
 struct rf2_rope_plan {
   rf2_rope_config cfg;
   rf2_rope_info info;
   int device;
-  rf2_rope_pair* d_pairs;  // device, 64 of them, and 64 that turn the other way
+  rf2_rope_table* d_table;  // device, two: the second one turns the other way
 };
 
 // The sums of the weights' gradients: so many workgroups for each of Q and K at most, head_dim numbers of 32 bits from each.
@@ -44,12 +44,12 @@ namespace {
 
 // What the kernels read of a plan.
 struct RopeArgs {
-  const rf2_rope_pair* pairs;
+  const rf2_rope_table* table;
   int axes, weights_f32;
   float eps;
 };
 inline RopeArgs rope_args(const rf2_rope_plan* p, bool inverse = false) {
-  return {p->d_pairs + (inverse ? 64 : 0), p->cfg.axes, p->cfg.weight_dtype == RF2_DTYPE_F32, p->cfg.eps};
+  return {p->d_table + (inverse ? 1 : 0), p->cfg.axes, p->cfg.weight_dtype == RF2_DTYPE_F32, p->cfg.eps};
 }
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -125,25 +125,36 @@ __device__ __forceinline__ void rope_partners(const float (&x)[8], float (&y)[8]
 template <int D, bool HALVES>
 __device__ __forceinline__ void rope_angles(const RopeArgs& a, const int32_t* __restrict__ pos, int c, float (&cs)[8], float (&sn)[8]) {
 #pragma clang fp contract(off)                  // (the kernels that share this are to give the same bits)
-  constexpr int N = HALVES ? 8 : 4;
-  int p[4] = {0, 0, 0, 0};
+  // (HALVES: the lanes of a pair's two channels have the same eight pairs, of which each works out four)
+  const bool upper = HALVES && c >= D / 16;
+  const int pair = HALVES ? 8 * c - (upper ? D / 2 - 4 : 0) : 4 * c;
+  // (without axes nothing turns, whatever is read here)
+  const int32_t* const at = a.axes > 0 ? pos : reinterpret_cast<const int32_t*>(a.table);
+  const int p0 = at[0], p1 = at[a.axes > 1 ? 1 : 0], p2 = at[a.axes > 2 ? 2 : 0], p3 = at[a.axes > 3 ? 3 : 0];
+  const double2 t01 = reinterpret_cast<const double2*>(a.table->turns + pair)[0], t23 = reinterpret_cast<const double2*>(a.table->turns + pair)[1];
+  const double turns[4] = {t01.x, t01.y, t23.x, t23.y};
+  const uint32_t axes = *reinterpret_cast<const uint32_t*>(a.table->axis + pair);
+  float co[4], si[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < a.axes) p[i] = pos[i];
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t low = axes & 1u << 8 * i, high = axes & 2u << 8 * i;
+    const int even = high ? p2 : p0, odd = high ? p3 : p1;
+    const double turn = (double)(low ? odd : even) * turns[i];
+    const float part = (float)(turn - __builtin_rint(turn));
+    co[i] = __builtin_amdgcn_cosf(part), si[i] = __builtin_amdgcn_sinf(part);
+  }
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const rf2_rope_pair pair = a.pairs[HALVES ? (8 * c + i) % (D / 2) : 4 * c + i];
-    const int at = pair.axis == 0 ? p[0] : pair.axis == 1 ? p[1] : pair.axis == 2 ? p[2] : p[3];
-    const double turns = (double)at * pair.turns;
-    const float part = (float)(turns - __builtin_rint(turns));
-    const float co = __builtin_amdgcn_cosf(part), si = __builtin_amdgcn_sinf(part);
+  for (int i = 0; i < 4; ++i) {
     if constexpr (HALVES) {
-      cs[i] = co;
-      sn[i] = c < D / 16 ? -si : si;
+      const float other_co = rope_other_half<D>(co[i]), other_si = rope_other_half<D>(si[i]);
+      cs[i] = upper ? other_co : co[i];
+      cs[4 + i] = upper ? co[i] : other_co;
+      sn[i] = upper ? other_si : -si[i];
+      sn[4 + i] = upper ? si[i] : -other_si;
     } else {
-      cs[2 * i] = cs[2 * i + 1] = co;
-      sn[2 * i] = -si;
-      sn[2 * i + 1] = si;
+      cs[2 * i] = cs[2 * i + 1] = co[i];
+      sn[2 * i] = -si[i];
+      sn[2 * i + 1] = si[i];
     }
   }
 }
@@ -220,15 +231,27 @@ struct RopeRows {
   int64_t batch, token, head;
 };
 
-// Rows of Q or of K, in and out, and how wavefronts share them.
-struct RopeSide {
-  RopeRows x, z;                 // in, out
-  const void* w;
-  int heads, heads_log2;     // heads; log2 of the rows of a wavefront that are neighbouring heads
-  int steps, groups;         // of heads a wavefront goes through, and wavefronts that share a token's heads
-  uint32_t workgroups;
+// How wavefronts share rows: one takes 2^heads_log2 neighbouring heads (they divide all) of as many tokens as that leaves rows for, and goes on
+// through the heads, `steps` times; `groups` of them have the same tokens.  Workgroups that start one after the other have neighbouring
+// groups of the same four wavefronts' tokens, a tile, or neighbouring tiles.
+struct RopeShare {
+  int heads, heads_log2, steps, groups;
+  uint32_t tiles, fast, inverse;     // fast: groups or tiles; inverse: (2^32 - 1) / fast
 };
-
+// Rows of Q or of K, in and out.
+struct RopeSide {
+  RopeRows x, z;
+  const void* w;
+  RopeShare share;
+};
+struct RopeUnit {
+  uint32_t tile, group;
+};
+__device__ __forceinline__ RopeUnit rope_unit(const RopeShare& s, uint32_t id) {
+  uint32_t slow = __umulhi(id, s.inverse), fast = id - slow * s.fast;      // id / fast, or one less (a division: 525 us in place of 512 for 75,600 tokens of 40 + 40 heads)
+  if (fast >= s.fast) ++slow, fast -= s.fast;
+  return s.fast == (uint32_t)s.groups ? RopeUnit{slow, fast} : RopeUnit{fast, slow};
+}
 // Tokens and their positions.
 struct RopeTokens {
   const int32_t* pos;
@@ -256,43 +279,41 @@ __device__ __forceinline__ RopeToken rope_token(uint32_t m, uint32_t tokens, uin
   return {b, m - b * tokens};
 }
 
-// What a workgroup of 256 threads does of a side: 4 * (64 / (d / 8)) rows at a time.
+// What workgroup `id` of 256 threads does of a side: a tile of tokens through a group of heads.
 template <class T, int D, bool HALVES, bool NORM, bool KEEP>
 __device__ __forceinline__ void rope_apply_rows(const RopeArgs& a, const RopeTokens& t, const RopeSide& s, uint32_t id) {
   constexpr int CH = D / 8, R = 64 / CH, U = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
-  const int by_head = 1 << s.heads_log2, by_token = R >> s.heads_log2;
-  const uint32_t tile = id / (uint32_t)s.groups, group = id - tile * (uint32_t)s.groups;
-  const uint32_t m = (tile * 4 + wave) * by_token + (g >> s.heads_log2);
+  const RopeUnit unit = rope_unit(s.share, id);
+  const int log2 = s.share.heads_log2, by_token = R >> log2;
+  const uint32_t m = (unit.tile * 4 + wave) * by_token + (g >> log2);
   if (m >= t.total) return;
   const RopeToken token = rope_token(m, t.tokens, t.total);
-  int h = group * s.steps * by_head + (g & (by_head - 1));
-  const int end = min(s.heads, (int)(group + 1) * s.steps * by_head);
+  const int first = unit.group * s.share.steps, end = min(s.share.heads >> log2, first + s.share.steps);
+  const int h = (first << log2) + (g & ((1 << log2) - 1));
   const uint16_t* from = s.x.at + token.b * s.x.batch + token.n * s.x.token + h * s.x.head + 8 * c;
   uint16_t* to = const_cast<uint16_t*>(s.z.at) + token.b * s.z.batch + token.n * s.z.token + h * s.z.head + 8 * c;
-  const int64_t from_step = s.x.head * by_head, to_step = s.z.head * by_head;
+  const int64_t from_step = s.x.head << log2, to_step = s.z.head << log2;
+  rope_u32x4 v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (first + u < end) v[u] = rope_load<false>(from + u * from_step);
   float A[8], B[8];
-  bool first = true;
-  while (h < end) {
-    rope_u32x4 v[U];
+  rope_factors<T, D, HALVES, NORM>(a, t.pos + token.b * t.pos_batch + (int64_t)token.n * a.axes, s.w, c, A, B);
+  for (int step = first; step < end; step += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (h + u * by_head < end) v[u] = rope_load<KEEP>(from + u * from_step);
-    if (first) {
-      rope_factors<T, D, HALVES, NORM>(a, t.pos + token.b * t.pos_batch + (int64_t)token.n * a.axes, s.w, c, A, B);
-      first = false;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (h + u * by_head < end) {
+      if (step + u < end) {
         float x[8];
         T::unpack(v[u], x);
         rope_row<D, HALVES, NORM>(a, A, B, x);
         rope_store<KEEP>(to + u * to_step, T::pack(x));
       }
-    h += U * by_head;
     from += U * from_step;
     to += U * to_step;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (step + U + u < end) v[u] = rope_load<false>(from + u * from_step);
   }
 }
 
@@ -300,31 +321,42 @@ __device__ __forceinline__ void rope_apply_rows(const RopeArgs& a, const RopeTok
 
 inline RopeRows rope_rows(const rf2_rows& r) { return {(const uint16_t*)r.at, r.batch, r.token, r.head}; }
 
-// How many rows of a wavefront are neighbouring heads of a token (log2): all where heads lie side by side and there are as many.
+// How many rows of a wavefront are neighbouring heads of a token (log2): where heads lie side by side, as many as divide all of them.
 inline int rope_heads_log2(const rf2_rows& r, int heads, int rows) {
   if (r.head >= r.token) return 0;
   int log2 = 0;
-  while (2 << log2 <= rows && 2 << log2 <= heads) ++log2;
+  while (2 << log2 <= rows && heads % (2 << log2) == 0) ++log2;
   return log2;
 }
 
-// How the wavefronts of a launch share rows: `wavefronts` of tokens, `groups` of heads for each.
-struct RopeShare {
-  int heads_log2, steps, groups;
-  uint32_t tiles;            // of four wavefronts' tokens
-};
-inline RopeShare rope_share(const rf2_rows& x, int heads, int head_dim, uint32_t tokens) {
-  const int rows = 512 / head_dim, log2 = rope_heads_log2(x, heads, rows), by_head = 1 << log2, all_steps = (heads + by_head - 1) / by_head;
-  const int64_t wavefronts = ((int64_t)tokens * by_head + rows - 1) / rows;
-  const int steps = (int)std::min<int64_t>(all_steps, std::max<int64_t>(1, wavefronts * all_steps / 8192));
-  return {log2, steps, (all_steps + steps - 1) / steps, (uint32_t)((wavefronts + 3) / 4)};
+// The share of each wavefront.  Angles are worked out once for all its steps (HALVES costs twice the exchange), loads of four steps are on their way
+// together, and what is read at a time should lie close together.  Measured (us, steps of a wavefront):
+//   heads side by side, 75,600 tokens x 40 + 40 heads      4 of 10: 511   5: 511   all: 541; groups slowest 557, 547, 541
+//     64 channels, 32,760 tokens x 40 + 40                 4 of 5: 119   all: 109;  HALVES, 20,000 x 32 + 8   4 of 8: 78   all: 73
+//   tokens side by side, 75,600 x 40 + 40                  1: 639   2: 507   3: 515   4: 526   8: 537   all: 586 (a copy of as much: 500)
+//     HALVES, 32,760 x 40 + 40                             2: 252   4: 234   5: 224   8: 231   all: 234
+//     4,096 x 12 + 12                                      2: 11.3  4: 9.4   8: 11.1;   1,000 x 40 + 40   2: 9.8   4: 8.2   all: 8.1
+// With few rows a wavefront takes fewer, so that there are 2,048.
+inline RopeShare rope_share(const rf2_rows& x, int heads, const rf2_rope_config& c, uint32_t tokens) {
+  if (!x.at) return {heads, 0, 1, 0, 0, 1, 0};
+  const int rows = 512 / c.head_dim, log2 = rope_heads_log2(x, heads, rows), all_steps = heads >> log2;
+  const int64_t wavefronts = (((int64_t)tokens << log2) + rows - 1) / rows, work = wavefronts * all_steps;
+  const bool halves = c.pairing == RF2_ROPE_HALVES, along_tokens = x.token < x.head;
+  const int most = along_tokens ? (halves ? 5 : work > 150000 ? 2 : 4) : halves ? 10 : 5;
+  const int parts = (all_steps + most - 1) / most, even = along_tokens ? most : (all_steps + parts - 1) / parts;
+  int steps = (int)std::min<int64_t>(std::min(even, all_steps), std::max<int64_t>(1, work / 2048));
+  // (a grid has less than 2^32 threads: at most 2^22 tiles, and 2^23 workgroups of a side)
+  while (steps < all_steps && (wavefronts + 3) / 4 * ((all_steps + steps - 1) / steps) >= (int64_t)1 << 22) steps = std::min(all_steps, 2 * steps);
+  const int groups = (all_steps + steps - 1) / steps;
+  const uint32_t tiles = (uint32_t)((wavefronts + 3) / 4), fast = along_tokens ? tiles : (uint32_t)groups;
+  return {heads, log2, steps, groups, tiles, fast, UINT32_MAX / fast};
 }
-inline RopeSide rope_side(const rf2_rows& x, const rf2_rows& z, const void* w, int heads, int head_dim, uint32_t tokens) {
-  const RopeShare s = rope_share(x, heads, head_dim, tokens);
-  return {rope_rows(x), rope_rows(z), w, heads, s.heads_log2, s.steps, s.groups, x.at ? s.tiles * (uint32_t)s.groups : 0};
-}
+inline uint32_t rope_workgroups(const RopeShare& s) { return s.tiles * (uint32_t)s.groups; }
 
-constexpr int64_t ROPE_KEEP = (int64_t)160 << 20;
+// Rows are read once and left to what reads them next.  Past the caches is the faster way (4,096 tokens, 10 + 10 heads, 42 MB: 7.5 us for 9.9,
+// 134 MB: 23.2 for 25.1), but rows that the L2s hold are there for the next kernel (17 MB, with rf2_permute behind: 15.0 us for 13.1; 42 MB: 22.1 for
+// 21.3).  So stores are kept up to 32 MiB, in bytes read and written.
+constexpr int64_t ROPE_KEEP = (int64_t)32 << 20;
 
 template <class F>
 int rope_for_types(const rf2_rope_config& c, F f) {

@@ -15,8 +15,9 @@ struct ApplyArgs {
 
 template <class T, int D, bool HALVES, bool NORM, bool KEEP>
 __global__ void __launch_bounds__(256) apply_kernel(ApplyArgs a) {
-  const bool second = blockIdx.x >= a.side[0].workgroups;
-  rope_apply_rows<T, D, HALVES, NORM, KEEP>(a.rope, a.tokens, a.side[second ? 1 : 0], blockIdx.x - (second ? a.side[0].workgroups : 0));
+  const uint32_t of_q = a.side[0].share.tiles * (uint32_t)a.side[0].share.groups;
+  const bool second = blockIdx.x >= of_q;
+  rope_apply_rows<T, D, HALVES, NORM, KEEP>(a.rope, a.tokens, a.side[second ? 1 : 0], blockIdx.x - (second ? of_q : 0));
 }
 
 // ---- gradients --------------------------------------------------------------------------------------------------
@@ -25,8 +26,8 @@ struct BackSide {
   RopeRows x, dz, dx;
   const void* w;
   float* sums;               // of the workgroups, [workgroups][d]; the gradient itself where there is one workgroup
-  int heads, heads_log2, steps, groups;
-  uint32_t workgroups, tiles;
+  RopeShare share;
+  uint32_t workgroups;
 };
 struct BackArgs {
   RopeArgs rope;
@@ -44,32 +45,33 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
   const BackSide& s = a.side[second ? 1 : 0];
   const uint32_t id = blockIdx.x - (second ? a.side[0].workgroups : 0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
-  const int by_head = 1 << s.heads_log2, by_token = R >> s.heads_log2;
+  const int log2 = s.share.heads_log2, by_token = R >> log2;
+  const int64_t x_step = s.x.head << log2, dz_step = s.dz.head << log2, dx_step = s.dx.head << log2;
   float w[8];
   rope_weights<T>(a.rope, s.w, c, w);
   double total[8] = {};
-  for (uint32_t unit = id; unit < s.tiles * (uint32_t)s.groups; unit += s.workgroups) {
-    const uint32_t tile = unit / (uint32_t)s.groups, group = unit - tile * (uint32_t)s.groups;
-    const uint32_t m = (tile * 4 + wave) * by_token + (g >> s.heads_log2);
-    int h = group * s.steps * by_head + (g & (by_head - 1));
-    const int end = m < a.tokens.total ? min(s.heads, (int)(group + 1) * s.steps * by_head) : 0;
+  for (uint32_t i = id; i < s.share.tiles * (uint32_t)s.share.groups; i += s.workgroups) {
+    const RopeUnit unit = rope_unit(s.share, i);
+    const uint32_t m = (unit.tile * 4 + wave) * by_token + (g >> log2);
+    const int first = unit.group * s.share.steps, end = m < a.tokens.total ? min(s.share.heads >> log2, first + s.share.steps) : 0;
+    const int h = (first << log2) + (g & ((1 << log2) - 1));
     const RopeToken t = rope_token(min(m, a.tokens.total - 1), a.tokens.tokens, a.tokens.total);
     const uint16_t* x_at = s.x.at + t.b * s.x.batch + t.n * s.x.token + h * s.x.head + 8 * c;
     const uint16_t* dz_at = s.dz.at + t.b * s.dz.batch + t.n * s.dz.token + h * s.dz.head + 8 * c;
     uint16_t* dx_at = const_cast<uint16_t*>(s.dx.at) + t.b * s.dx.batch + t.n * s.dx.token + h * s.dx.head + 8 * c;
+    rope_u32x4 vx[U], vz[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (first + u < end) {
+        vx[u] = rope_load<KEEP>(x_at + u * x_step);
+        vz[u] = rope_load<KEEP>(dz_at + u * dz_step);
+      }
     float cs[8], sn[8], sum[8] = {};
     rope_angles<D, HALVES>(a.rope, a.tokens.pos + t.b * a.tokens.pos_batch + (int64_t)t.n * a.rope.axes, c, cs, sn);
-    while (h < end) {
-      rope_u32x4 vx[U], vz[U];
+    for (int step = first; step < end; step += U) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (h + u * by_head < end) {
-          vx[u] = rope_load<KEEP>(x_at + u * by_head * s.x.head);
-          vz[u] = rope_load<KEEP>(dz_at + u * by_head * s.dz.head);
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (h + u * by_head < end) {
+        if (step + u < end) {
           float x[8], z[8], y[8];
           T::unpack(vx[u], x);
           T::unpack(vz[u], z);
@@ -86,12 +88,17 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
           m = rope_row_sum<D>(m) * (1.f / D);
 #pragma unroll
           for (int e = 0; e < 8; ++e) z[e] = r * fmaf(-x[e], m, z[e]);
-          rope_store<KEEP>(dx_at + u * by_head * s.dx.head, T::pack(z));
+          rope_store<KEEP>(dx_at + u * dx_step, T::pack(z));
         }
-      h += U * by_head;
-      x_at += U * by_head * s.x.head;
-      dz_at += U * by_head * s.dz.head;
-      dx_at += U * by_head * s.dx.head;
+      x_at += U * x_step;
+      dz_at += U * dz_step;
+      dx_at += U * dx_step;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (step + U + u < end) {
+          vx[u] = rope_load<KEEP>(x_at + u * x_step);
+          vz[u] = rope_load<KEEP>(dz_at + u * dz_step);
+        }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) total[e] += (double)sum[e];
@@ -186,10 +193,10 @@ int launch_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, con
   for (int i = 0; i < 2; ++i) {
     const rf2_rows& x = i == 0 ? q : k;
     const int heads = i == 0 ? c.heads : c.kv_heads;
-    a.side[i] = rope_side(x, i == 0 ? q_out : k_out, i == 0 ? wq : wk, heads, c.head_dim, a.tokens.total);
+    a.side[i] = {rope_rows(x), rope_rows(i == 0 ? q_out : k_out), i == 0 ? wq : wk, rope_share(x, heads, c, a.tokens.total)};
     if (x.at) bytes += (int64_t)a.tokens.total * heads * c.head_dim * 4;
   }
-  const dim3 grid(a.side[0].workgroups + a.side[1].workgroups);
+  const dim3 grid(rope_workgroups(a.side[0].share) + rope_workgroups(a.side[1].share));
   return rope_for_types(c, [&](auto type, auto d, auto halves) {
     const auto launch = [&](auto with_norm, auto keep) {
       apply_kernel<decltype(type), d(), halves(), with_norm(), keep()><<<grid, 256, 0, st>>>(a);
@@ -251,14 +258,13 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     s.dz = rope_rows(i == 0 ? rows->dq_out : rows->dk_out);
     s.dx = rope_rows(i == 0 ? rows->dq : rows->dk);
     s.w = i == 0 ? wq : wk;
-    s.heads = i == 0 ? c.heads : c.kv_heads;
-    const RopeShare share = rope_share(i == 0 ? rows->q : rows->k, s.heads, c.head_dim, a.tokens.total);
-    s.heads_log2 = share.heads_log2, s.steps = share.steps, s.groups = share.groups, s.tiles = share.tiles;
-    s.workgroups = nothing ? 0 : (uint32_t)std::min<int64_t>(RF2_ROPE_PARTS, (int64_t)s.tiles * s.groups);
+    const int heads = i == 0 ? c.heads : c.kv_heads;
+    s.share = rope_share(i == 0 ? rows->q : rows->k, heads, c, a.tokens.total);
+    s.workgroups = nothing ? 0 : (uint32_t)std::min<int64_t>(RF2_ROPE_PARTS, rope_workgroups(s.share));
     float* const sums = (float*)workspace + (size_t)i * RF2_ROPE_PARTS * c.head_dim;
     s.sums = s.workgroups == 1 ? dw[i] : sums;
     if (s.workgroups != 1) join.sums[i] = sums, join.dw[i] = dw[i], join.lines[i] = s.workgroups;
-    bytes += (int64_t)a.tokens.total * s.heads * c.head_dim * 6;
+    bytes += (int64_t)a.tokens.total * heads * c.head_dim * 6;
   }
   const dim3 grid(a.side[0].workgroups + a.side[1].workgroups);
   if (!nothing) {

@@ -29,20 +29,21 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
 
   // turns per position of each pair; pairs behind the last axis do not turn
   constexpr double TWO_PI = 6.283185307179586476925286766559;
-  rf2_rope_pair pairs[128] = {};
+  rf2_rope_table tables[2] = {};
   int i = 0;
   for (int a = 0; a < c.axes; ++a)
     for (int j = 0; j < c.axis_dim[a] / 2; ++j, ++i) {
       const double f = inv_freq_host ? inv_freq_host[i] : std::pow(c.theta, -2.0 * j / c.axis_dim[a]);
       if (!(std::fabs(f) <= 65536.0)) return RF2_ERR_INVALID_ARG;
-      pairs[i] = {f / TWO_PI, a, 0};
-      pairs[64 + i] = {-f / TWO_PI, a, 0};
+      tables[0].turns[i] = f / TWO_PI;
+      tables[1].turns[i] = -f / TWO_PI;
+      tables[0].axis[i] = tables[1].axis[i] = (uint8_t)a;
     }
 
   rf2_rope_plan* p = new (std::nothrow) rf2_rope_plan();
   if (!p) return RF2_ERR_ALLOC;
   p->cfg = c;
-  p->d_pairs = nullptr;
+  p->d_table = nullptr;
   p->info.workspace_bytes = c.norm == RF2_NORM_RMS ? rf2_rope_workspace(c.head_dim) : 0;
   int n_dev = 0;
   if (hipGetDeviceCount(&n_dev) != hipSuccess || n_dev == 0) {
@@ -52,8 +53,8 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
     return RF2_OK;
   }
   hipError_t e = hipGetDevice(&p->device);
-  if (e == hipSuccess) e = hipMalloc((void**)&p->d_pairs, sizeof pairs);
-  if (e == hipSuccess) e = hipMemcpy(p->d_pairs, pairs, sizeof pairs, hipMemcpyHostToDevice);
+  if (e == hipSuccess) e = hipMalloc((void**)&p->d_table, sizeof tables);
+  if (e == hipSuccess) e = hipMemcpy(p->d_table, tables, sizeof tables, hipMemcpyHostToDevice);
   if (e != hipSuccess) {
     const int rc = e == hipErrorOutOfMemory ? ((void)hipGetLastError(), (int)RF2_ERR_ALLOC) : rf2_note_hip_error(e);
     rf2_rope_plan_destroy(p);
@@ -65,7 +66,7 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
 
 int rf2_rope_plan_destroy(rf2_rope_plan* plan) {
   if (!plan) return RF2_OK;
-  if (plan->d_pairs) (void)hipFree(plan->d_pairs);
+  if (plan->d_table) (void)hipFree(plan->d_table);
   delete plan;
   return RF2_OK;
 }
