@@ -27,14 +27,15 @@ template <class T, int D, bool HALVES, bool KEEP>
 __global__ void __launch_bounds__(256) store_rope_kernel(StoreRopeArgs a) {
   if (blockIdx.x < 8 * a.run) {
     const auto prepare = [&](const u32x4& row, int64_t token, int c) {
-      const int32_t* const pos = a.pos + token * a.rope.axes;
+      const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
+      const RopePlace place = rope_place(a.rope, angles, a.pos + token * a.rope.axes);
       float A[8], B[8], x[8];
       T::unpack(row, x);
       if (a.norm) {
-        rope_factors<T, D, HALVES, true>(a.rope, pos, a.wk, c, A, B);
+        rope_factors<T, D, HALVES, true>(a.rope, angles, place, a.wk, c, A, B);
         rope_row<D, HALVES, true>(a.rope, A, B, x);
       } else {
-        rope_factors<T, D, HALVES, false>(a.rope, pos, nullptr, c, A, B);
+        rope_factors<T, D, HALVES, false>(a.rope, angles, place, nullptr, c, A, B);
         rope_row<D, HALVES, false>(a.rope, A, B, x);
       }
       return T::pack(x);

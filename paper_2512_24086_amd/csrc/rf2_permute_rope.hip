@@ -1,8 +1,11 @@
 // Window permutation and block means of a layer, Q and K normalised and rotated on the way (gfx950).
 //
 // HBM bound, like the permutation by itself: the same bytes are read and written, and a pass over Q and K before it is saved.  A workgroup takes
-// a block of rows through four heads: cosines and sines belong to a token, and the loads of the heads' rows are on their way
-// together.  A wavefront holds eight rows, d / 8 lanes to a row (d = 64) or in two sets of four (d = 128).
+// a block of rows through two heads, a wavefront 64 / (d / 8) rows at a time, d / 8 lanes to a row.  Cosines and sines belong to a token, so both
+// heads have them from one calculation, which is about as much work as a head's rows themselves (one head at a time: 75,600 tokens of 40 heads
+// 826 us, two 806, three 807, four 1,057; rf2_permute by itself 790).  Small layers, which the latency of a block bounds, ask for the
+// rows of the next turn before they work on this one (4,301 tokens of 12 heads 18.7 -> 15.6 us); elsewhere the registers that it takes cost
+// wavefronts (64 channels, 32,760 tokens of 40 heads 191 -> 207).
 #include "rf2_permute_rows.h"
 #include "rf2_rope.h"
 
@@ -19,7 +22,7 @@ struct PermuteRopeArgs {
   uint32_t groups;                   // of heads
 };
 
-constexpr int HEADS = 4;
+constexpr int HEADS = 2;
 
 template <bool KEEP>
 __device__ __forceinline__ rope_u32x4 ld_row(const u16* p) {
@@ -33,12 +36,15 @@ __device__ __forceinline__ void st_row(u16* p, const rope_u32x4& v) {
 }
 
 template <int D>
-using mean_sums = float[4][HEADS][D];
+struct rope_lds {
+  float weights[2][D], sums[4][HEADS][D];        // weights of the grid's tokens, and of the text
+};
 
 // Rows of a block of Q (row by row) or K (operand parts, see rf2.h), HEADS heads from h0 on.
-template <int D, bool IS_K, bool HALVES, bool NORM, int KEEP>
-__device__ __forceinline__ void rope_block(const PermuteRopeArgs& a, int rows, int n_blocks, int last_valid, int blk, int b, int h0, mean_sums<D>& sums) {
-  constexpr int CH = D / 8, SETS = CH / 8;                  // sets of rows of a wavefront
+template <int D, bool IS_K, bool HALVES, bool NORM, int KEEP, bool RAGGED>
+__device__ __forceinline__ void rope_rows_of(const PermuteRopeArgs& a, int rows, int n_blocks, int last_valid, int blk, int b, int h0,
+                                           rope_lds<D>& lds) {
+  constexpr int CH = D / 8, ROWS = 64 / CH;                 // rows of a wavefront
   const PermuteArgs& p = a.p;
   const u16* const x = reinterpret_cast<const u16*>(IS_K ? p.k : p.q) + (int64_t)b * p.st.batch * D;
   u16* const xp = reinterpret_cast<u16*>(IS_K ? p.kp : p.qp);
@@ -46,61 +52,100 @@ __device__ __forceinline__ void rope_block(const PermuteRopeArgs& a, int rows, i
   const int heads = min(HEADS, p.heads - h0);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH, g = lane / CH;
   const int half = rows / 2;
-  float sum[HEADS][8] = {};
-  for (int r0 = 8 * wave; r0 < rows; r0 += 32) {
-    int n[SETS];
-    rope_u32x4 v[SETS][HEADS];
+  const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
+  if constexpr (NORM) {
+    // (a row's lanes turn them into 32 bits, the first those of the grid, the next those of the text)
+    if (threadIdx.x < 2 * CH) {
+      float own[8];
+      rope_weights<RopeBf16>(a.rope, threadIdx.x < CH || !a.w_text[IS_K] ? a.w[IS_K] : a.w_text[IS_K], threadIdx.x % CH, own);
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) n[s] = p.perm[blk * rows + r0 + 4 * s + g];
-#pragma unroll
-    for (int s = 0; s < SETS; ++s)
-#pragma unroll
-      for (int i = 0; i < HEADS; ++i) {
-        v[s][i] = rope_u32x4{0, 0, 0, 0};
-        if (i < heads && n[s] >= 0) v[s][i] = ld_row<KEEP == 2>(x + ((h0 + i) * p.st.head + (int64_t)n[s] * p.st.token) * D + 8 * c);
-      }
-#pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-      const int at = max(n[s], 0);
-      const void* const w = NORM && at >= a.video && a.w_text[IS_K] ? a.w_text[IS_K] : a.w[IS_K];
-      float A[8], B[8];
-      rope_factors<RopeBf16, D, HALVES, NORM>(a.rope, a.pos + b * a.pos_batch + (int64_t)at * a.rope.axes, w, c, A, B);
-      if (n[s] < 0)                                          // rows behind the last are 0, not -0
-#pragma unroll
-        for (int e = 0; e < 8; ++e) A[e] = B[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < HEADS; ++i) {
-        float y[8];
-        RopeBf16::unpack(v[s][i], y);
-        rope_row<D, HALVES, NORM>(a.rope, A, B, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[i][e] += y[e];
-        v[s][i] = RopeBf16::pack(y);
-      }
+      for (int e = 0; e < 8; ++e) lds.weights[threadIdx.x / CH][8 * (threadIdx.x % CH) + e] = own[e];
     }
-    if constexpr (IS_K && SETS == 2) {
-      // The first set's upper chunks against the second's lower ones: a store then covers eight rows of eight chunks, whole lines of 128 bytes.
+    __syncthreads();
+  }
+  float sum[HEADS][8] = {};
+  // Turns of ROWS rows, whose loads are asked for a turn ahead, their places two turns.
+  const int turns = rows / (4 * ROWS);
+  const auto row0 = [&](int turn) { return D == 128 ? 8 * wave + 32 * (turn / 2) + 4 * (turn % 2) : 8 * wave + 32 * turn; };
+  const auto entry = [&](int turn) { return p.perm[blk * rows + row0(min(turn, turns - 1)) + g]; };
+  rope_u32x4 v[HEADS], before[HEADS];
+  RopePlace place;
+  const auto ask = [&](int n) {
+    const int at = RAGGED ? max(n, 0) : n;
+    const u16* const from = x + (h0 * p.st.head + (int64_t)at * p.st.token) * D + 8 * c;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) v[i] = ld_row<KEEP == 2>(from + min(i, heads - 1) * p.st.head * D);
+    place = rope_place(a.rope, angles, a.pos + b * a.pos_batch + (int64_t)at * a.rope.axes);
+    if constexpr (RAGGED) {
 #pragma unroll
       for (int i = 0; i < HEADS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t first = v[0][i][e], second = v[1][i][e];
-          v[0][i][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)first, (int)second, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
-          v[1][i][e] = (uint32_t)__builtin_amdgcn_update_dpp((int)second, (int)first, 0x128, 0xf, 0x3, false);      // and into lanes 0-7
-        }
+        if (n < 0) v[i] = rope_u32x4{0, 0, 0, 0};
     }
+  };
+  constexpr bool AHEAD = KEEP == 2;
+  int n = entry(0), next = entry(1);
+  if constexpr (AHEAD) ask(n);
+#pragma unroll 1
+  for (int turn = 0; turn < turns; ++turn) {
+    if constexpr (!AHEAD) ask(n);
+    float A[8], B[8], own[8], other[8];
+    if constexpr (NORM) {
+      const float* const w = lds.weights[n >= a.video ? 1 : 0];
 #pragma unroll
-    for (int i = 0; i < HEADS; ++i)
-      if (i < heads) {
-        u16* const to = xp + ((int64_t)(b * p.heads + h0 + i) * n_blocks + blk) * rows * D;
+      for (int e = 0; e < 8; ++e) own[e] = w[8 * c + e];
+      if constexpr (HALVES)
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) {
-          int r = r0 + 4 * s + g, chunk = c;
-          if (IS_K && SETS == 2) r = r0 + 4 * (c / 8) + g, chunk = 8 * s + c % 8;
-          const int k_slot = ((r % half) / 32 * CH + chunk) * 64 + r / half * 32 + r % 32;
-          st_row<KEEP >= 1>(to + (IS_K ? k_slot : r * CH + chunk) * 8, v[s][i]);
-        }
+        for (int e = 0; e < 8; ++e) other[e] = w[8 * (c ^ (CH / 2)) + e];
+    }
+    rope_factors<D, HALVES, NORM>(angles, place, own, other, c, A, B);
+    rope_u32x4 now[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) now[i] = v[i];
+    const bool behind = n < 0;
+    n = next;
+    if constexpr (AHEAD) ask(n);
+    next = entry(turn + 2);
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+      float y[8];
+      RopeBf16::unpack(now[i], y);
+      rope_row<D, HALVES, NORM>(a.rope, A, B, y);
+      now[i] = RopeBf16::pack(y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[i][e] += y[e];
+      if constexpr (RAGGED)
+        if (behind) now[i] = rope_u32x4{0, 0, 0, 0};         // rows behind the last are 0, not -0
+    }
+    const auto to = [&](int i) { return xp + ((int64_t)(b * p.heads + h0 + i) * n_blocks + blk) * rows * D; };
+    const auto k_slot = [&](int r, int chunk) { return ((r % half) / 32 * CH + chunk) * 64 + r / half * 32 + r % 32; };
+    if constexpr (IS_K && D == 128) {
+      // K: the upper chunks of four rows against the lower ones of the next four: a store then covers eight rows of eight chunks, whole lines
+      // of 128 bytes (half lines: 358 us for K of 75,600 tokens of 40 heads, whole ones 281).
+      if (turn % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) before[i] = now[i];
+      } else {
+        const int r = row0(turn - 1) + 4 * (c / 8) + g;
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i)
+          if (i < heads) {
+            rope_u32x4 low, high;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t first = before[i][e], second = now[i][e];
+              low[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)first, (int)second, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
+              high[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)second, (int)first, 0x128, 0xf, 0x3, false);     // and into lanes 0-7
+            }
+            st_row<KEEP >= 1>(to(i) + k_slot(r, c % 8) * 8, low);
+            st_row<KEEP >= 1>(to(i) + k_slot(r, 8 + c % 8) * 8, high);
+          }
       }
+    } else {
+      const int r = row0(turn) + g;
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i)
+        if (i < heads) st_row<KEEP >= 1>(to(i) + (IS_K ? k_slot(r, c) : r * CH + c) * 8, now[i]);
+    }
   }
   if (mean == nullptr) return;
   // the wavefront's rows are added lane by lane, the wavefronts' sums in LDS: a fixed order
@@ -108,38 +153,51 @@ __device__ __forceinline__ void rope_block(const PermuteRopeArgs& a, int rows, i
   for (int i = 0; i < HEADS; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if constexpr (D == 64) sum[i][e] += __shfl_xor(sum[i][e], 8);
+      if constexpr (D == 64) sum[i][e] += rope_dpp<0x128>(sum[i][e]);
       sum[i][e] += __shfl_xor(sum[i][e], 16);
       sum[i][e] += __shfl_xor(sum[i][e], 32);
-      if (lane < CH) sums[wave][i][8 * c + e] = sum[i][e];
     }
+  if (lane < CH) {
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) lds.sums[wave][i][8 * c + e] = sum[i][e];
+  }
   __syncthreads();
   const int count = blk == n_blocks - 1 ? last_valid : rows;
   for (int i = threadIdx.x; i < heads * D; i += 256) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) s += sums[w][i / D][i % D];
+    for (int w = 0; w < 4; ++w) s += lds.sums[w][i / D][i % D];
     mean[((int64_t)(b * p.heads + h0 + i / D) * n_blocks + blk) * D + i % D] = s / (float)count;
   }
+}
+
+template <int D, bool IS_K, bool HALVES, int KEEP>
+__device__ __forceinline__ void rope_block(const PermuteRopeArgs& a, int rows, int n_blocks, int last_valid, int blk, int b, int h0, rope_lds<D>& lds) {
+  const auto with = [&](auto norm) {
+    // (a block with rows behind the last one has code of its own, which costs the others no registers)
+    if (blk == n_blocks - 1 && last_valid < rows) rope_rows_of<D, IS_K, HALVES, norm(), KEEP, true>(a, rows, n_blocks, last_valid, blk, b, h0, lds);
+    else rope_rows_of<D, IS_K, HALVES, norm(), KEEP, false>(a, rows, n_blocks, last_valid, blk, b, h0, lds);
+  };
+  a.norm ? with(std::true_type()) : with(std::false_type());
 }
 
 // First the Q blocks, then the K blocks, then V's parts, as in the permutation by itself.
 template <int D, int BK, bool HALVES, int KEEP>
 __global__ void __launch_bounds__(256) permute_rope_kernel(PermuteRopeArgs a, int q_rows) {
-  __shared__ __attribute__((aligned(16))) union { mean_sums<D> sums; v_rows<D> tile; } lds;
+  __shared__ __attribute__((aligned(16))) union { rope_lds<D> rope; v_rows<D> tile; } lds;
   const PermuteArgs& p = a.p;
   uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
   if (id < p.q_wgs) {
-    const uint32_t blk = id % p.n_q, at = id / p.n_q, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
-    if (a.norm) rope_block<D, false, HALVES, true, KEEP>(a, q_rows, p.n_q, p.last_q, blk, b, h0, lds.sums);
-    else rope_block<D, false, HALVES, false, KEEP>(a, q_rows, p.n_q, p.last_q, blk, b, h0, lds.sums);
+    const uint32_t at = id / p.n_q, blk = id - at * p.n_q, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
+    rope_block<D, false, HALVES, KEEP>(a, q_rows, p.n_q, p.last_q, blk, b, h0, lds.rope);
     return;
   }
   id -= p.q_wgs;
   if (id < p.k_wgs) {
-    const uint32_t blk = id % p.n_k, at = id / p.n_k, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
-    if (a.norm) rope_block<D, true, HALVES, true, KEEP>(a, BK, p.n_k, p.last_k, blk, b, h0, lds.sums);
-    else rope_block<D, true, HALVES, false, KEEP>(a, BK, p.n_k, p.last_k, blk, b, h0, lds.sums);
+    const uint32_t at = id / p.n_k, blk = id - at * p.n_k, b = at / a.groups, h0 = (at - b * a.groups) * HEADS;
+    rope_block<D, true, HALVES, KEEP>(a, BK, p.n_k, p.last_k, blk, b, h0, lds.rope);
     return;
   }
   id -= p.k_wgs;
@@ -147,13 +205,31 @@ __global__ void __launch_bounds__(256) permute_rope_kernel(PermuteRopeArgs a, in
   if (id < p.v_wgs) permute_vtile_part<D, BK, KEEP>(p.v, p.vp, p.perm, p.n_k, p.heads, p.st, id % parts, id / parts, lds.tile);
 }
 
+// V's parts by themselves, for large layers: they have no use for the registers of the others (75,600 tokens of 40 heads: 250 us with eight
+// wavefronts to a SIMD, 320 with four).
+template <int D, int BK, int KEEP>
+__global__ void __launch_bounds__(256) permute_v_kernel(PermuteArgs p) {
+  __shared__ __attribute__((aligned(16))) v_rows<D> tile;
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, parts = p.n_k * (BK / 64);
+  if (id < p.v_wgs) permute_vtile_part<D, BK, KEEP>(p.v, p.vp, p.perm, p.n_k, p.heads, p.st, id % parts, id / parts, tile);
+}
+
 template <int D, int BK>
 int launch(const rf2_plan* plan, PermuteRopeArgs a, bool halves, uint32_t q_wgs, uint32_t k_wgs, uint32_t v_wgs, hipStream_t st) {
-  const uint32_t n = q_wgs + k_wgs + v_wgs, rows = (n + 65535u) / 65536u;
-  a.p.q_wgs = q_wgs, a.p.k_wgs = k_wgs, a.p.v_wgs = v_wgs;
-  const dim3 grid((n + rows - 1) / rows, rows);
+  const auto grid = [](uint32_t n) {
+    const uint32_t rows = (n + 65535u) / 65536u;
+    return dim3((n + rows - 1) / rows, rows);
+  };
   const int64_t bytes = (3 * plan->info.N + plan->info.N_pad + 2 * plan->info.N_pad_k) * (int64_t)a.p.bh * D * 2;
-  const auto with = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a, plan->cfg.block); };
+  const bool apart = bytes > KEEP_STORES && v_wgs > 0;
+  a.p.q_wgs = q_wgs, a.p.k_wgs = k_wgs, a.p.v_wgs = v_wgs;
+  if (apart) {
+    permute_v_kernel<D, BK, 0><<<grid(v_wgs), 256, 0, st>>>(a.p);
+    RF2_LAUNCH_CHECK();
+    a.p.v_wgs = 0;
+  }
+  if (q_wgs + k_wgs + a.p.v_wgs == 0) return RF2_OK;
+  const auto with = [&](auto kernel) { kernel<<<grid(q_wgs + k_wgs + a.p.v_wgs), 256, 0, st>>>(a, plan->cfg.block); };
   if (halves) {
     if (bytes <= KEEP_ALL) with(permute_rope_kernel<D, BK, true, 2>);
     else if (bytes <= KEEP_STORES) with(permute_rope_kernel<D, BK, true, 1>);

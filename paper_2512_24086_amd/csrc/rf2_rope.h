@@ -5,9 +5,10 @@
 
 #include "rf2_internal.h"
 
-// Of each pair of channels, turns per unit of its axis' position, and the axis: a lane reads those of its pairs in a few wide loads.
+// Of each pair of channels, turns per unit of its axis' position, whole turns left out, in units of 2^-32 (rounded to the nearest) and what is
+// left of them in units of 2^-64; and the axis.  A lane reads those of its pairs in a few wide loads.
 struct rf2_rope_table {
-  double turns[64];
+  int32_t turns[64], rest[64];
   uint8_t axis[64];
 };
 
@@ -118,34 +119,45 @@ __device__ __forceinline__ void rope_partners(const float (&x)[8], float (&y)[8]
   for (int e = 0; e < 8; ++e) y[e] = HALVES ? rope_other_half<D>(x[e]) : x[e ^ 1];
 }
 
-// Cosine and signed sine for each of a lane's channels: channel c turns to x_c cs_c + x_partner sn_c.
-// The angle is taken in turns in 64 bits, less the nearest whole number, which leaves an error of 2^-22 turns at positions of 2^31 and
-// frequencies of 1; sine and cosine of what is left are the hardware's, off by 1.3e-7 at most (measured over 2^20 angles: 3.5e-8 on average,
-// where rounding to 32 bits alone is 1.5e-8).
+// What a lane keeps of the frequencies: of its four pairs (HALVES: the lanes of a pair's two channels have the same eight pairs, of which each
+// has four), turns per unit of position and where the position is among a token's.
+struct RopeLane {
+  int32_t turns[4], rest[4], axis[4];
+};
 template <int D, bool HALVES>
-__device__ __forceinline__ void rope_angles(const RopeArgs& a, const int32_t* __restrict__ pos, int c, float (&cs)[8], float (&sn)[8]) {
-#pragma clang fp contract(off)                  // (the kernels that share this are to give the same bits)
-  // (HALVES: the lanes of a pair's two channels have the same eight pairs, of which each works out four)
-  const bool upper = HALVES && c >= D / 16;
-  const int pair = HALVES ? 8 * c - (upper ? D / 2 - 4 : 0) : 4 * c;
-  // (without axes nothing turns, whatever is read here)
-  const int32_t* const at = a.axes > 0 ? pos : reinterpret_cast<const int32_t*>(a.table);
-  const int p0 = at[0], p1 = at[a.axes > 1 ? 1 : 0], p2 = at[a.axes > 2 ? 2 : 0], p3 = at[a.axes > 3 ? 3 : 0];
-  const double2 t01 = reinterpret_cast<const double2*>(a.table->turns + pair)[0], t23 = reinterpret_cast<const double2*>(a.table->turns + pair)[1];
-  const double turns[4] = {t01.x, t01.y, t23.x, t23.y};
+__device__ __forceinline__ RopeLane rope_lane(const RopeArgs& a, int c) {
+  const int pair = HALVES ? 8 * c - (c >= D / 16 ? D / 2 - 4 : 0) : 4 * c;
+  const int4 t = *reinterpret_cast<const int4*>(a.table->turns + pair), r = *reinterpret_cast<const int4*>(a.table->rest + pair);
   const uint32_t axes = *reinterpret_cast<const uint32_t*>(a.table->axis + pair);
+  return {{t.x, t.y, t.z, t.w}, {r.x, r.y, r.z, r.w}, {(int)(axes & 255), (int)(axes >> 8 & 255), (int)(axes >> 16 & 255), (int)(axes >> 24)}};
+}
+struct RopePlace {
+  int32_t at[4];
+};
+// A token's positions for a lane's pairs (without axes nothing turns, whatever is read).
+__device__ __forceinline__ RopePlace rope_place(const RopeArgs& a, const RopeLane& lane, const int32_t* __restrict__ pos) {
+  const int32_t* const from = a.axes > 0 ? pos : reinterpret_cast<const int32_t*>(a.table);
+  return {{from[lane.axis[0]], from[lane.axis[1]], from[lane.axis[2]], from[lane.axis[3]]}};
+}
+
+// Cosine and signed sine for each of a lane's channels: channel c turns to x_c cs_c + x_partner sn_c.
+// Position times frequency in whole numbers, of which the carries out of 32 bits are whole turns and fall away: what is left is the angle's
+// fraction of a turn with a sign, off by 2^-32 of one at any position.  In 32 bits (2^-26 turns off at most) it goes to the hardware's sine and
+// cosine (off by 1.3e-7 at most, measured over 2^20 angles; 3.5e-8 on average, where rounding to 32 bits alone is 1.5e-8).
+template <int D, bool HALVES>
+__device__ __forceinline__ void rope_angles(const RopeLane& lane, const RopePlace& place, int c, float (&cs)[8], float (&sn)[8]) {
   float co[4], si[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t low = axes & 1u << 8 * i, high = axes & 2u << 8 * i;
-    const int even = high ? p2 : p0, odd = high ? p3 : p1;
-    const double turn = (double)(low ? odd : even) * turns[i];
-    const float part = (float)(turn - __builtin_rint(turn));
+    const int64_t high = (int64_t)((uint64_t)((uint32_t)place.at[i] * (uint32_t)lane.turns[i]) << 32);
+    const int64_t turns = (int64_t)((uint64_t)((int64_t)place.at[i] * lane.rest[i]) + (uint64_t)high);
+    const float part = (float)(int32_t)(turns >> 32) * 0x1p-32f;
     co[i] = __builtin_amdgcn_cosf(part), si[i] = __builtin_amdgcn_sinf(part);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (HALVES) {
+      const bool upper = c >= D / 16;
       const float other_co = rope_other_half<D>(co[i]), other_si = rope_other_half<D>(si[i]);
       cs[i] = upper ? other_co : co[i];
       cs[4 + i] = upper ? co[i] : other_co;
@@ -171,48 +183,50 @@ __device__ __forceinline__ void rope_weights(const RopeArgs& a, const void* __re
 }
 
 // Weights and angles in one: channel c of a row x, normalised, becomes x_c A_c + x_partner B_c, A = w_c cos, B = -+ w_partner sin.
-template <class T, int D, bool HALVES, bool NORM>
-__device__ __forceinline__ void rope_factors(const RopeArgs& a, const int32_t* __restrict__ pos, const void* __restrict__ w, int c, float (&A)[8],
-                                             float (&B)[8]) {
+template <int D, bool HALVES, bool NORM>
+__device__ __forceinline__ void rope_factors(const RopeLane& lane, const RopePlace& place, const float (&own)[8], const float (&other)[8], int c,
+                                             float (&A)[8], float (&B)[8]) {
+  rope_angles<D, HALVES>(lane, place, c, A, B);
   if constexpr (NORM) {
-    float own[8], other[8];
-    rope_weights<T>(a, w, c, own);
-    if constexpr (HALVES) rope_weights<T>(a, w, c ^ (D / 16), other);
-    rope_angles<D, HALVES>(a, pos, c, A, B);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       A[e] *= own[e];
       B[e] *= HALVES ? other[e] : own[e ^ 1];
     }
-  } else {
-    rope_angles<D, HALVES>(a, pos, c, A, B);
   }
+}
+template <class T, int D, bool HALVES, bool NORM>
+__device__ __forceinline__ void rope_factors(const RopeArgs& a, const RopeLane& lane, const RopePlace& place, const void* __restrict__ w, int c,
+                                             float (&A)[8], float (&B)[8]) {
+  float own[8], other[8];
+  if constexpr (NORM) rope_weights<T>(a, w, c, own);
+  if constexpr (NORM && HALVES) rope_weights<T>(a, w, c ^ (D / 16), other);
+  rope_factors<D, HALVES, NORM>(lane, place, own, other, c, A, B);
 }
 
 // x becomes x / sqrt(mean(x^2) + eps); returns the factor.  A row whose squares leave 32 bits is made smaller first, by a power of two (next to
 // it eps is nothing).
 template <int D>
+__device__ __forceinline__ float rope_squares(const float (&x)[8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
+  return rope_row_sum<D>(s);
+}
+template <int D>
 __device__ __forceinline__ float rope_normalise(const RopeArgs& a, float (&x)[8]) {
-  const auto squares = [&] {
-    float s = 0.f;
+  float s = rope_squares<D>(x), eps = a.eps, less = 1.f;
+  if (__builtin_amdgcn_ballot_w64(!(s < 0x1p120f)) != 0) {       // (the whole wavefront or none of it: a factor of 1 changes nothing)
+    less = s < 0x1p120f ? 1.f : 0x1p-70f;
+    eps = s < 0x1p120f ? eps : 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
-    return rope_row_sum<D>(s);
-  };
-  float s = squares(), r;
-  if (s < 0x1p120f) {
-    r = __builtin_amdgcn_rsqf(fmaf(s, 1.f / D, a.eps));
-  } else {                                      // (all lanes of a row are here, or none)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= 0x1p-70f;
-    r = __builtin_amdgcn_rsqf(squares() * (1.f / D));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= r;
-    return r * 0x1p-70f;
+    for (int e = 0; e < 8; ++e) x[e] *= less;
+    s = rope_squares<D>(x);
   }
+  const float r = __builtin_amdgcn_rsqf(fmaf(s, 1.f / D, eps));
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= r;
-  return r;
+  return r * less;
 }
 
 // A row's channels in 32 bits, normalised, weighted and rotated.
@@ -298,8 +312,10 @@ __device__ __forceinline__ void rope_apply_rows(const RopeArgs& a, const RopeTok
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (first + u < end) v[u] = rope_load<false>(from + u * from_step);
+  const RopeLane angles = rope_lane<D, HALVES>(a, c);
+  const RopePlace place = rope_place(a, angles, t.pos + token.b * t.pos_batch + (int64_t)token.n * a.axes);
   float A[8], B[8];
-  rope_factors<T, D, HALVES, NORM>(a, t.pos + token.b * t.pos_batch + (int64_t)token.n * a.axes, s.w, c, A, B);
+  rope_factors<T, D, HALVES, NORM>(a, angles, place, s.w, c, A, B);
   for (int step = first; step < end; step += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u)

@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
   const int64_t x_step = s.x.head << log2, dz_step = s.dz.head << log2, dx_step = s.dx.head << log2;
   float w[8];
   rope_weights<T>(a.rope, s.w, c, w);
+  const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
   double total[8] = {};
   for (uint32_t i = id; i < s.share.tiles * (uint32_t)s.share.groups; i += s.workgroups) {
     const RopeUnit unit = rope_unit(s.share, i);
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
         vz[u] = rope_load<KEEP>(dz_at + u * dz_step);
       }
     float cs[8], sn[8], sum[8] = {};
-    rope_angles<D, HALVES>(a.rope, a.tokens.pos + t.b * a.tokens.pos_batch + (int64_t)t.n * a.rope.axes, c, cs, sn);
+    rope_angles<D, HALVES>(angles, rope_place(a.rope, angles, a.tokens.pos + t.b * a.tokens.pos_batch + (int64_t)t.n * a.rope.axes), c, cs, sn);
     for (int step = first; step < end; step += U) {
 #pragma unroll
       for (int u = 0; u < U; ++u)

@@ -27,16 +27,22 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
   if (dims > c.head_dim) return RF2_ERR_INVALID_ARG;
   if (c.axes > 0 && !inv_freq_host && !(c.theta > 0.0 && std::isfinite(c.theta))) return RF2_ERR_INVALID_ARG;
 
-  // turns per position of each pair; pairs behind the last axis do not turn
-  constexpr double TWO_PI = 6.283185307179586476925286766559;
+  // turns per position of each pair, in the 64 bits of a long double; pairs behind the last axis do not turn
+  constexpr long double TWO_PI = 6.283185307179586476925286766559L;
   rf2_rope_table tables[2] = {};
   int i = 0;
   for (int a = 0; a < c.axes; ++a)
     for (int j = 0; j < c.axis_dim[a] / 2; ++j, ++i) {
-      const double f = inv_freq_host ? inv_freq_host[i] : std::pow(c.theta, -2.0 * j / c.axis_dim[a]);
-      if (!(std::fabs(f) <= 65536.0)) return RF2_ERR_INVALID_ARG;
-      tables[0].turns[i] = f / TWO_PI;
-      tables[1].turns[i] = -f / TWO_PI;
+      const long double f = inv_freq_host ? (long double)inv_freq_host[i] : powl((long double)c.theta, -2.0L * j / c.axis_dim[a]);
+      if (!(fabsl(f) <= 65536.0L)) return RF2_ERR_INVALID_ARG;
+      for (int way = 0; way < 2; ++way) {
+        const long double turns = (way == 0 ? f : -f) / TWO_PI, part = (turns - rintl(turns)) * 0x1p32L, whole = rintl(part);     // |part| <= 2^31
+        const int64_t rest = llrintl((part - whole) * 0x1p32L);                                                                  // |rest| <= 2^31
+        // (2^31 units are as good as -2^31, but so many of the rest are one more or less of the others)
+        const int64_t carry = rest > INT32_MAX ? 1 : 0;
+        tables[way].turns[i] = (int32_t)(uint32_t)(uint64_t)((int64_t)whole + carry);
+        tables[way].rest[i] = (int32_t)(rest - (carry << 32));
+      }
       tables[0].axis[i] = tables[1].axis[i] = (uint8_t)a;
     }
 
