@@ -8,13 +8,13 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int TOKENS = 32, MORE = 11, ROWS = TOKENS + MORE;
 
-// 16-bit values are moved, whatever they stand for; those of K as `prepare` (16 bytes of a row, its token, which 16 bytes) returns them.
-template <int D, class Prepare>
+// 16-bit values are moved, whatever they stand for.  K may be left out.
+template <int D, bool WITH_K>
 __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t k_stride, int64_t v_stride,
                                            const int32_t* __restrict__ slots, int n_tokens, int64_t n_slots, int page_shift, int kv_heads, unsigned windows,
-                                           unsigned run, uint16_t* __restrict__ k_cache, uint16_t* __restrict__ v_cache, unsigned group, Prepare prepare) {
+                                           unsigned run, uint16_t* __restrict__ k_cache, uint16_t* __restrict__ v_cache, unsigned group) {
   constexpr int C = D / 8, PITCH = D + 8;                       // 16-byte chunks of a row; LDS rows are 16 bytes further apart
-  __shared__ __attribute__((aligned(16))) uint16_t k_rows[TOKENS * PITCH], v_rows[ROWS * PITCH];
+  __shared__ __attribute__((aligned(16))) uint16_t k_rows[WITH_K ? TOKENS * PITCH : 1], v_rows[ROWS * PITCH];
   __shared__ int32_t slot_of[MORE + ROWS];
   __shared__ int32_t todo[TOKENS + 1];                          // tokens of V that lead a group, four keys, or none; how many
   // Workgroups with equal number % 8 share an XCD: each XCD gets a run of windows head by head, so that lines which two
@@ -28,7 +28,7 @@ __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const
   // (rows are read once: marked as not to be kept, they leave the caches to what is written; 4,680 tokens of 40 heads 47.1 -> 36.0 us)
   u32x4 x[TOKENS * C / 256], y[(ROWS * C + 255) / 256];
 #pragma unroll
-  for (int i = 0; i < TOKENS * C / 256; ++i) {
+  for (int i = 0; i < TOKENS * C / 256 && WITH_K; ++i) {
     const int r = min((i * 256 + tid) / C, count - 1);
     x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + (n0 + r) * k_stride + column + tid % C * 8));
   }
@@ -43,9 +43,9 @@ __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const
     slot_of[tid] = slot >= 0 && slot < n_slots ? slot : -1;
   }
 #pragma unroll
-  for (int i = 0; i < TOKENS * C / 256; ++i) {
+  for (int i = 0; i < TOKENS * C / 256 && WITH_K; ++i) {
     const int r = (i * 256 + tid) / C;
-    if (r < count) *reinterpret_cast<u32x4*>(&k_rows[r * PITCH + tid % C * 8]) = prepare(x[i], n0 + r, tid % C);
+    if (r < count) *reinterpret_cast<u32x4*>(&k_rows[r * PITCH + tid % C * 8]) = x[i];
   }
 #pragma unroll
   for (int i = 0; i < (ROWS * C + 255) / 256; ++i) {
@@ -80,7 +80,7 @@ __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const
     return (((int64_t)page * kv_heads + head) * (1 << (page_shift - 5)) + (r >> 5)) * (32 * D);
   };
 #pragma unroll
-  for (int i = 0; i < TOKENS * C / 256; ++i) {
+  for (int i = 0; i < TOKENS * C / 256 && WITH_K; ++i) {
     const int z = i * 256 + tid, c = z / TOKENS, r = z % TOKENS, slot = slot_of[MORE + r];
     if (r < count && slot >= 0)
       *reinterpret_cast<uint4*>(k_cache + tile_of(slot) + (c * 32 + (slot & 31)) * 8) = *reinterpret_cast<const uint4*>(&k_rows[r * PITCH + 8 * c]);

@@ -1,7 +1,8 @@
 // New tokens of a paged cache, one launch: Q normalised and rotated, K too and into the cache's operand tiles, V into its own (gfx950).
 //
-// HBM bound, or by the launch where tokens are few: every row is read once and written once.  The first workgroups do K and V as rf2_paged_store
-// does (a row of K passes through its lanes' registers on the way into LDS), the others Q as rf2_rope_apply does.
+// HBM bound, or by the launch where tokens are few: every row is read once and written once.  The first workgroups do V as rf2_paged_store does,
+// the next K, the others Q as rf2_rope_apply does.  K goes from the registers in which it is rotated to its tiles: a wavefront has eight tokens, whose
+// 16-byte chunks stand side by side there, and goes through a few heads with their cosines and sines.
 #include "rf2_paged_store.h"
 #include "rf2_rope.h"
 
@@ -19,35 +20,91 @@ struct StoreRopeArgs {
   const int32_t* pos;
   const void* wk;
   int norm;
+  int k_steps;                       // heads of a wavefront
+  unsigned k_workgroups;
   const int32_t* n_live;             // tokens that are not padding, or NULL
   RopeSide q;
 };
 
-template <class T, int D, bool HALVES, bool KEEP>
-__global__ void __launch_bounds__(256) store_rope_kernel(StoreRopeArgs a) {
-  if (blockIdx.x < 8 * a.run) {
-    const auto prepare = [&](const u32x4& row, int64_t token, int c) {
-      const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
-      const RopePlace place = rope_place(a.rope, angles, a.pos + token * a.rope.axes);
-      float A[8], B[8], x[8];
-      T::unpack(row, x);
-      if (a.norm) {
-        rope_factors<T, D, HALVES, true>(a.rope, angles, place, a.wk, c, A, B);
-        rope_row<D, HALVES, true>(a.rope, A, B, x);
-      } else {
-        rope_factors<T, D, HALVES, false>(a.rope, angles, place, nullptr, c, A, B);
-        rope_row<D, HALVES, false>(a.rope, A, B, x);
+template <class T, int D, bool HALVES, bool NORM>
+__device__ __forceinline__ void store_k(const StoreRopeArgs& a, unsigned id) {
+  constexpr int C = D / 8, SETS = C / 8, AHEAD = 2;              // sets of rows of a wavefront
+  const unsigned group = id / a.windows, window = id - group * a.windows;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % C, g = lane / C;
+  const int first = (int)window * TOKENS + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
+  if (first >= a.n_tokens) return;
+  const uint16_t* from[SETS];
+  u32x4 v[AHEAD][SETS];
+#pragma unroll
+  for (int s = 0; s < SETS; ++s) {
+    from[s] = a.k + min(first + 4 * s + g, a.n_tokens - 1) * a.k_stride + (int64_t)h0 * D + 8 * c;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(i, end - 1 - h0) * D));
+  }
+  // the token whose rows a lane stores (below), and where
+  const int mine = first + (SETS == 2 ? 4 * (c / 8) : 0) + g;
+  const int slot = mine < a.n_tokens ? a.slots[mine] : -1;
+  const bool store = slot >= 0 && slot < a.n_slots;
+  const int page = slot >> a.page_shift, r = slot & ((1 << a.page_shift) - 1);
+  const int64_t head = (int64_t)D << a.page_shift;               // elements of a head of a page
+  uint16_t* to = a.k_cache + ((int64_t)page * a.kv_heads + h0) * head + (r >> 5) * (32 * D) + (c % 8 * 32 + (r & 31)) * 8;
+  const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
+  float own[8], other[8], A[SETS][8], B[SETS][8];
+  if constexpr (NORM) rope_weights<T>(a.rope, a.wk, c, own);
+  if constexpr (NORM && HALVES) rope_weights<T>(a.rope, a.wk, c ^ (C / 2), other);
+#pragma unroll
+  for (int s = 0; s < SETS; ++s) {
+    const RopePlace place = rope_place(a.rope, angles, a.pos + (int64_t)min(first + 4 * s + g, a.n_tokens - 1) * a.rope.axes);
+    rope_factors<D, HALVES, NORM>(angles, place, own, other, c, A[s], B[s]);
+  }
+  for (int h = h0; h < end; h += AHEAD)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (h + i >= end) break;
+      u32x4 z[SETS];
+#pragma unroll
+      for (int s = 0; s < SETS; ++s) {
+        float x[8];
+        T::unpack(v[i][s], x);
+        v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(h + i + AHEAD, end - 1) * D - h0 * D));
+        rope_row<D, HALVES, NORM>(a.rope, A[s], B[s], x);
+        z[s] = T::pack(x);
       }
-      return T::pack(x);
-    };
-    store_rows<D>(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache, a.v_cache,
-                  blockIdx.x, prepare);
+      if constexpr (SETS == 2) {
+        // the upper chunks of four tokens against the lower ones of the next four: a store covers eight chunks of eight tokens
+        u32x4 low, high;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t one = z[0][e], two = z[1][e];
+          low[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)one, (int)two, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
+          high[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)two, (int)one, 0x128, 0xf, 0x3, false);     // and into lanes 0-7
+        }
+        if (store) {
+          *reinterpret_cast<u32x4*>(to) = low;
+          *reinterpret_cast<u32x4*>(to + 8 * 32 * 8) = high;
+        }
+      } else if (store) {
+        *reinterpret_cast<u32x4*>(to) = z[0];
+      }
+      to += head;
+    }
+}
+
+template <class T, int D, bool HALVES, bool NORM, bool KEEP>
+__global__ void __launch_bounds__(256) store_rope_kernel(StoreRopeArgs a) {
+  unsigned id = blockIdx.x;
+  if (id < 8 * a.run) {
+    store_rows<D, false>(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache, a.v_cache, id);
     return;
   }
+  id -= 8 * a.run;
+  if (id < a.k_workgroups) {
+    store_k<T, D, HALVES, NORM>(a, id);
+    return;
+  }
+  id -= a.k_workgroups;
   const uint32_t live = a.n_live ? (uint32_t)min(max(*a.n_live, 0), a.n_tokens) : (uint32_t)a.n_tokens;
-  const RopeTokens tokens{a.pos, 0, live, live};
-  if (a.norm) rope_apply_rows<T, D, HALVES, true, KEEP>(a.rope, tokens, a.q, blockIdx.x - 8 * a.run);
-  else rope_apply_rows<T, D, HALVES, false, KEEP>(a.rope, tokens, a.q, blockIdx.x - 8 * a.run);
+  rope_apply_rows<T, D, HALVES, NORM, KEEP>(a.rope, RopeTokens{a.pos, 0, live, live}, a.q, id);
 }
 
 }  // namespace
@@ -72,19 +129,24 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
   if (!rf2_aligned(slots, 4) || !rf2_aligned(n_live, 4)) return RF2_ERR_INVALID_ARG;
   if (n_tokens > 0 && (!rf2_rope_pos_fits(rope, pos) || !rf2_rope_weight_fits(rope, wq) || !rf2_rope_weight_fits(rope, wk))) return RF2_ERR_INVALID_ARG;
   const unsigned windows = (unsigned)(n_tokens + TOKENS - 1) / TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
-  if (run >= 1u << 20) return RF2_ERR_UNSUPPORTED;           // (a grid has less than 2^32 threads, half of them for Q)
+  if (run >= 1u << 20) return RF2_ERR_UNSUPPORTED;           // (a grid has less than 2^32 threads, half of them for V and K)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;
   const rf2_rows q_rows{q, 0, n_tokens > 1 ? q_stride : q_row, c.head_dim}, out_rows{q_out, 0, n_tokens > 1 ? q_out_stride : q_row, c.head_dim};
   const RopeSide side{rope_rows(q_rows), rope_rows(out_rows), wq, rope_share(q_rows, c.heads, r, (uint32_t)n_tokens)};
+  // K's wavefronts take as many heads as leave 2,048 of them, four (HALVES: five) at most
+  const int64_t k_work = (int64_t)((n_tokens + 7) / 8) * c.kv_heads;
+  const int k_steps = (int)std::min<int64_t>(r.pairing == RF2_ROPE_HALVES ? 5 : 4, std::max<int64_t>(1, k_work / 2048));
+  const unsigned k_workgroups = windows * (unsigned)((c.kv_heads + k_steps - 1) / k_steps);
   const StoreRopeArgs a{(const uint16_t*)k, (const uint16_t*)v, k_stride, v_stride, slots, n_tokens, __builtin_ctz((unsigned)c.page), c.kv_heads,
                         (int64_t)c.n_pages * c.page, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
-                        r.norm == RF2_NORM_RMS, n_live, side};
-  const dim3 grid(8 * run + rope_workgroups(side.share));
+                        r.norm == RF2_NORM_RMS, k_steps, k_workgroups, n_live, side};
+  const dim3 grid(8 * run + k_workgroups + rope_workgroups(side.share));
   const bool keep = (int64_t)n_tokens * q_row * 4 <= ROPE_KEEP;
   hipStream_t st = (hipStream_t)stream;
   return rope_for_types(r, [&](auto type, auto d, auto halves) {
-    if (keep) store_rope_kernel<decltype(type), d(), halves(), true><<<grid, 256, 0, st>>>(a);
-    else store_rope_kernel<decltype(type), d(), halves(), false><<<grid, 256, 0, st>>>(a);
+    const auto launch = [&](auto norm, auto kept) { store_rope_kernel<decltype(type), d(), halves(), norm(), kept()><<<grid, 256, 0, st>>>(a); };
+    const auto with = [&](auto norm) { keep ? launch(norm, std::true_type()) : launch(norm, std::false_type()); };
+    a.norm ? with(std::true_type()) : with(std::false_type());
   });
 }
