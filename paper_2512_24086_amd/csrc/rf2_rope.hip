@@ -166,11 +166,14 @@ bool in_range(const rf2_rows& r, int32_t batch, int32_t tokens, int32_t heads) {
 template <bool B>
 using flag = std::integral_constant<bool, B>;
 
-// Rows of Q and K, in and out: all of a side or nothing.
-int check_rows(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rows* const (&rows)[2][3], int n) {
+// Rows of Q and K, in and out: all of a side or nothing.  Strides of axes of one say nothing.
+int check_rows(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, rf2_rows* const (&rows)[2][3], int n) {
   for (int i = 0; i < 2; ++i) {
     const int32_t heads = i == 0 ? plan->cfg.heads : plan->cfg.kv_heads;
     for (int j = 0; j < n; ++j) {
+      if (batch == 1) rows[i][j]->batch = 0;
+      if (n_tokens == 1) rows[i][j]->token = rows[i][j]->batch;
+      if (heads == 1) rows[i][j]->head = 0;
       if ((rows[i][j]->at == nullptr) != (rows[i][n - 1]->at == nullptr)) return RF2_ERR_INVALID_ARG;
       if (rows[i][j]->at && (!readable(*rows[i][j]) || !in_range(*rows[i][j], batch, n_tokens, heads))) return RF2_ERR_INVALID_ARG;
     }
@@ -212,31 +215,33 @@ int launch_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, con
 extern "C" int rf2_rope_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rope_tensors* rows, const int32_t* pos,
                               int64_t pos_batch, const void* wq, const void* wk, void* stream) {
   if (!plan || !rows) return RF2_ERR_INVALID_ARG;
+  rf2_rope_tensors t = *rows;
   if (const int rc = check_tokens(batch, n_tokens, pos_batch)) return rc;
   if (batch == 0 || n_tokens == 0) return rf2_check_rope_device(plan);     // (an empty tensor may have no address)
-  const rf2_rows* const sides[2][3] = {{&rows->q, &rows->q_out}, {&rows->k, &rows->k_out}};
+  rf2_rows* const sides[2][3] = {{&t.q, &t.q_out}, {&t.k, &t.k_out}};
   if (const int rc = check_rows(plan, batch, n_tokens, sides, 2)) return rc;
   if (!rf2_rope_pos_fits(plan, pos)) return RF2_ERR_INVALID_ARG;
-  if ((rows->q.at && !rf2_rope_weight_fits(plan, wq)) || (rows->k.at && !rf2_rope_weight_fits(plan, wk))) return RF2_ERR_INVALID_ARG;
+  if ((t.q.at && !rf2_rope_weight_fits(plan, wq)) || (t.k.at && !rf2_rope_weight_fits(plan, wk))) return RF2_ERR_INVALID_ARG;
   if (const int rc = rf2_check_rope_device(plan)) return rc;
-  return launch_apply(plan, batch, n_tokens, rows->q, rows->k, pos, pos_batch, wq, wk, rows->q_out, rows->k_out, plan->cfg.norm == RF2_NORM_RMS, false,
+  return launch_apply(plan, batch, n_tokens, t.q, t.k, pos, pos_batch, wq, wk, t.q_out, t.k_out, plan->cfg.norm == RF2_NORM_RMS, false,
                       (hipStream_t)stream);
 }
 
 extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, const rf2_rope_gradients* rows, const int32_t* pos,
                                  int64_t pos_batch, const void* wq, const void* wk, float* dwq, float* dwk, void* workspace, void* stream) {
   if (!plan || !rows) return RF2_ERR_INVALID_ARG;
+  rf2_rope_gradients t = *rows;
   if (const int rc = check_tokens(batch, n_tokens, pos_batch)) return rc;
   const rf2_rope_config& c = plan->cfg;
   const bool norm = c.norm == RF2_NORM_RMS, nothing = batch == 0 || n_tokens == 0;
   // without a norm the rows themselves are not read
-  const rf2_rows* const sides[2][3] = {{norm ? &rows->q : &rows->dq_out, &rows->dq_out, &rows->dq}, {norm ? &rows->k : &rows->dk_out, &rows->dk_out, &rows->dk}};
+  rf2_rows* const sides[2][3] = {{norm ? &t.q : &t.dq_out, &t.dq_out, &t.dq}, {norm ? &t.k : &t.dk_out, &t.dk_out, &t.dk}};
   if (!nothing) {
     if (const int rc = check_rows(plan, batch, n_tokens, sides, 3)) return rc;
     if (!rf2_rope_pos_fits(plan, pos)) return RF2_ERR_INVALID_ARG;
   }
   float* const dw[2] = {dwq, dwk};
-  const bool have[2] = {nothing ? dwq != nullptr : rows->dq.at != nullptr, nothing ? dwk != nullptr : rows->dk.at != nullptr};
+  const bool have[2] = {nothing ? dwq != nullptr : t.dq.at != nullptr, nothing ? dwk != nullptr : t.dk.at != nullptr};
   for (int i = 0; i < 2; ++i) {
     if (have[i] && !nothing && !rf2_rope_weight_fits(plan, i == 0 ? wq : wk)) return RF2_ERR_INVALID_ARG;
     if (norm ? (have[i] && !dw[i]) || !rf2_rope_aligned(dw[i], 4) : dw[i] != nullptr) return RF2_ERR_INVALID_ARG;
@@ -246,7 +251,7 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
   const hipStream_t st = (hipStream_t)stream;
   if (!norm) {
     if (nothing) return RF2_OK;
-    return launch_apply(plan, batch, n_tokens, rows->dq_out, rows->dk_out, pos, pos_batch, nullptr, nullptr, rows->dq, rows->dk, false, true, st);
+    return launch_apply(plan, batch, n_tokens, t.dq_out, t.dk_out, pos, pos_batch, nullptr, nullptr, t.dq, t.dk, false, true, st);
   }
 
   BackArgs a{rope_args(plan, false), {pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens}, {}};
@@ -255,12 +260,12 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
   for (int i = 0; i < 2; ++i) {
     if (!have[i]) continue;
     BackSide& s = a.side[i];
-    s.x = rope_rows(i == 0 ? rows->q : rows->k);
-    s.dz = rope_rows(i == 0 ? rows->dq_out : rows->dk_out);
-    s.dx = rope_rows(i == 0 ? rows->dq : rows->dk);
+    s.x = rope_rows(i == 0 ? t.q : t.k);
+    s.dz = rope_rows(i == 0 ? t.dq_out : t.dk_out);
+    s.dx = rope_rows(i == 0 ? t.dq : t.dk);
     s.w = i == 0 ? wq : wk;
     const int heads = i == 0 ? c.heads : c.kv_heads;
-    s.share = rope_share(i == 0 ? rows->q : rows->k, heads, c, a.tokens.total);
+    s.share = rope_share(i == 0 ? t.q : t.k, heads, c, a.tokens.total);
     s.workgroups = nothing ? 0 : (uint32_t)std::min<int64_t>(RF2_ROPE_PARTS, rope_workgroups(s.share));
     float* const sums = (float*)workspace + (size_t)i * RF2_ROPE_PARTS * c.head_dim;
     s.sums = s.workgroups == 1 ? dw[i] : sums;

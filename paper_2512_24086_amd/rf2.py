@@ -494,48 +494,52 @@ class RopePlan:
         return torch.empty(self.info.workspace_bytes, dtype=torch.uint8, device=device)
 
     # -- arguments -----------------------------------------------------------------------------
-    def _rows(self, t, what, heads, batch, tokens):
-        """(address, strides of the batch, a token, a head) of a tensor of rows; batch and tokens as another one has them, or None."""
-        shape, stride, n = t.shape, t.stride(), t.dim()
-        token, head = (n - 3, n - 2) if self.layout == RF2_LAYOUT_BNHD else (n - 2, n - 3)
-        if (n not in (3, 4) or t.dtype is not self.dtype or t.get_device() != self.device or shape[head] != heads
-                or shape[-1] != self.cfg.head_dim or stride[-1] != 1 or (tokens is not None and (shape[token] != tokens or
-                                                                                                 (shape[0] if n == 4 else 1) != batch))):
-            order = "tokens, heads" if self.layout == RF2_LAYOUT_BNHD else "heads, tokens"
-            raise ValueError(f"{what}: expected [batch, {order}, head_dim] of {self.dtype} on device {self.device} with {heads} heads of "
-                             f"{self.cfg.head_dim} channels side by side, batch and tokens as the others have, got {tuple(shape)} of {t.dtype} on "
-                             f"{t.device}, strides {stride}")
-        # (the stride of an axis of one says nothing)
-        return (t.data_ptr(), stride[0] if n == 4 and shape[0] > 1 else 0, stride[token] if shape[token] > 1 else 0,
-                stride[head] if heads > 1 else 0)
+    def _sizes(self, t):
+        """Batch and tokens of a tensor of rows, and the shapes that all of Q's and all of K's have then."""
+        c, shape = self.cfg, t.shape
+        if self.layout == RF2_LAYOUT_BNHD:
+            if len(shape) == 4:
+                batch, tokens = shape[0], shape[1]
+                return batch, tokens, (batch, tokens, c.heads, c.head_dim), (batch, tokens, c.kv_heads, c.head_dim)
+            if len(shape) == 3:
+                return 1, shape[0], (shape[0], c.heads, c.head_dim), (shape[0], c.kv_heads, c.head_dim)
+        elif len(shape) == 4:
+            batch, tokens = shape[0], shape[2]
+            return batch, tokens, (batch, c.heads, tokens, c.head_dim), (batch, c.kv_heads, tokens, c.head_dim)
+        elif len(shape) == 3:
+            return 1, shape[1], (c.heads, shape[1], c.head_dim), (c.kv_heads, shape[1], c.head_dim)
+        raise ValueError(f"expected rows of three or four axes, got {tuple(shape)}")
 
-    def _sides(self, q, k, more):
-        """The rows of q's tensors and k's, (q, k, q, k, ...), and batch and tokens."""
-        one = q[0] if q[0] is not None else k[0]
-        if one is None:
-            raise ValueError("q and k: expected one at least")
-        n = one.dim()
-        batch, tokens = one.shape[0] if n == 4 else 1, one.shape[n - 3 if self.layout == RF2_LAYOUT_BNHD else n - 2] if n >= 3 else 0
-        rows = []
-        for i, name in enumerate(more):
-            for t, side, heads in ((q[i], "q", self.cfg.heads), (k[i], "k", self.cfg.kv_heads)):
-                if (t is None) != ((q if side == "q" else k)[0] is None):
-                    raise ValueError(f"{name.format(side)}: expected with the other tensors of {side}, or without them")
-                rows += _NO_ROWS if t is None else self._rows(t, name.format(side), heads, batch, tokens)
-        return rows, batch, tokens
+    def _rows(self, t, what, shape):
+        """(address, strides of the batch, a token, a head) of a tensor of rows."""
+        if t is None:
+            raise ValueError(f"{what}: expected with the others of its side")
+        stride = t.stride()
+        if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.device or stride[-1] != 1:
+            raise ValueError(f"{what}: expected {shape} of {self.dtype} on device {self.device}, channels side by side, got {tuple(t.shape)} of "
+                             f"{t.dtype} on {t.device}, strides {stride}")
+        if len(stride) == 4:
+            return (t.data_ptr(), *stride[:3]) if self.layout == RF2_LAYOUT_BNHD else (t.data_ptr(), stride[0], stride[2], stride[1])
+        return (t.data_ptr(), 0, stride[0], stride[1]) if self.layout == RF2_LAYOUT_BNHD else (t.data_ptr(), 0, stride[1], stride[0])
 
     def _pos(self, pos, batch, tokens):
         axes = self.cfg.axes
         if axes == 0:
             return None, 0
-        if (pos is None or pos.dtype is not torch.int32 or pos.get_device() != self.device or not pos.is_contiguous()
-                or tuple(pos.shape) not in ((tokens, axes), (batch, tokens, axes))):
+        shape = None if pos is None else pos.shape
+        if shape == (tokens, axes):
+            step = 0
+        elif shape == (batch, tokens, axes):
+            step = tokens * axes
+        else:
+            step = -1
+        if step < 0 or pos.dtype is not torch.int32 or pos.get_device() != self.device or not pos.is_contiguous():
             raise ValueError(f"pos: expected contiguous {(tokens, axes)} or {(batch, tokens, axes)} of torch.int32 on device {self.device}, got "
                              + ("none" if pos is None else f"{tuple(pos.shape)} of {pos.dtype} on {pos.device}, strides {pos.stride()}"))
-        return pos.data_ptr(), tokens * axes if pos.dim() == 3 else 0
+        return pos.data_ptr(), step
 
     def _weight(self, w, what, there=True):
-        if (w is None) == (self.cfg.norm == RF2_NORM_RMS and there):
+        if (w is None) == (there and self.cfg.norm == RF2_NORM_RMS):
             raise ValueError(f"{what}: expected " + ("weights of the norm" if w is None else "none: there is no norm, or no rows that have it"))
         return None if w is None else _arg(w, what, self.weight_dtype, self.cfg.head_dim, self.device)
 
@@ -545,25 +549,35 @@ class RopePlan:
     # -- the calls -----------------------------------------------------------------------------
     def rf2_rope_apply(self, q, k, pos, q_out, k_out, wq=None, wk=None, stream=None):
         """q_out and k_out from q and k (either of them may be None, with its output).  q_out may be q, k_out k."""
-        rows, batch, tokens = self._sides((q, q_out), (k, k_out), ("{}", "{}_out"))
+        if q is None and k is None:
+            raise ValueError("q and k: expected one at least")
+        batch, tokens, q_shape, k_shape = self._sizes(k if q is None else q)
+        rows = self._rows
         at, step = self._pos(pos, batch, tokens)
-        _check(lib().rf2_rope_apply(self._h, batch, tokens, _two_rows_twice.pack(*rows), at, step, self._weight(wq, "wq", q is not None),
-                                    self._weight(wk, "wk", k is not None), self._stream(stream)), "rf2_rope_apply")
+        q, q_out = (_NO_ROWS, _NO_ROWS) if q is None and q_out is None else (rows(q, "q", q_shape), rows(q_out, "q_out", q_shape))
+        k, k_out = (_NO_ROWS, _NO_ROWS) if k is None and k_out is None else (rows(k, "k", k_shape), rows(k_out, "k_out", k_shape))
+        _check(lib().rf2_rope_apply(self._h, batch, tokens, _two_rows_twice.pack(*q, *k, *q_out, *k_out), at, step,
+                                    self._weight(wq, "wq", q is not _NO_ROWS), self._weight(wk, "wk", k is not _NO_ROWS), self._stream(stream)),
+               "rf2_rope_apply")
 
     def rf2_rope_backward(self, q, k, pos, dq_out, dk_out, dq, dk, wq=None, wk=None, dwq=None, dwk=None, workspace=None, stream=None):
         """dq, dk, dwq, dwk from q, k and the gradients of q_out and k_out.  Without a norm q and k are not read and may be None."""
         norm = self.cfg.norm == RF2_NORM_RMS
         if not norm:
             q, k = dq_out, dk_out
-        rows, batch, tokens = self._sides((q, dq_out, dq), (k, dk_out, dk), ("{}", "d{}_out", "d{}"))
+        if q is None and k is None:
+            raise ValueError("q and k: expected one at least")
+        batch, tokens, q_shape, k_shape = self._sizes(k if q is None else q)
         at, step = self._pos(pos, batch, tokens)
-        f32, d = torch.float32, self.cfg.head_dim
-        for name, dw, side in (("dwq", dwq, q), ("dwk", dwk, k)):
-            if (dw is None) == (norm and side is not None):
-                raise ValueError(f"{name}: expected " + (f"{d} elements of {f32}" if dw is None else "none: there is no norm, or no rows that have it"))
+        sides = []
+        for name, tensors, w, dw, shape in (("q", (q, dq_out, dq), wq, dwq, q_shape), ("k", (k, dk_out, dk), wk, dwk, k_shape)):
+            there = tensors != (None, None, None) if tensors[0] is None else True
+            if (dw is None) == (norm and there):
+                raise ValueError(f"dw{name}: expected " + ("the gradient of the weights" if dw is None else "none: there is no norm, or no rows that have it"))
+            sides.append(([self._rows(t, what, shape) for t, what in zip(tensors, (name, f"d{name}_out", f"d{name}"))] if there else [_NO_ROWS] * 3,
+                          self._weight(w, "w" + name, there), None if dw is None else _arg(dw, "dw" + name, torch.float32, self.cfg.head_dim, self.device)))
+        (qs, wq, dwq), (ks, wk, dwk) = sides
         _check(lib().rf2_rope_backward(
-            self._h, batch, tokens, _two_rows_thrice.pack(*rows), at, step, self._weight(wq, "wq", q is not None),
-            self._weight(wk, "wk", k is not None), None if dwq is None else _arg(dwq, "dwq", f32, d, self.device),
-            None if dwk is None else _arg(dwk, "dwk", f32, d, self.device),
+            self._h, batch, tokens, _two_rows_thrice.pack(*qs[0], *ks[0], *qs[1], *ks[1], *qs[2], *ks[2]), at, step, wq, wk, dwq, dwk,
             None if not norm or workspace is None else _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, self.device),
             self._stream(stream)), "rf2_rope_backward")

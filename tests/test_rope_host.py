@@ -243,10 +243,13 @@ def test_rows_of_the_binding_are_those_of_c():
     p.device = -1
     joint = torch.zeros(3, 7, 8, 64, dtype=torch.bfloat16)
     q = joint[:, :, 1:5].transpose(1, 2)
-    assert p._rows(q, "q", 4, 3, 7) == (joint.data_ptr() + 128, 7 * 512, 512, 64)
-    assert p._rows(q[0], "q", 4, 1, 7) == (joint.data_ptr() + 128, 0, 512, 64)
+    assert p._sizes(q) == (3, 7, (3, 4, 7, 64), (3, 2, 7, 64)) and p._sizes(q[0]) == (1, 7, (4, 7, 64), (2, 7, 64))
+    assert p._rows(q, "q", (3, 4, 7, 64)) == (joint.data_ptr() + 128, 7 * 512, 512, 64)
+    assert p._rows(q[0], "q", (4, 7, 64)) == (joint.data_ptr() + 128, 0, 512, 64)
     p = make()
     p.device = -1
-    assert p._rows(joint[:, :, 1:5], "q", 4, 3, 7) == (joint.data_ptr() + 128, 7 * 512, 512, 64)
-    assert p._rows(joint[:, :1, 1:5], "q", 4, 3, 1)[2] == 0
+    q = joint[:, :, 1:5]
+    assert p._sizes(q) == (3, 7, (3, 7, 4, 64), (3, 7, 2, 64)) and p._sizes(q[0]) == (1, 7, (7, 4, 64), (7, 2, 64))
+    assert p._rows(q, "q", (3, 7, 4, 64)) == (joint.data_ptr() + 128, 7 * 512, 512, 64)
+    assert p._rows(q[1], "q", (7, 4, 64)) == (joint.data_ptr() + 128 + 2 * 7 * 512, 0, 512, 64)
     assert math.isclose(p.cfg.theta, 10000.0)
