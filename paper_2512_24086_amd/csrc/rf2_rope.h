@@ -19,9 +19,17 @@ struct rf2_rope_plan {
   rf2_rope_table* d_table;  // device, two: the second one turns the other way
 };
 
-// The sums of the weights' gradients: so many workgroups for each of Q and K at most, head_dim numbers of 32 bits from each.
-constexpr int RF2_ROPE_PARTS = 1024;
-inline int64_t rf2_rope_workspace(int head_dim) { return (int64_t)2 * RF2_ROPE_PARTS * head_dim * 4; }
+// The sums of the weights' gradients: so many workgroups for each of Q and K at most, head_dim numbers of 32 bits from each, and so many runs of
+// them, in 64 bits.
+constexpr int RF2_ROPE_PARTS = 8192, RF2_ROPE_RUNS = 128, RF2_ROPE_FEW = 512, RF2_ROPE_MANY = 2048;
+struct RopeWorkspace {
+  int64_t sums, runs;        // in bytes, of Q (side 0) or K
+};
+inline RopeWorkspace rope_workspace(int head_dim, int side) {
+  const int64_t sums = (int64_t)RF2_ROPE_PARTS * head_dim * 4, runs = (int64_t)RF2_ROPE_RUNS * head_dim * 8;
+  return {side * sums, 2 * sums + side * runs};
+}
+inline int64_t rf2_rope_workspace(int head_dim) { return rope_workspace(head_dim, 2).runs; }
 
 inline bool rf2_rope_aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 

@@ -37,6 +37,11 @@ struct BackArgs {
 
 // With g = R(-phi) dz and x^ = x r:  dx = r (g w - x^ mean(g w x^)),  dw = sum over rows of g x^.  Sums of dw: a token's heads in 32 bits, a
 // lane's tokens in 64, then the rows of the workgroup in order.
+//
+// HBM bound: x and dz are read once, dx is written once.  Loads of a token's next two heads are asked for before those in hand are worked on.  Large
+// calls take 8,192 workgroups for each of Q and K, many more than are resident, which reads faster than few that go round (32,760 tokens of
+// 40 + 40 heads: 1,024 354 us, 4,096 336, 8,192 323, and 10 for their sums; sums by elements, read and written alike, take 312).  Smaller ones are
+// better off with 512, whose sums one launch adds up.
 template <class T, int D, bool HALVES, bool KEEP>
 __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
   constexpr int CH = D / 8, R = 64 / CH, U = 2;
@@ -115,27 +120,73 @@ __global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
   }
 }
 
-// The workgroups' sums to one, in 64 bits and a fixed order.  A workgroup takes 16 channels, 16 lines of sums at a time.
-struct JoinArgs {
-  const float* sums[2];
-  float* dw[2];
-  uint32_t lines[2];
+// The workgroups' sums to one, in 64 bits and a fixed order.  Latency of loads and launches is all it costs.  Up to 512 lines, or runs of many, are added
+// up by workgroups of 8 channels each, 128 lines at a time (join_kernel); more lines go to runs of 64 first (runs_kernel): 8,192 lines 9.3
+// us, without 23, and 25 in one launch whose last workgroup ends it (counting up in one place for all XCDs is slow).
+template <class IN, class OUT>
+struct JoinSide {
+  const IN* in;              // [lines][d]
+  OUT* out;                  // [groups][d]
+  uint32_t lines, groups;
 };
+template <class IN, class OUT>
+struct JoinArgs {
+  JoinSide<IN, OUT> side[2];
+};
+
 template <int D>
-__global__ void __launch_bounds__(256) join_kernel(JoinArgs a) {
-  __shared__ double part[16][16];
-  const int side = blockIdx.x / (D / 16), ch = blockIdx.x % (D / 16) * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
-  if (a.dw[side] == nullptr) return;
-  double sum = 0;
-#pragma unroll 8
-  for (uint32_t i = slice; i < a.lines[side]; i += 16) sum += (double)a.sums[side][(size_t)i * D + ch];
-  part[slice][threadIdx.x % 16] = sum;
-  __syncthreads();
-  if (slice == 0) {
+__global__ void __launch_bounds__(256) runs_kernel(JoinArgs<float, double> a) {
+  constexpr int LANES = D / 4, SLICES = 256 / LANES, U = 64 / SLICES;
+  __shared__ double part[SLICES][D];
+  const bool second = blockIdx.x >= a.side[0].groups;
+  const JoinSide<float, double>& s = a.side[second ? 1 : 0];
+  const uint32_t group = blockIdx.x - (second ? a.side[0].groups : 0);
+  const int slice = threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+  float4 x[U];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) sum += part[i][threadIdx.x];
-    a.dw[side][ch] = (float)sum;
+  for (int u = 0; u < U; ++u) {
+    const uint32_t line = group * 64 + u * SLICES + slice;
+    x[u] = line < s.lines ? *reinterpret_cast<const float4*>(s.in + (size_t)line * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
+  double sum[4] = {};
+#pragma unroll
+  for (int u = 0; u < U; ++u) sum[0] += x[u].x, sum[1] += x[u].y, sum[2] += x[u].z, sum[3] += x[u].w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[slice][c + e] = sum[e];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    double total = 0;
+#pragma unroll
+    for (int i = 0; i < SLICES; ++i) total += part[i][threadIdx.x];
+    s.out[(size_t)group * D + threadIdx.x] = total;
+  }
+}
+
+template <int D, class IN>
+__global__ void __launch_bounds__(1024) join_kernel(JoinArgs<IN, float> a) {
+  __shared__ double part[128][8];
+  const JoinSide<IN, float>& s = a.side[blockIdx.x / (D / 8)];
+  if (s.out == nullptr) return;
+  const int ch = blockIdx.x % (D / 8) * 8 + threadIdx.x % 8, slice = threadIdx.x / 8;
+  double sum = 0;
+#pragma unroll 4
+  for (uint32_t i = slice; i < s.lines; i += 128) sum += (double)s.in[(size_t)i * D + ch];
+  part[slice][threadIdx.x % 8] = sum;
+  __syncthreads();
+#pragma unroll
+  for (int half = 64; half >= 1; half /= 2) {
+    if (slice < half) part[slice][threadIdx.x % 8] += part[slice + half][threadIdx.x % 8];
+    __syncthreads();
+  }
+  if (slice == 0) s.out[ch] = (float)part[0][threadIdx.x];
+}
+template <class IN>
+int launch_join(int d, const JoinArgs<IN, float>& a, hipStream_t st) {
+  if (!a.side[0].out && !a.side[1].out) return RF2_OK;
+  if (d == 128) join_kernel<128, IN><<<2 * 128 / 8, 1024, 0, st>>>(a);
+  else join_kernel<64, IN><<<2 * 64 / 8, 1024, 0, st>>>(a);
+  RF2_LAUNCH_CHECK();
+  return RF2_OK;
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
@@ -255,7 +306,9 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
   }
 
   BackArgs a{rope_args(plan, false), {pos, pos_batch, (uint32_t)n_tokens, (uint32_t)batch * (uint32_t)n_tokens}, {}};
-  JoinArgs join{};
+  JoinArgs<float, double> runs{};
+  JoinArgs<double, float> join_runs{};
+  JoinArgs<float, float> join{};
   int64_t bytes = 0;
   for (int i = 0; i < 2; ++i) {
     if (!have[i]) continue;
@@ -266,10 +319,19 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     s.w = i == 0 ? wq : wk;
     const int heads = i == 0 ? c.heads : c.kv_heads;
     s.share = rope_share(i == 0 ? t.q : t.k, heads, c, a.tokens.total);
-    s.workgroups = nothing ? 0 : (uint32_t)std::min<int64_t>(RF2_ROPE_PARTS, rope_workgroups(s.share));
-    float* const sums = (float*)workspace + (size_t)i * RF2_ROPE_PARTS * c.head_dim;
+    const uint32_t units = rope_workgroups(s.share);
+    s.workgroups = nothing ? 0 : std::min<uint32_t>(units, units > RF2_ROPE_MANY ? RF2_ROPE_PARTS : RF2_ROPE_FEW);
+    const RopeWorkspace ws = rope_workspace(c.head_dim, i);
+    float* const sums = (float*)((char*)workspace + ws.sums);
     s.sums = s.workgroups == 1 ? dw[i] : sums;
-    if (s.workgroups != 1) join.sums[i] = sums, join.dw[i] = dw[i], join.lines[i] = s.workgroups;
+    if (s.workgroups > RF2_ROPE_FEW) {
+      const uint32_t n = (s.workgroups + 63) / 64;
+      double* const at = (double*)((char*)workspace + ws.runs);
+      runs.side[i] = {sums, at, s.workgroups, n};
+      join_runs.side[i] = {at, dw[i], n, 1};
+    } else if (s.workgroups != 1) {
+      join.side[i] = {sums, dw[i], s.workgroups, 1};
+    }
     bytes += (int64_t)a.tokens.total * heads * c.head_dim * 6;
   }
   const dim3 grid(a.side[0].workgroups + a.side[1].workgroups);
@@ -280,10 +342,11 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     });
     if (rc) return rc;
   }
-  if (join.dw[0] || join.dw[1]) {
-    if (c.head_dim == 128) join_kernel<128><<<2 * 128 / 16, 256, 0, st>>>(join);
-    else join_kernel<64><<<2 * 64 / 16, 256, 0, st>>>(join);
+  if (const uint32_t groups = runs.side[0].groups + runs.side[1].groups) {
+    if (c.head_dim == 128) runs_kernel<128><<<groups, 256, 0, st>>>(runs);
+    else runs_kernel<64><<<groups, 256, 0, st>>>(runs);
     RF2_LAUNCH_CHECK();
+    if (const int rc = launch_join(c.head_dim, join_runs, st)) return rc;
   }
-  return RF2_OK;
+  return launch_join(c.head_dim, join, st);
 }

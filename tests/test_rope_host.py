@@ -109,7 +109,7 @@ def test_weights_of_the_other_type_are_refused():
                                   dict(theta=1e-3), dict(axis_dims=(4, 2), inv_freq=(0.5, -0.25, 0.0), theta=-1.0)], ids=str)
 def test_sizes(over):
     p = make(**over)
-    assert p.info.workspace_bytes == (0 if p.cfg.norm == rf2.RF2_NORM_NONE else 2 * 1024 * 64 * 4)
+    assert p.info.workspace_bytes == (0 if p.cfg.norm == rf2.RF2_NORM_NONE else 2 * (8192 * 64 * 4 + 128 * 64 * 8))
     assert p.alloc_workspace("cpu").numel() == p.info.workspace_bytes
     p.close()
     p.close()
