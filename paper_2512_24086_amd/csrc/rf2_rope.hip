@@ -43,7 +43,7 @@ struct BackArgs {
 // 40 + 40 heads: 1,024 354 us, 4,096 336, 8,192 323, and 10 for their sums; sums by elements, read and written alike, take 312).  Smaller ones are
 // better off with 512, whose sums one launch adds up.
 template <class T, int D, bool HALVES, bool KEEP>
-__global__ void __launch_bounds__(256) backward_kernel(BackArgs a) {
+__global__ void __launch_bounds__(256, 4) backward_kernel(BackArgs a) {
   constexpr int CH = D / 8, R = 64 / CH, U = 2;
   __shared__ float part[4 * R][D + 4];
   const bool second = blockIdx.x >= a.side[0].workgroups;

@@ -569,15 +569,14 @@ class RopePlan:
             raise ValueError("q and k: expected one at least")
         batch, tokens, q_shape, k_shape = self._sizes(k if q is None else q)
         at, step = self._pos(pos, batch, tokens)
-        sides = []
-        for name, tensors, w, dw, shape in (("q", (q, dq_out, dq), wq, dwq, q_shape), ("k", (k, dk_out, dk), wk, dwk, k_shape)):
-            there = tensors != (None, None, None) if tensors[0] is None else True
-            if (dw is None) == (norm and there):
-                raise ValueError(f"dw{name}: expected " + ("the gradient of the weights" if dw is None else "none: there is no norm, or no rows that have it"))
-            sides.append(([self._rows(t, what, shape) for t, what in zip(tensors, (name, f"d{name}_out", f"d{name}"))] if there else [_NO_ROWS] * 3,
-                          self._weight(w, "w" + name, there), None if dw is None else _arg(dw, "dw" + name, torch.float32, self.cfg.head_dim, self.device)))
-        (qs, wq, dwq), (ks, wk, dwk) = sides
+        with_q, with_k = not (q is None and dq_out is None and dq is None), not (k is None and dk_out is None and dk is None)
+        if (dwq is None) == (norm and with_q) or (dwk is None) == (norm and with_k):
+            raise ValueError("dwq, dwk: expected the gradients of the weights where there is a norm and rows that have it, and none elsewhere")
+        rows, f32, d, dev = self._rows, torch.float32, self.cfg.head_dim, self.device
+        qs = (rows(q, "q", q_shape), rows(dq_out, "dq_out", q_shape), rows(dq, "dq", q_shape)) if with_q else (_NO_ROWS,) * 3
+        ks = (rows(k, "k", k_shape), rows(dk_out, "dk_out", k_shape), rows(dk, "dk", k_shape)) if with_k else (_NO_ROWS,) * 3
         _check(lib().rf2_rope_backward(
-            self._h, batch, tokens, _two_rows_thrice.pack(*qs[0], *ks[0], *qs[1], *ks[1], *qs[2], *ks[2]), at, step, wq, wk, dwq, dwk,
-            None if not norm or workspace is None else _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, self.device),
+            self._h, batch, tokens, _two_rows_thrice.pack(*qs[0], *ks[0], *qs[1], *ks[1], *qs[2], *ks[2]), at, step, self._weight(wq, "wq", with_q),
+            self._weight(wk, "wk", with_k), None if dwq is None else _arg(dwq, "dwq", f32, d, dev), None if dwk is None else _arg(dwk, "dwk", f32, d, dev),
+            _arg(workspace, "workspace", torch.uint8, self.info.workspace_bytes, dev) if norm and workspace is not None else None,
             self._stream(stream)), "rf2_rope_backward")

@@ -6,7 +6,7 @@ from tests.test_paged_kernel_resources import resources
 
 
 @pytest.mark.parametrize("source, instances, least", [
-    ("rf2_rope.hip", 54, dict(apply_kernel=6, backward_kernel=3, runs_kernel=8, join_kernel=8)),
+    ("rf2_rope.hip", 54, dict(apply_kernel=6, backward_kernel=4, runs_kernel=4, join_kernel=8)),
     ("rf2_permute_rope.hip", 28, dict(permute_rope_kernel=3, permute_v_kernel=8)),
     ("rf2_paged_store_rope.hip", 32, dict(store_rope_kernel=4)),
 ])
