@@ -163,3 +163,21 @@ def test_steps_of_a_program_eager_and_from_a_graph():
                 assert torch.equal(a, b), (i, "plain" if p is plain else "graph")
         for o in fused.o:
             assert (o[at:] == 7.0).all() and o[:at].isfinite().all()
+
+
+def test_offsets_beyond_32_bits():
+    # a cache of 5.2e9 elements, tokens in its last pages
+    c = Case(tokens=40, heads=8, kv=8, page=256, n_pages=20000)
+    size = c.plan.info.cache_elements
+    assert size > 2 ** 32
+    k_cache, v_cache = torch.zeros(size, dtype=BF16, device="cuda"), torch.zeros(size, dtype=BF16, device="cuda")
+    slots = (c.plan.cfg.n_pages * 256 - 1 - 3 * torch.arange(40)).int().cuda()
+    q_out, k_want = torch.empty_like(c.q), torch.empty_like(c.k)
+    c.plan.rf2_paged_store_rope(c.rope, c.q, c.k, c.v, c.pos, slots, k_cache, v_cache, q_out, *c.w)
+    c.rope.rf2_rope_apply(None, c.k, c.pos, None, k_want, None, c.w[1])
+    r = slots.long() % 256
+    page = slots.long() // 256
+    k = k_cache.view(-1, 8, 8, 16, 32, 8)[page, :, r // 32, :, r % 32]
+    v = v_cache.view(-1, 8, 8, 4, 128, 8)[page, :, r // 32, r % 32 // 16 * 2 + r % 8 // 4, :, r % 16 // 8 * 4 + r % 4]
+    assert torch.equal(k.reshape(40, 8, 128), k_want) and torch.equal(v, c.v)
+    assert int((k_cache != 0).sum()) <= 40 * 8 * 128 and int((v_cache != 0).sum()) <= 40 * 8 * 128

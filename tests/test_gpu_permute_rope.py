@@ -169,3 +169,26 @@ def test_graph():
         c.plan.layer_fused(c.q, c.k, c.v, eager, rope=c.rope, pos=c.pos, weights=weights)
         torch.cuda.synchronize()
         assert torch.equal(buf["o"], eager["o"]) and torch.equal(buf["blk_idx"], eager["blk_idx"]) and torch.equal(buf["qbar"], eager["qbar"]), rep
+
+
+def test_offsets_beyond_32_bits():
+    # 4.6 GB and 2.3e9 elements a tensor, token-major: rows of late tokens and heads lie behind both limits
+    heads, T, H, W = 150, 33, 45, 80
+    plan = rf2.Plan(batch=1, heads=heads, head_dim=128, T=T, H=H, W=W, block=128, sparsity=0.8, sink_frames=1, qkv_layout=BNHD)
+    rope = rf2.RopePlan(heads=heads, kv_heads=heads, head_dim=128, axis_dims=(44, 42, 42))
+    n = T * H * W
+    torch.manual_seed(0)
+    q, k, v = (torch.randn(1, n, heads, 128, dtype=BF16, device="cuda") for _ in range(3))
+    pos = torch.randint(0, 100, (n, 3), dtype=torch.int32, device="cuda")
+    w = [torch.randn(128, dtype=BF16, device="cuda") for _ in range(2)]
+    got, want = plan.alloc("cuda"), plan.alloc("cuda")
+    plan.rf2_permute_rope(rope, q, k, v, pos, got["qp"], got["kp"], got["vp"], got["qbar"], got["kbar"], *w)
+    rope.rf2_rope_apply(q, k, pos, q, k, *w)
+    plan.rf2_permute(q, k, v, want["qp"], want["kp"], want["vp"], want["qbar"], want["kbar"])
+    for name in ("qp", "kp", "vp"):
+        assert torch.equal(got[name], want[name]), name
+    for name in ("qbar", "kbar"):                              # rows before and behind their rounding: half a step of up to 8, averaged
+        assert (got[name] - want[name]).abs().max() < 2.0 ** -6, name
+    perm, _ = plan.rf2_plan_perm()
+    last = torch.from_numpy(perm[-300:].astype(np.int64)).cuda()
+    assert torch.equal(got["qp"][0, -1, n - 300:n], q[0, last, -1])

@@ -326,3 +326,48 @@ def test_many_rows_of_one_weight():
     # would be 1/1100 of this)
     assert ((dwq.double() - want).abs() <= 60 * ref.U * size + 1e-7 * want.abs()).all()
     assert ((dwq.double() - want).norm() / want.norm()).item() < 1e-5
+
+
+@pytest.mark.parametrize("tokens, heads, layout", [(1 << 24, 1, BNHD), (1 << 24, 1, BHND), (5, 65535, BNHD), (5, 65535, BHND), (70001, 300, BNHD)], ids=str)
+def test_the_largest_sizes(tokens, heads, layout):
+    # against calls of a few tokens, bit for bit
+    rope = rf2.RopePlan(heads=heads, kv_heads=1, head_dim=64, axis_dims=(40, 20), layout=layout)
+    torch.manual_seed(0)
+    shape = (tokens, heads, 64) if layout == BNHD else (heads, tokens, 64)
+    q = torch.randn(shape, dtype=BF16, device="cuda")
+    pos = torch.randint(-2 ** 31, 2 ** 31 - 1, (tokens, 2), dtype=torch.int32, device="cuda")
+    w = torch.randn(64, dtype=BF16, device="cuda")
+    out = torch.empty_like(q)
+    rope.rf2_rope_apply(q, None, pos, out, None, w)
+    few = sorted({0, 1, tokens // 3, tokens // 2 + 1, tokens - 2, tokens - 1})
+    for n in few:
+        row = q[n:n + 1] if layout == BNHD else q[:, n:n + 1]
+        one = torch.empty(row.shape, dtype=BF16, device="cuda")
+        rope.rf2_rope_apply(row, None, pos[n:n + 1], one, None, w)
+        assert torch.equal(out[n:n + 1] if layout == BNHD else out[:, n:n + 1], one), n
+    # gradients: of an output of zeros but for one token, the row's own and nothing else
+    dz, dx, dw, dw_one = torch.zeros_like(q), torch.full_like(q, 7.0), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    n = few[-2]
+    (dz[n:n + 1] if layout == BNHD else dz[:, n:n + 1]).normal_()
+    ws = rope.alloc_workspace()
+    rope.rf2_rope_backward(q, None, pos, dz, None, dx, None, w, None, dw, None, ws)
+    at = (slice(n, n + 1),) if layout == BNHD else (slice(None), slice(n, n + 1))
+    one = torch.empty(dz[at].shape, dtype=BF16, device="cuda")
+    rope.rf2_rope_backward(q[at], None, pos[n:n + 1], dz[at], None, one, None, w, None, dw_one, None, ws)
+    assert torch.equal(dx[at], one)
+    assert int((dx != 0).sum()) == int((one != 0).sum())
+    assert torch.allclose(dw, dw_one, rtol=1e-5, atol=1e-5 * dw_one.abs().max().item())          # (sums of up to 65,535 rows in another order)
+
+
+def test_batches_whose_elements_have_one_token():
+    # [batch, 1, heads, d], as a step of single tokens may come, strides of the axis of one of no account
+    c = Case(batch=37, tokens=1, heads=8, kv=2, own_pos=True)
+    want = c.forward()
+    flat = [x.view(37, x.shape[2], 128) for x in (c.q, c.k)]
+    out = [torch.empty_like(x) for x in flat]
+    c.plan.rf2_rope_apply(flat[0], flat[1], c.pos[:, 0].contiguous(), *out, c.wq, c.wk)
+    assert all(torch.equal(a, b[:, 0]) for a, b in zip(out, want))
+    odd = c.q.as_strided(c.q.shape, (c.q.stride(0), 3, 128, 1))
+    q_out = c.like(c.q)
+    c.plan.rf2_rope_apply(odd, None, c.pos, q_out, None, c.wq)
+    assert torch.equal(q_out, want[0])
