@@ -2,7 +2,9 @@
 //
 // HBM bound, or by the launch where tokens are few: every row is read once and written once.  The first workgroups do V as rf2_paged_store does,
 // the next K, the others Q as rf2_rope_apply does.  K goes from the registers in which it is rotated to its tiles: a wavefront has eight tokens, whose
-// 16-byte chunks stand side by side there, and goes through a few heads with their cosines and sines.
+// 16-byte chunks stand side by side there, and goes through a few heads with their cosines and sines.  (With K through LDS, head by head, as in
+// rf2_paged_store: 62.8 us for 4,680 tokens of 40 heads in place of 58.6, 7.7 for 48 single tokens in place of 6.3.)  288 MB in 58.6 us are 4.9 TB/s: V by itself
+// takes 21, K 26, of which half is for stores to lines that two wavefronts complete where slots do not begin with a line, Q 19.
 #include "rf2_paged_store.h"
 #include "rf2_rope.h"
 

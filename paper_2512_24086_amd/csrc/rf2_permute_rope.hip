@@ -3,7 +3,7 @@
 // HBM bound, like the permutation by itself: the same bytes are read and written, and a pass over Q and K before it is saved.  A workgroup takes
 // a block of rows through two heads, a wavefront 64 / (d / 8) rows at a time, d / 8 lanes to a row.  Cosines and sines belong to a token, so both
 // heads have them from one calculation, which is about as much work as a head's rows themselves (one head at a time: 75,600 tokens of 40 heads
-// 826 us, two 806, three 807, four 1,057; rf2_permute by itself 790).  Small layers, which the latency of a block bounds, ask for the
+// 826 us, two 806, three 807; rf2_permute by itself 790).  Small layers, which the latency of a block bounds, ask for the
 // rows of the next turn before they work on this one (4,301 tokens of 12 heads 18.7 -> 15.6 us); elsewhere the registers that it takes cost
 // wavefronts (64 channels, 32,760 tokens of 40 heads 191 -> 207).
 #include "rf2_permute_rows.h"

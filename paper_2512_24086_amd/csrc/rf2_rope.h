@@ -355,11 +355,11 @@ inline int rope_heads_log2(const rf2_rows& r, int heads, int rows) {
 
 // The share of each wavefront.  Angles are worked out once for all its steps (HALVES costs twice the exchange), loads of four steps are on their way
 // together, and what is read at a time should lie close together.  Measured (us, steps of a wavefront):
-//   heads side by side, 75,600 tokens x 40 + 40 heads      4 of 10: 511   5: 511   all: 541; groups slowest 557, 547, 541
-//     64 channels, 32,760 tokens x 40 + 40                 4 of 5: 119   all: 109;  HALVES, 20,000 x 32 + 8   4 of 8: 78   all: 73
-//   tokens side by side, 75,600 x 40 + 40                  1: 639   2: 507   3: 515   4: 526   8: 537   all: 586 (a copy of as much: 500)
-//     HALVES, 32,760 x 40 + 40                             2: 252   4: 234   5: 224   8: 231   all: 234
-//     4,096 x 12 + 12                                      2: 11.3  4: 9.4   8: 11.1;   1,000 x 40 + 40   2: 9.8   4: 8.2   all: 8.1
+//   heads side by side, 75,600 tokens x 40 + 40 heads      1: 641   2: 515   4 of 10: 511   5: 516   all: 541
+//     64 channels, 32,760 tokens x 40 + 40                 4 of 5: 115   all: 109;   HALVES, 20,000 x 32 + 8   4 of 8: 75   all: 72
+//   tokens side by side, 75,600 x 40 + 40                  1: 650   2: 496   3: 511   4: 518   8: 530   all: 582 (a copy of as much: 498)
+//     HALVES, 32,760 x 40 + 40                             2: 254   4: 229   5: 221   8: 228   all: 245
+//     4,096 x 12 + 12                                      2: 11.6  4: 9.5   8: 11.0;   1,000 x 40 + 40   2: 9.7   4: 8.1   all: 8.2
 // With few rows a wavefront takes fewer, so that there are 2,048.
 inline RopeShare rope_share(const rf2_rows& x, int heads, const rf2_rope_config& c, uint32_t tokens) {
   if (!x.at) return {heads, 0, 1, 0, 0, 1, 0};

@@ -2,7 +2,9 @@
 //
 // HBM bound: each row is read once and written once.  d / 8 neighbouring lanes hold a row, 16 bytes each.  Cosines and sines belong to a
 // token, not to a head: a wavefront takes a few tokens, works their angles out once and goes through the heads, 64 / (d / 8) rows at a
-// time.  Those are consecutive tokens of a head where tokens lie side by side, consecutive heads of a token where heads do.
+// time.  Those are consecutive tokens of a head where tokens lie side by side, consecutive heads of a token where heads do.  75,600 tokens of
+// 40 + 40 heads: 3.1 GB in 494 us, 6.3 TB/s (a large copy reaches 6.2); the vector unit is 77 % busy beside it.  48 tokens: 3.0 us in a graph, 8.2 with
+// the host's part of a call.
 #include "rf2_rope.h"
 
 namespace {
