@@ -220,8 +220,8 @@ int launch(const rf2_plan* plan, PermuteRopeArgs a, bool halves, uint32_t q_wgs,
     const uint32_t rows = (n + 65535u) / 65536u;
     return dim3((n + rows - 1) / rows, rows);
   };
-  const int64_t bytes = (3 * plan->info.N + plan->info.N_pad + 2 * plan->info.N_pad_k) * (int64_t)a.p.bh * D * 2;
-  const bool apart = bytes > KEEP_STORES && v_wgs > 0;
+  const int keep = rf2_permute_keep(plan, a.p.bh);
+  const bool apart = keep == 0 && v_wgs > 0;
   a.p.q_wgs = q_wgs, a.p.k_wgs = k_wgs, a.p.v_wgs = v_wgs;
   if (apart) {
     permute_v_kernel<D, BK, 0><<<grid(v_wgs), 256, 0, st>>>(a.p);
@@ -231,12 +231,12 @@ int launch(const rf2_plan* plan, PermuteRopeArgs a, bool halves, uint32_t q_wgs,
   if (q_wgs + k_wgs + a.p.v_wgs == 0) return RF2_OK;
   const auto with = [&](auto kernel) { kernel<<<grid(q_wgs + k_wgs + a.p.v_wgs), 256, 0, st>>>(a, plan->cfg.block); };
   if (halves) {
-    if (bytes <= KEEP_ALL) with(permute_rope_kernel<D, BK, true, 2>);
-    else if (bytes <= KEEP_STORES) with(permute_rope_kernel<D, BK, true, 1>);
+    if (keep == 2) with(permute_rope_kernel<D, BK, true, 2>);
+    else if (keep == 1) with(permute_rope_kernel<D, BK, true, 1>);
     else with(permute_rope_kernel<D, BK, true, 0>);
   } else {
-    if (bytes <= KEEP_ALL) with(permute_rope_kernel<D, BK, false, 2>);
-    else if (bytes <= KEEP_STORES) with(permute_rope_kernel<D, BK, false, 1>);
+    if (keep == 2) with(permute_rope_kernel<D, BK, false, 2>);
+    else if (keep == 1) with(permute_rope_kernel<D, BK, false, 1>);
     else with(permute_rope_kernel<D, BK, false, 0>);
   }
   RF2_LAUNCH_CHECK();

@@ -2,25 +2,15 @@
 #pragma once
 #include "rf2_internal.h"
 
+// KEEP of a layer of `bh` heads in all (rf2_permute.hip)
+int rf2_permute_keep(const rf2_plan* plan, int64_t bh);
+
 namespace {
 
 typedef unsigned short u16;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
-// Every row is read once and written once: non-temporal accesses keep the stream from displacing
-// other data in the caches on its way (measured on the 720p layer: loads alone -4 %, stores alone
-// +0.5 %, both -9 % of the time).  Layers small beside the Infinity Cache (256 MB) are better kept in it: the attention
-// finds qp, kp, vp there, and the inputs, which the program has just made, are.  Measured on image layers of 4,096 tokens, the
-// buffers of three layers in turn (us, layer / permutation alone; bytes read and written):
-//   non-temporal     stores kept      both kept
-//   70.5 /  -        67.4 /  -        64.6 /  -         10 heads,  63 MB
-//   76.6 / 15.3      75.2 / 15.8      73.4 / 12.6       12 heads,  75 MB
-//   91.2 / 19.3      88.6 / 18.8      89.6 / 21.8       16 heads, 101 MB
-//   145  / 28.7      140  / 28.5      140  / 31.3       24 heads, 151 MB
-//   169  / 36.6      165  / 38.5      166  / 40.5       32 heads, 201 MB
-// Both are kept up to 80 MiB (84 MB), stores alone up to 160 MiB (168 MB; beyond, the permutation itself gets slower, up to 8 %).
-// Bytes read and written, rows of the last, partly filled blocks included.
-constexpr int64_t KEEP_ALL = (int64_t)80 << 20, KEEP_STORES = (int64_t)160 << 20;
+// KEEP 0: every row is read and written past the caches, 1: stores are kept there, 2: loads too
 template <bool KEEP>
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   const u32x4* const from = reinterpret_cast<const u32x4*>(p);
