@@ -6,13 +6,15 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int TOKENS = 32, MORE = 11, ROWS = TOKENS + MORE;
+constexpr int STORE_TOKENS = 32;
 
-// 16-bit values are moved, whatever they stand for.  K may be left out.
-template <int D, bool WITH_K>
+// A workgroup has TOKENS tokens of a K/V head; MORE rows of V are those that groups of its last tokens may need.  16-bit values are moved, whatever
+// they stand for.  K may be left out.
+template <int D, bool WITH_K, int TOKENS>
 __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t k_stride, int64_t v_stride,
                                            const int32_t* __restrict__ slots, int n_tokens, int64_t n_slots, int page_shift, int kv_heads, unsigned windows,
                                            unsigned run, uint16_t* __restrict__ k_cache, uint16_t* __restrict__ v_cache, unsigned group) {
+  constexpr int MORE = 11, ROWS = TOKENS + MORE;
   constexpr int C = D / 8, PITCH = D + 8;                       // 16-byte chunks of a row; LDS rows are 16 bytes further apart
   __shared__ __attribute__((aligned(16))) uint16_t k_rows[WITH_K ? TOKENS * PITCH : 1], v_rows[ROWS * PITCH];
   __shared__ int32_t slot_of[MORE + ROWS];
@@ -26,7 +28,7 @@ __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const
   const int count = (int)min((int64_t)TOKENS, n_tokens - n0), more = (int)min((int64_t)ROWS, n_tokens - n0);
   const int64_t column = (int64_t)head * D;
   // (rows are read once: marked as not to be kept, they leave the caches to what is written; 4,680 tokens of 40 heads 47.1 -> 36.0 us)
-  u32x4 x[TOKENS * C / 256], y[(ROWS * C + 255) / 256];
+  u32x4 x[WITH_K ? TOKENS * C / 256 : 1], y[(ROWS * C + 255) / 256];
 #pragma unroll
   for (int i = 0; i < TOKENS * C / 256 && WITH_K; ++i) {
     const int r = min((i * 256 + tid) / C, count - 1);

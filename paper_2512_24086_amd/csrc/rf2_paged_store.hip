@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(256) store_kernel(const uint16_t* __restrict__
                                                     int64_t v_stride, const int32_t* __restrict__ slots, int n_tokens, int64_t n_slots,
                                                     int page_shift, int kv_heads, unsigned windows, unsigned run, uint16_t* __restrict__ k_cache,
                                                     uint16_t* __restrict__ v_cache) {
-  store_rows<D, true>(k, v, k_stride, v_stride, slots, n_tokens, n_slots, page_shift, kv_heads, windows, run, k_cache, v_cache, blockIdx.x);
+  store_rows<D, true, STORE_TOKENS>(k, v, k_stride, v_stride, slots, n_tokens, n_slots, page_shift, kv_heads, windows, run, k_cache, v_cache, blockIdx.x);
 }
 
 }  // namespace
@@ -34,7 +34,7 @@ extern "C" int rf2_paged_store(const rf2_paged_plan* plan, int32_t n_tokens, con
   if (k_stride % 8 != 0 || v_stride % 8 != 0) return RF2_ERR_INVALID_ARG;
   if (!rf2_aligned(k, 16) || !rf2_aligned(v, 16) || !rf2_aligned(k_cache, 16) || !rf2_aligned(v_cache, 16) || !rf2_aligned(slots, 4))
     return RF2_ERR_INVALID_ARG;
-  const unsigned windows = (unsigned)(n_tokens + TOKENS - 1) / TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
+  const unsigned windows = (unsigned)(n_tokens + STORE_TOKENS - 1) / STORE_TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
   if (run >= 1u << 21) return RF2_ERR_UNSUPPORTED;         // (a grid has less than 2^32 threads)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;

@@ -3,12 +3,18 @@
 // HBM bound, or by the launch where tokens are few: every row is read once and written once.  The first workgroups do V as rf2_paged_store does,
 // the next K, the others Q as rf2_rope_apply does.  K goes from the registers in which it is rotated to its tiles: a wavefront has eight tokens, whose
 // 16-byte chunks stand side by side there, and goes through a few heads with their cosines and sines.  (With K through LDS, head by head, as in
-// rf2_paged_store: 62.8 us for 4,680 tokens of 40 heads in place of 58.6, 7.7 for 48 single tokens in place of 6.3.)  288 MB in 58.6 us are 4.9 TB/s: V by itself
-// takes 21, K 26, of which half is for stores to lines that two wavefronts complete where slots do not begin with a line, Q 19.
+// rf2_paged_store: 62.8 us for 4,680 tokens of 40 heads in place of 58.6; 48 single tokens, with V's still 32 to a workgroup, 7.7 in place of 6.3.)
+// 288 MB in 58.6 us are 4.9 TB/s: V by itself takes 21, K 26, of which half is for stores to lines that two wavefronts complete where slots do not
+// begin with a line, Q 19.
 #include "rf2_paged_store.h"
 #include "rf2_rope.h"
 
 namespace {
+
+// Tokens of a workgroup for K, and for V where there are many.  V of single tokens goes out key by key, one behind the other, so V's workgroups have 8
+// as long as there are no more of them than compute units.  us in a graph, 32 and 8 to a workgroup: 48 single tokens on 8 heads 6.2, 3.7, 200 of them
+// 7.1, 4.7, 48 on 40 heads 7.2, 4.7, a run of 200 on 8 heads 4.3, 3.9; beyond: 256 single tokens on 40 heads 13.9, 16.4, a run of 500 on 8 5.8, 6.4.
+constexpr int MANY = STORE_TOKENS, FEW = 8, COMPUTE_UNITS = 256;
 
 struct StoreRopeArgs {
   const uint16_t *k, *v;
@@ -16,14 +22,15 @@ struct StoreRopeArgs {
   const int32_t* slots;
   int n_tokens, page_shift, kv_heads;
   int64_t n_slots;
-  unsigned windows, run;
+  int few;                           // V's tokens FEW at a time
+  unsigned windows, run;             // of V
   uint16_t *k_cache, *v_cache;
   RopeArgs rope;
   const int32_t* pos;
   const void* wk;
   int norm;
   int k_steps;                       // heads of a wavefront
-  unsigned k_workgroups;
+  unsigned k_windows, k_workgroups;
   const int32_t* n_live;             // tokens that are not padding, or NULL
   RopeSide q;
 };
@@ -31,9 +38,9 @@ struct StoreRopeArgs {
 template <class T, int D, bool HALVES, bool NORM>
 __device__ __forceinline__ void store_k(const StoreRopeArgs& a, unsigned id) {
   constexpr int C = D / 8, SETS = C / 8, AHEAD = 2;              // sets of rows of a wavefront
-  const unsigned group = id / a.windows, window = id - group * a.windows;
+  const unsigned group = id / a.k_windows, window = id - group * a.k_windows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % C, g = lane / C;
-  const int first = (int)window * TOKENS + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
+  const int first = (int)window * MANY + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
   if (first >= a.n_tokens) return;
   const uint16_t* from[SETS];
   u32x4 v[AHEAD][SETS];
@@ -96,7 +103,11 @@ template <class T, int D, bool HALVES, bool NORM, bool KEEP>
 __global__ void __launch_bounds__(256) store_rope_kernel(StoreRopeArgs a) {
   unsigned id = blockIdx.x;
   if (id < 8 * a.run) {
-    store_rows<D, false>(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache, a.v_cache, id);
+    const auto rows = [&](auto tokens) {
+      store_rows<D, false, tokens()>(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache,
+                                     a.v_cache, id);
+    };
+    a.few ? rows(std::integral_constant<int, FEW>()) : rows(std::integral_constant<int, MANY>());
     return;
   }
   id -= 8 * a.run;
@@ -130,8 +141,8 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
     if (!rf2_aligned(t, 16)) return RF2_ERR_INVALID_ARG;
   if (!rf2_aligned(slots, 4) || !rf2_aligned(n_live, 4)) return RF2_ERR_INVALID_ARG;
   if (n_tokens > 0 && (!rf2_rope_pos_fits(rope, pos) || !rf2_rope_weight_fits(rope, wq) || !rf2_rope_weight_fits(rope, wk))) return RF2_ERR_INVALID_ARG;
-  const unsigned windows = (unsigned)(n_tokens + TOKENS - 1) / TOKENS, run = (windows * (unsigned)c.kv_heads + 7) / 8;
-  if (run >= 1u << 20) return RF2_ERR_UNSUPPORTED;           // (a grid has less than 2^32 threads, half of them for V and K)
+  const unsigned k_windows = (unsigned)(n_tokens + MANY - 1) / MANY;
+  if ((k_windows * (unsigned)c.kv_heads + 7) / 8 >= 1u << 20) return RF2_ERR_UNSUPPORTED;   // (a grid has less than 2^32 threads, half of them for V and K)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;
   const rf2_rows q_rows{q, 0, n_tokens > 1 ? q_stride : q_row, c.head_dim}, out_rows{q_out, 0, n_tokens > 1 ? q_out_stride : q_row, c.head_dim};
@@ -139,10 +150,13 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
   // K's wavefronts take as many heads as leave 2,048 of them, four (HALVES: five) at most
   const int64_t k_work = (int64_t)((n_tokens + 7) / 8) * c.kv_heads;
   const int k_steps = (int)std::min<int64_t>(r.pairing == RF2_ROPE_HALVES ? 5 : 4, std::max<int64_t>(1, k_work / 2048));
-  const unsigned k_workgroups = windows * (unsigned)((c.kv_heads + k_steps - 1) / k_steps);
+  const unsigned k_workgroups = k_windows * (unsigned)((c.kv_heads + k_steps - 1) / k_steps);
+  const unsigned few_windows = (unsigned)(n_tokens + FEW - 1) / FEW;
+  const bool few = (int64_t)few_windows * c.kv_heads <= COMPUTE_UNITS;
+  const unsigned windows = few ? few_windows : k_windows, run = (windows * (unsigned)c.kv_heads + 7) / 8;
   const StoreRopeArgs a{(const uint16_t*)k, (const uint16_t*)v, k_stride, v_stride, slots, n_tokens, __builtin_ctz((unsigned)c.page), c.kv_heads,
-                        (int64_t)c.n_pages * c.page, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
-                        r.norm == RF2_NORM_RMS, k_steps, k_workgroups, n_live, side};
+                        (int64_t)c.n_pages * c.page, few, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
+                        r.norm == RF2_NORM_RMS, k_steps, k_windows, k_workgroups, n_live, side};
   const dim3 grid(8 * run + k_workgroups + rope_workgroups(side.share));
   const bool keep = (int64_t)n_tokens * q_row * 4 <= ROPE_KEEP;
   hipStream_t st = (hipStream_t)stream;

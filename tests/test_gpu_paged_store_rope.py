@@ -57,6 +57,28 @@ def test_equals_the_two_calls(case):
     Case(**case).both()
 
 
+@pytest.mark.parametrize("slots", ["run", "single", "threes", "backwards", "mixed"])
+@pytest.mark.parametrize("tokens,kv,d", [(8, 8, 128), (9, 8, 128), (48, 8, 128), (256, 8, 128), (257, 8, 128), (48, 40, 128), (49, 40, 128), (256, 8, 64), (264, 8, 64), (2048, 1, 128),
+                                         (2049, 1, 64)])
+def test_workgroups_of_few_and_of_many_tokens(tokens, kv, d, slots):
+    # V is stored eight tokens to a workgroup up to 256 workgroups: both sides, with keys of V that go out whole and one by one
+    c = Case(tokens=tokens, heads=kv, kv=kv, d=d, dims=(d,), n_pages=tokens // 4 + 6)
+    i = torch.arange(tokens)
+    order = torch.randperm(c.plan.cfg.n_pages, generator=torch.Generator().manual_seed(1))
+    if slots == "single":                                     # sixteen keys apart
+        at = i * 16 + 5
+    elif slots == "threes":
+        at = i // 3 * 32 + i % 3 + 7
+    elif slots == "backwards":
+        at = tokens + 20 - i
+    else:
+        at = i + 5
+    at = order[at // 64] * 64 + at % 64
+    if slots == "mixed":                                      # a third of a run is padding
+        at = torch.where(torch.rand(tokens, generator=torch.Generator().manual_seed(2)) < 0.3, -1, at)
+    c.both(slots=at.int().cuda())
+
+
 @pytest.mark.parametrize("live", [0, 1, 30, 50])
 def test_padding_stays(live):
     c = Case(tokens=50)
