@@ -362,7 +362,7 @@ inline int rope_heads_log2(const rf2_rows& r, int heads, int rows) {
 //     4,096 x 12 + 12                                      2: 11.6  4: 9.5   8: 11.0;   1,000 x 40 + 40   2: 9.7   4: 8.1   all: 8.2
 // With few rows a wavefront takes fewer, so that there are 2,048.
 inline RopeShare rope_share(const rf2_rows& x, int heads, const rf2_rope_config& c, uint32_t tokens) {
-  if (!x.at) return {heads, 0, 1, 0, 0, 1, 0};
+  if (!x.at || tokens == 0) return {heads, 0, 1, 0, 0, 1, 0};
   const int rows = 512 / c.head_dim, log2 = rope_heads_log2(x, heads, rows), all_steps = heads >> log2;
   const int64_t wavefronts = (((int64_t)tokens << log2) + rows - 1) / rows, work = wavefronts * all_steps;
   const bool halves = c.pairing == RF2_ROPE_HALVES, along_tokens = x.token < x.head;

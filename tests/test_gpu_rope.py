@@ -202,6 +202,21 @@ def test_nothing_to_do():
     assert (dw[0] == 0).all() and (dw[1] == 0).all()            # sums over no rows
 
 
+@pytest.mark.parametrize("batch,tokens", [(0, 5), (2, 0), (0, 0)])
+@pytest.mark.parametrize("layout", [BHND, BNHD])
+def test_nothing_to_do_with_rows_that_have_an_address(batch, tokens, layout):
+    # torch's empty tensors have none; those of other programs may
+    plan, at = rf2.RopePlan(heads=4, kv_heads=2, head_dim=128, axis_dims=(128,)), torch.full((4096,), 9.0, dtype=BF16, device="cuda")
+    token, head = (128, 128 * 5) if layout == BHND else (128 * 4, 128)
+    rows, dw = (at.data_ptr(), 128 * 5 * 4, token, head), [torch.full((128,), 9.0, device="cuda") for _ in range(2)]
+    pos, w, workspace = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.ones(128, dtype=BF16, device="cuda"), plan.alloc_workspace()
+    stream = torch.cuda.current_stream().cuda_stream
+    assert rf2.lib().rf2_rope_apply(plan._h, batch, tokens, rf2.struct.pack("=" + "Qqqq" * 4, *rows * 4), pos.data_ptr(), 0, w.data_ptr(), w.data_ptr(), stream) == 0
+    assert rf2.lib().rf2_rope_backward(plan._h, batch, tokens, rf2.struct.pack("=" + "Qqqq" * 6, *rows * 6), pos.data_ptr(), 0, w.data_ptr(), w.data_ptr(),
+                                       dw[0].data_ptr(), dw[1].data_ptr(), workspace.data_ptr(), stream) == 0
+    assert (at == 9.0).all() and (dw[0] == 0).all() and (dw[1] == 0).all()
+
+
 def test_rows_of_zeros_and_rows_that_are_not_finite():
     c = Case(tokens=12, heads=2, kv=2)
     c.q[:, 3] = 0
