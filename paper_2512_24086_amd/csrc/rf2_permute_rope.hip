@@ -110,11 +110,13 @@ __device__ __forceinline__ void rope_rows_of(const PermuteRopeArgs& a, int rows,
       float y[8];
       RopeBf16::unpack(now[i], y);
       rope_row<D, HALVES, NORM>(a.rope, A, B, y);
+      if constexpr (RAGGED) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = behind ? 0.f : y[e];      // rows behind the last are 0: not -0, and whatever the weights are
+      }
       now[i] = RopeBf16::pack(y);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[i][e] += y[e];
-      if constexpr (RAGGED)
-        if (behind) now[i] = rope_u32x4{0, 0, 0, 0};         // rows behind the last are 0, not -0
     }
     const auto to = [&](int i) { return xp + ((int64_t)(b * p.heads + h0 + i) * n_blocks + blk) * rows * D; };
     const auto k_slot = [&](int r, int chunk) { return ((r % half) / 32 * CH + chunk) * 64 + r / half * 32 + r % 32; };

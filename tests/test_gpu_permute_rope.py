@@ -113,6 +113,21 @@ def test_equals_the_two_calls_and_its_means_the_formulas(case):
         assert torch.equal(buf[name].view(torch.int16), want[name].view(torch.int16)), name
 
 
+@pytest.mark.parametrize("halves", [False, True])
+def test_rows_behind_the_last_are_zeros_whatever_the_weights_are(halves):
+    # 850 tokens of which the last 200 are text: the last block has 82 rows of text and 46 behind them
+    c = Case(text=200, halves=halves)
+    want, buf = filled(c.plan), filled(c.plan)
+    c.permute(want)
+    c.w = [torch.full_like(w, float("inf")) for w in c.w]
+    c.permute(buf)
+    for name in ("qbar", "kbar"):
+        got, last = buf[name].view(5, -1, 128), want[name].view(5, -1, 128)[:, -1]
+        assert torch.equal(got[:, -1], last) and not got[:, 0].isfinite().any(), name
+    assert torch.equal(buf["qp"].view(5, -1, 128, 128)[:, -1], want["qp"].view(5, -1, 128, 128)[:, -1])
+    assert torch.equal(buf["kp"].view(5, -1, 128, 128)[:, -1], want["kp"].view(5, -1, 128, 128)[:, -1])
+
+
 @pytest.mark.parametrize("layout", [BHND, BNHD])
 def test_outputs_over_inputs(layout):
     # kp over q, vp over k, as for a caller short of memory: three launches, the same values (16 blocks, none partly filled)
