@@ -8,17 +8,25 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int STORE_TOKENS = 32;
 
-// A workgroup has TOKENS tokens of a K/V head; MORE rows of V are those that groups of its last tokens may need.  16-bit values are moved, whatever
-// they stand for.  K may be left out.
+constexpr int MORE = 11;                                        // rows of V that groups of a workgroup's last tokens may need
+template <int D, bool WITH_K, int TOKENS>
+struct StoreLds {
+  static constexpr int PITCH = D + 8;                           // rows are 16 bytes further apart
+  __attribute__((aligned(16))) uint16_t k_rows[WITH_K ? TOKENS * PITCH : 8];
+  __attribute__((aligned(16))) uint16_t v_rows[(TOKENS + MORE) * PITCH];
+  int32_t slot_of[2 * MORE + TOKENS];
+  int32_t todo[TOKENS + 1];                                     // tokens of V that lead a group, four keys, or none; how many
+};
+
+// A workgroup has TOKENS tokens of a K/V head, 64 at most.  16-bit values are moved, whatever they stand for.  K may be left out.
 template <int D, bool WITH_K, int TOKENS>
 __device__ __forceinline__ void store_rows(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t k_stride, int64_t v_stride,
                                            const int32_t* __restrict__ slots, int n_tokens, int64_t n_slots, int page_shift, int kv_heads, unsigned windows,
-                                           unsigned run, uint16_t* __restrict__ k_cache, uint16_t* __restrict__ v_cache, unsigned group) {
-  constexpr int MORE = 11, ROWS = TOKENS + MORE;
-  constexpr int C = D / 8, PITCH = D + 8;                       // 16-byte chunks of a row; LDS rows are 16 bytes further apart
-  __shared__ __attribute__((aligned(16))) uint16_t k_rows[WITH_K ? TOKENS * PITCH : 1], v_rows[ROWS * PITCH];
-  __shared__ int32_t slot_of[MORE + ROWS];
-  __shared__ int32_t todo[TOKENS + 1];                          // tokens of V that lead a group, four keys, or none; how many
+                                           unsigned run, uint16_t* __restrict__ k_cache, uint16_t* __restrict__ v_cache, unsigned group,
+                                           StoreLds<D, WITH_K, TOKENS>& lds) {
+  constexpr int ROWS = TOKENS + MORE, C = D / 8, PITCH = StoreLds<D, WITH_K, TOKENS>::PITCH;      // 16-byte chunks of a row
+  uint16_t *const k_rows = lds.k_rows, *const v_rows = lds.v_rows;
+  int32_t *const slot_of = lds.slot_of, *const todo = lds.todo;
   // Workgroups with equal number % 8 share an XCD: each XCD gets a run of windows head by head, so that lines which two
   // windows write in parts are completed in its L2.
   const unsigned at = (group & 7) * run + (group >> 3);

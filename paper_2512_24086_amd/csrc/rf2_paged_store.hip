@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(256) store_kernel(const uint16_t* __restrict__
                                                     int64_t v_stride, const int32_t* __restrict__ slots, int n_tokens, int64_t n_slots,
                                                     int page_shift, int kv_heads, unsigned windows, unsigned run, uint16_t* __restrict__ k_cache,
                                                     uint16_t* __restrict__ v_cache) {
-  store_rows<D, true, STORE_TOKENS>(k, v, k_stride, v_stride, slots, n_tokens, n_slots, page_shift, kv_heads, windows, run, k_cache, v_cache, blockIdx.x);
+  __shared__ StoreLds<D, true, STORE_TOKENS> lds;
+  store_rows(k, v, k_stride, v_stride, slots, n_tokens, n_slots, page_shift, kv_heads, windows, run, k_cache, v_cache, blockIdx.x, lds);
 }
 
 }  // namespace

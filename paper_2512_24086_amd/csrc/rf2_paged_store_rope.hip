@@ -11,10 +11,12 @@
 
 namespace {
 
-// Tokens of a workgroup for K, and for V where there are many.  V of single tokens goes out key by key, one behind the other, so V's workgroups have 8
-// as long as there are no more of them than compute units.  us in a graph, 32 and 8 to a workgroup: 48 single tokens on 8 heads 6.2, 3.7, 200 of them
-// 7.1, 4.7, 48 on 40 heads 7.2, 4.7, a run of 200 on 8 heads 4.3, 3.9; beyond: 256 single tokens on 40 heads 13.9, 16.4, a run of 500 on 8 5.8, 6.4.
-constexpr int MANY = STORE_TOKENS, FEW = 8, COMPUTE_UNITS = 256;
+// Tokens of a workgroup of K, and of V.  V's read 11 rows more than they have, so 64 tokens are better than 32 where there are enough of them for all
+// compute units, COMPUTE_UNITS (us in a graph, 32 and 64: 4,680 tokens of 40 heads 59.4, 57.2, 1,000 18.8, 17.6, 8,000 of 8 39.8, 38.4).  V of single
+// tokens goes out key by key, one behind the other, so fewer are 32 to a workgroup (512 single tokens on 8 heads 8.7, 64: 12.4), or 8 as long as those are
+// no more than compute units (32 and 8: 48 single tokens on 8 heads 6.2, 3.7, 200 7.1, 4.7, 48 on 40 heads 7.2, 4.7, a run of 200 on 8 4.3, 3.9; beyond:
+// 256 single tokens on 40 heads 13.9, 16.4, a run of 500 on 8 5.8, 6.4).
+constexpr int K_TOKENS = 32, COMPUTE_UNITS = 256;
 
 struct StoreRopeArgs {
   const uint16_t *k, *v;
@@ -22,7 +24,7 @@ struct StoreRopeArgs {
   const int32_t* slots;
   int n_tokens, page_shift, kv_heads;
   int64_t n_slots;
-  int few;                           // V's tokens FEW at a time
+  int v_tokens;                      // of a workgroup, 8, 32 or 64
   unsigned windows, run;             // of V
   uint16_t *k_cache, *v_cache;
   RopeArgs rope;
@@ -40,7 +42,7 @@ __device__ __forceinline__ void store_k(const StoreRopeArgs& a, unsigned id) {
   constexpr int C = D / 8, SETS = C / 8, AHEAD = 2;              // sets of rows of a wavefront
   const unsigned group = id / a.k_windows, window = id - group * a.k_windows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % C, g = lane / C;
-  const int first = (int)window * MANY + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
+  const int first = (int)window * K_TOKENS + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
   if (first >= a.n_tokens) return;
   const uint16_t* from[SETS];
   u32x4 v[AHEAD][SETS];
@@ -101,13 +103,17 @@ __device__ __forceinline__ void store_k(const StoreRopeArgs& a, unsigned id) {
 
 template <class T, int D, bool HALVES, bool NORM, bool KEEP>
 __global__ void __launch_bounds__(256) store_rope_kernel(StoreRopeArgs a) {
+  __shared__ union {
+    StoreLds<D, false, 8> few;
+    StoreLds<D, false, 32> some;
+    StoreLds<D, false, 64> many;
+  } lds;
   unsigned id = blockIdx.x;
   if (id < 8 * a.run) {
-    const auto rows = [&](auto tokens) {
-      store_rows<D, false, tokens()>(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache,
-                                     a.v_cache, id);
+    const auto rows = [&](auto& part) {
+      store_rows(a.k, a.v, a.k_stride, a.v_stride, a.slots, a.n_tokens, a.n_slots, a.page_shift, a.kv_heads, a.windows, a.run, a.k_cache, a.v_cache, id, part);
     };
-    a.few ? rows(std::integral_constant<int, FEW>()) : rows(std::integral_constant<int, MANY>());
+    a.v_tokens == 64 ? rows(lds.many) : a.v_tokens == 32 ? rows(lds.some) : rows(lds.few);
     return;
   }
   id -= 8 * a.run;
@@ -141,7 +147,7 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
     if (!rf2_aligned(t, 16)) return RF2_ERR_INVALID_ARG;
   if (!rf2_aligned(slots, 4) || !rf2_aligned(n_live, 4)) return RF2_ERR_INVALID_ARG;
   if (n_tokens > 0 && (!rf2_rope_pos_fits(rope, pos) || !rf2_rope_weight_fits(rope, wq) || !rf2_rope_weight_fits(rope, wk))) return RF2_ERR_INVALID_ARG;
-  const unsigned k_windows = (unsigned)(n_tokens + MANY - 1) / MANY;
+  const unsigned k_windows = (unsigned)(n_tokens + K_TOKENS - 1) / K_TOKENS;
   if ((k_windows * (unsigned)c.kv_heads + 7) / 8 >= 1u << 20) return RF2_ERR_UNSUPPORTED;   // (a grid has less than 2^32 threads, half of them for V and K)
   if (const int rc = rf2_check_paged_device(plan)) return rc;
   if (n_tokens == 0) return RF2_OK;
@@ -151,11 +157,11 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
   const int64_t k_work = (int64_t)((n_tokens + 7) / 8) * c.kv_heads;
   const int k_steps = (int)std::min<int64_t>(r.pairing == RF2_ROPE_HALVES ? 5 : 4, std::max<int64_t>(1, k_work / 2048));
   const unsigned k_workgroups = k_windows * (unsigned)((c.kv_heads + k_steps - 1) / k_steps);
-  const unsigned few_windows = (unsigned)(n_tokens + FEW - 1) / FEW;
-  const bool few = (int64_t)few_windows * c.kv_heads <= COMPUTE_UNITS;
-  const unsigned windows = few ? few_windows : k_windows, run = (windows * (unsigned)c.kv_heads + 7) / 8;
+  const auto v_workgroups = [&](int tokens) { return (int64_t)((n_tokens + tokens - 1) / tokens) * c.kv_heads; };
+  const int v_tokens = v_workgroups(8) <= COMPUTE_UNITS ? 8 : v_workgroups(64) < COMPUTE_UNITS ? 32 : 64;
+  const unsigned windows = (unsigned)(n_tokens + v_tokens - 1) / v_tokens, run = (unsigned)((v_workgroups(v_tokens) + 7) / 8);
   const StoreRopeArgs a{(const uint16_t*)k, (const uint16_t*)v, k_stride, v_stride, slots, n_tokens, __builtin_ctz((unsigned)c.page), c.kv_heads,
-                        (int64_t)c.n_pages * c.page, few, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
+                        (int64_t)c.n_pages * c.page, v_tokens, windows, run, (uint16_t*)k_cache, (uint16_t*)v_cache, rope_args(rope), pos, wk,
                         r.norm == RF2_NORM_RMS, k_steps, k_windows, k_workgroups, n_live, side};
   const dim3 grid(8 * run + k_workgroups + rope_workgroups(side.share));
   const bool keep = (int64_t)n_tokens * q_row * 4 <= ROPE_KEEP;
