@@ -3,9 +3,8 @@
 // HBM bound, or by the launch where tokens are few: every row is read once and written once.  The first workgroups do V as rf2_paged_store does,
 // the next K, the others Q as rf2_rope_apply does.  K goes from the registers in which it is rotated to its tiles: a wavefront has eight tokens, whose
 // 16-byte chunks stand side by side there, and goes through a few heads with their cosines and sines.  (With K through LDS, head by head, as in
-// rf2_paged_store: 62.8 us for 4,680 tokens of 40 heads in place of 58.6; 48 single tokens, with V's still 32 to a workgroup, 7.7 in place of 6.3.)
-// 288 MB in 58.6 us are 4.9 TB/s: V by itself takes 21, K 26, of which half is for stores to lines that two wavefronts complete where slots do not
-// begin with a line, Q 19.
+// rf2_paged_store, 62.8 us for 4,680 tokens of 40 heads where this way took 58.6.)  288 MB in 52.2 us are 5.5 TB/s; by themselves V takes 21, K 23,
+// Q 20.  Stores of K and V stay in the caches, for the attention (past them 56.1).
 #include "rf2_paged_store.h"
 #include "rf2_rope.h"
 
@@ -42,63 +41,81 @@ __device__ __forceinline__ void store_k(const StoreRopeArgs& a, unsigned id) {
   constexpr int C = D / 8, SETS = C / 8, AHEAD = 2;              // sets of rows of a wavefront
   const unsigned group = id / a.k_windows, window = id - group * a.k_windows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % C, g = lane / C;
-  const int first = (int)window * K_TOKENS + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
-  if (first >= a.n_tokens) return;
-  const uint16_t* from[SETS];
-  u32x4 v[AHEAD][SETS];
-#pragma unroll
-  for (int s = 0; s < SETS; ++s) {
-    from[s] = a.k + min(first + 4 * s + g, a.n_tokens - 1) * a.k_stride + (int64_t)h0 * D + 8 * c;
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(i, end - 1 - h0) * D));
+  const int at = (int)window * K_TOKENS + 8 * wave, h0 = (int)group * a.k_steps, end = min(a.kv_heads, h0 + a.k_steps);
+  if (at >= a.n_tokens) return;
+  // In large calls a wavefront's tokens begin with the first of the eight keys that share lines with token `at`, where that is a few tokens before:
+  // within a run they are eight whose lines are theirs alone, at its ends 1 to 15 (4,680 tokens of 40 heads 57.1 -> 53.4 us, 1,000 16.9 -> 16.4, but 1,000
+  // of 8 heads, which wait for the slots, 8.2 -> 9.3).
+  int begin = at, last = min(at + 8, a.n_tokens);
+  if (a.k_steps > 1) {
+    const int near = a.slots[min(max(at - 8 + min(lane, 23), 0), a.n_tokens - 1)];                   // of the tokens from at - 8 to at + 15
+    const auto early = [&](int i) {
+      const int slot = __builtin_amdgcn_readlane(near, i), before = slot & 7;
+      return slot >= 0 && before <= at + i - 8 && __builtin_amdgcn_readlane(near, i - before) == slot - before ? before : 0;
+    };
+    begin -= early(8);
+    if (last < a.n_tokens) last -= early(16);
   }
-  // the token whose rows a lane stores (below), and where
-  const int mine = first + (SETS == 2 ? 4 * (c / 8) : 0) + g;
-  const int slot = mine < a.n_tokens ? a.slots[mine] : -1;
-  const bool store = slot >= 0 && slot < a.n_slots;
-  const int page = slot >> a.page_shift, r = slot & ((1 << a.page_shift) - 1);
-  const int64_t head = (int64_t)D << a.page_shift;               // elements of a head of a page
-  uint16_t* to = a.k_cache + ((int64_t)page * a.kv_heads + h0) * head + (r >> 5) * (32 * D) + (c % 8 * 32 + (r & 31)) * 8;
-  const RopeLane angles = rope_lane<D, HALVES>(a.rope, c);
-  float own[8], other[8], A[SETS][8], B[SETS][8];
-  if constexpr (NORM) rope_weights<T>(a.rope, a.wk, c, own);
-  if constexpr (NORM && HALVES) rope_weights<T>(a.rope, a.wk, c ^ (C / 2), other);
+  for (int first = begin; first < last; first += 8) {
+    const uint16_t* from[SETS];
+    u32x4 v[AHEAD][SETS];
 #pragma unroll
-  for (int s = 0; s < SETS; ++s) {
-    const RopePlace place = rope_place(a.rope, angles, a.pos + (int64_t)min(first + 4 * s + g, a.n_tokens - 1) * a.rope.axes);
-    rope_factors<D, HALVES, NORM>(angles, place, own, other, c, A[s], B[s]);
-  }
-  for (int h = h0; h < end; h += AHEAD)
+    for (int s = 0; s < SETS; ++s) {
+      from[s] = a.k + min(first + 4 * s + g, last - 1) * a.k_stride + (int64_t)h0 * D + 8 * c;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (h + i >= end) break;
-      u32x4 z[SETS];
-#pragma unroll
-      for (int s = 0; s < SETS; ++s) {
-        float x[8];
-        T::unpack(v[i][s], x);
-        v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(h + i + AHEAD, end - 1) * D - h0 * D));
-        rope_row<D, HALVES, NORM>(a.rope, A[s], B[s], x);
-        z[s] = T::pack(x);
-      }
-      if constexpr (SETS == 2) {
-        // the upper chunks of four tokens against the lower ones of the next four: a store covers eight chunks of eight tokens
-        u32x4 low, high;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t one = z[0][e], two = z[1][e];
-          low[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)one, (int)two, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
-          high[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)two, (int)one, 0x128, 0xf, 0x3, false);     // and into lanes 0-7
-        }
-        if (store) {
-          *reinterpret_cast<u32x4*>(to) = low;
-          *reinterpret_cast<u32x4*>(to + 8 * 32 * 8) = high;
-        }
-      } else if (store) {
-        *reinterpret_cast<u32x4*>(to) = z[0];
-      }
-      to += head;
+      for (int i = 0; i < AHEAD; ++i) v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(i, end - 1 - h0) * D));
     }
+    // the token whose rows a lane stores (below), and where
+    const int mine = first + (SETS == 2 ? 4 * (c / 8) : 0) + g;
+    const int slot = mine < last ? a.slots[mine] : -1;
+    const bool store = slot >= 0 && slot < a.n_slots;
+    const int page = slot >> a.page_shift, r = slot & ((1 << a.page_shift) - 1);
+    const int64_t head = (int64_t)D << a.page_shift;               // elements of a head of a page
+    uint16_t* to = a.k_cache + ((int64_t)page * a.kv_heads + h0) * head + (r >> 5) * (32 * D) + (c % 8 * 32 + (r & 31)) * 8;
+    RopeArgs rope = a.rope;
+    const void* wk = a.wk;
+    asm volatile("" : "+s"(rope.table), "+s"(wk));                 // (what a second turn needs again is read again: in registers it costs wavefronts)
+    float own[8], other[8], A[SETS][8], B[SETS][8];
+    const RopeLane angles = rope_lane<D, HALVES>(rope, c);
+    if constexpr (NORM) rope_weights<T>(rope, wk, c, own);
+    if constexpr (NORM && HALVES) rope_weights<T>(rope, wk, c ^ (C / 2), other);
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      const RopePlace place = rope_place(rope, angles, a.pos + (int64_t)min(first + 4 * s + g, last - 1) * a.rope.axes);
+      rope_factors<D, HALVES, NORM>(angles, place, own, other, c, A[s], B[s]);
+    }
+    for (int h = h0; h < end; h += AHEAD)
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (h + i >= end) break;
+        u32x4 z[SETS];
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+          float x[8];
+          T::unpack(v[i][s], x);
+          v[i][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from[s] + min(h + i + AHEAD, end - 1) * D - h0 * D));
+          rope_row<D, HALVES, NORM>(a.rope, A[s], B[s], x);
+          z[s] = T::pack(x);
+        }
+        if constexpr (SETS == 2) {
+          // the upper chunks of four tokens against the lower ones of the next four: a store covers eight chunks of eight tokens
+          u32x4 low, high;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t one = z[0][e], two = z[1][e];
+            low[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)one, (int)two, 0x128, 0xf, 0xc, false);      // row_ror:8 into lanes 8-15
+            high[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)two, (int)one, 0x128, 0xf, 0x3, false);     // and into lanes 0-7
+          }
+          if (store) {
+            *reinterpret_cast<u32x4*>(to) = low;
+            *reinterpret_cast<u32x4*>(to + 8 * 32 * 8) = high;
+          }
+        } else if (store) {
+          *reinterpret_cast<u32x4*>(to) = z[0];
+        }
+        to += head;
+      }
+  }
 }
 
 template <class T, int D, bool HALVES, bool NORM, bool KEEP>
@@ -153,9 +170,10 @@ extern "C" int rf2_paged_store_rope(const rf2_paged_plan* plan, const rf2_rope_p
   if (n_tokens == 0) return RF2_OK;
   const rf2_rows q_rows{q, 0, n_tokens > 1 ? q_stride : q_row, c.head_dim}, out_rows{q_out, 0, n_tokens > 1 ? q_out_stride : q_row, c.head_dim};
   const RopeSide side{rope_rows(q_rows), rope_rows(out_rows), wq, rope_share(q_rows, c.heads, r, (uint32_t)n_tokens)};
-  // K's wavefronts take as many heads as leave 2,048 of them, four (HALVES: five) at most
+  // K's wavefronts take as many heads as leave 2,048 of them, eight (64 channels: five) at most (us, most heads 4, 8, 16: 4,680 tokens of 40 heads 53.5,
+  // 52.3, 53.1, 20,000 of 32 207, 197, 199; 64 channels, HALVES, 4,680 of 40: 4 31.1, 5 30.6, 8 30.9)
   const int64_t k_work = (int64_t)((n_tokens + 7) / 8) * c.kv_heads;
-  const int k_steps = (int)std::min<int64_t>(r.pairing == RF2_ROPE_HALVES ? 5 : 4, std::max<int64_t>(1, k_work / 2048));
+  const int k_steps = (int)std::min<int64_t>(c.head_dim == 128 ? 8 : 5, std::max<int64_t>(1, k_work / 2048));
   const unsigned k_workgroups = k_windows * (unsigned)((c.kv_heads + k_steps - 1) / k_steps);
   const auto v_workgroups = [&](int tokens) { return (int64_t)((n_tokens + tokens - 1) / tokens) * c.kv_heads; };
   const int v_tokens = v_workgroups(8) <= COMPUTE_UNITS ? 8 : v_workgroups(64) < COMPUTE_UNITS ? 32 : 64;

@@ -79,6 +79,28 @@ def test_workgroups_of_few_and_of_many_tokens(tokens, kv, d, slots):
     c.both(slots=at.int().cuda())
 
 
+@pytest.mark.parametrize("slots", ["run", "runs", "single", "backwards", "padding", "anything"])
+@pytest.mark.parametrize("tokens,kv,d,halves", [(700, 48, 128, False), (1025, 33, 128, True), (999, 40, 64, False), (4099, 8, 64, True)])
+def test_wavefronts_that_begin_where_lines_do(tokens, kv, d, halves, slots):
+    # K in large calls, whose wavefronts take 1 to 15 tokens: each of them once, wherever runs begin and end
+    c = Case(tokens=tokens, heads=kv, kv=kv, d=d, dims=(d,), halves=halves, page=32, n_pages=tokens // 4 + 8)
+    gen = torch.Generator().manual_seed(tokens)
+    i, order = torch.arange(tokens), torch.randperm(c.plan.cfg.n_pages, generator=gen)
+    if slots == "runs":                                       # of 1 to 40 tokens, up to 16 slots apart
+        step = torch.ones(tokens, dtype=torch.long)
+        at = 0
+        while (at := at + int(torch.randint(1, 41, (), generator=gen))) < tokens:
+            step[at] = int(torch.randint(1, 17, (), generator=gen))
+        at = step.cumsum(0) + 2
+    else:
+        at = {"run": i + 13, "single": i * 8 + i % 8, "backwards": tokens + 9 - i, "padding": i + 3, "anything": torch.randperm(4 * tokens, generator=gen)[:tokens]}[slots]
+    at = order[at // 32] * 32 + at % 32
+    if slots == "padding":                                    # and slots that the cache does not have
+        bad = torch.tensor([-1, -8, c.plan.cfg.n_pages * 32, 2 ** 31 - 1, -2 ** 31])
+        at = torch.where(torch.rand(tokens, generator=gen) < 0.2, bad[torch.randint(0, 5, (tokens,), generator=gen)], at)
+    c.both(slots=at.int().cuda())
+
+
 @pytest.mark.parametrize("live", [0, 1, 30, 50])
 def test_padding_stays(live):
     c = Case(tokens=50)
