@@ -463,7 +463,8 @@ int rf2_rope_apply(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, c
  * all rows of all heads.
  *   rows      : as above; dq may be dq_out or q (the same address and strides), dk dk_out or k.  Without a norm q and k are not read and
  *               their `at` is of no account                                                     (host struct)
- *   dwq, dwk  : [d] fp32, written over; NULL without a norm.  Two tensors even where wq is wk: what the weights get is their sum (out)
+ *   dwq, dwk  : [d] fp32, written over: with zeros where there are no rows or the side is left out, for which they may be NULL; NULL
+ *               without a norm.  Two tensors even where wq is wk: what the weights get is their sum (out)
  *   workspace : rf2_rope_info.workspace_bytes, written and read by this call alone: calls that may run at the same time need one each;
  *               may be NULL without a norm                                                     (scratch)
  * The same call gives the same bits each time.

@@ -293,10 +293,11 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     if (const int rc = check_rows(plan, batch, n_tokens, sides, 3)) return rc;
     if (!rf2_rope_pos_fits(plan, pos)) return RF2_ERR_INVALID_ARG;
   }
+  // Sides with rows; sums over no rows, of a side that is left out too, are zeros.
+  const bool have[2] = {!nothing && t.dq.at != nullptr, !nothing && t.dk.at != nullptr};
   float* const dw[2] = {dwq, dwk};
-  const bool have[2] = {nothing ? dwq != nullptr : t.dq.at != nullptr, nothing ? dwk != nullptr : t.dk.at != nullptr};
   for (int i = 0; i < 2; ++i) {
-    if (have[i] && !nothing && !rf2_rope_weight_fits(plan, i == 0 ? wq : wk)) return RF2_ERR_INVALID_ARG;
+    if (have[i] && !rf2_rope_weight_fits(plan, i == 0 ? wq : wk)) return RF2_ERR_INVALID_ARG;
     if (norm ? (have[i] && !dw[i]) || !rf2_rope_aligned(dw[i], 4) : dw[i] != nullptr) return RF2_ERR_INVALID_ARG;
   }
   if (norm && (!workspace || !rf2_rope_aligned(workspace, 16))) return RF2_ERR_INVALID_ARG;
@@ -313,7 +314,12 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
   JoinArgs<float, float> join{};
   int64_t bytes = 0;
   for (int i = 0; i < 2; ++i) {
-    if (!have[i]) continue;
+    const RopeWorkspace ws = rope_workspace(c.head_dim, i);
+    float* const sums = (float*)((char*)workspace + ws.sums);
+    if (!have[i]) {
+      if (dw[i]) join.side[i] = {sums, dw[i], 0, 1};
+      continue;
+    }
     BackSide& s = a.side[i];
     s.x = rope_rows(i == 0 ? t.q : t.k);
     s.dz = rope_rows(i == 0 ? t.dq_out : t.dk_out);
@@ -322,9 +328,7 @@ extern "C" int rf2_rope_backward(const rf2_rope_plan* plan, int32_t batch, int32
     const int heads = i == 0 ? c.heads : c.kv_heads;
     s.share = rope_share(i == 0 ? t.q : t.k, heads, c, a.tokens.total);
     const uint32_t units = rope_workgroups(s.share);
-    s.workgroups = nothing ? 0 : std::min<uint32_t>(units, units > RF2_ROPE_MANY ? RF2_ROPE_PARTS : RF2_ROPE_FEW);
-    const RopeWorkspace ws = rope_workspace(c.head_dim, i);
-    float* const sums = (float*)((char*)workspace + ws.sums);
+    s.workgroups = std::min<uint32_t>(units, units > RF2_ROPE_MANY ? RF2_ROPE_PARTS : RF2_ROPE_FEW);
     s.sums = s.workgroups == 1 ? dw[i] : sums;
     if (s.workgroups > RF2_ROPE_FEW) {
       const uint32_t n = (s.workgroups + 63) / 64;
