@@ -6,7 +6,7 @@
 #include "rf2_internal.h"
 
 // Of each pair of channels, turns per unit of its axis' position, whole turns left out, in units of 2^-32 (rounded to the nearest) and what is
-// left of them in units of 2^-64; and the axis.  A lane reads those of its pairs in a few wide loads.
+// left of them in units of 2^-64 (to the nearest too); and the axis.  A lane reads those of its pairs in a few wide loads.
 struct rf2_rope_table {
   int32_t turns[64], rest[64];
   uint8_t axis[64];
@@ -150,8 +150,10 @@ __device__ __forceinline__ RopePlace rope_place(const RopeArgs& a, const RopeLan
 
 // Cosine and signed sine for each of a lane's channels: channel c turns to x_c cs_c + x_partner sn_c.
 // Position times frequency in whole numbers, of which the carries out of 32 bits are whole turns and fall away: what is left is the angle's
-// fraction of a turn with a sign, off by 2^-32 of one at any position.  In 32 bits (2^-26 turns off at most) it goes to the hardware's sine and
-// cosine (off by 1.3e-7 at most, measured over 2^20 angles; 3.5e-8 on average, where rounding to 32 bits alone is 1.5e-8).
+// fraction of a turn with a sign.  At any position it is off by 1.5 2^-32 of one at most: cut off below 2^-32, a frequency half of 2^-64 off, and half
+// of 2^-64 more where it comes from a base of 1 or more (a smaller base has frequencies above 1, in 64 bits: (|ln f| + 2) f 2^-64 radians).  In 32 bits
+// (2^-26 turns off at most) it goes to the hardware's sine and cosine (off by 1.3e-7 at most, measured over 2^20 angles; 3.5e-8 on average, where
+// rounding to 32 bits alone is 1.5e-8).
 template <int D, bool HALVES>
 __device__ __forceinline__ void rope_angles(const RopeLane& lane, const RopePlace& place, int c, float (&cs)[8], float (&sn)[8]) {
   float co[4], si[4];

@@ -4,6 +4,24 @@
 #include <cmath>
 #include <new>
 
+namespace {
+
+// Turns of a frequency, f / 2 pi, |f| <= 2^16, in units of 2^-64, whole turns left out, to the nearest.  f has 64 bits, 1 / 2 pi here 126: the product
+// in whole numbers is 2^16 2^64 2^-128 units off at most.  (A quotient of 64 bits loses of the fraction what the whole turns take, and a
+// position multiplies it.)
+uint64_t fraction_of_turns(long double f) {
+  typedef unsigned __int128 u128;
+  constexpr uint64_t HIGH = 0x28be60db9391054a, LOW = 0x7f09d5f47d4d3770;             // 2^128 / 2 pi
+  int e = 0;
+  const uint64_t m = (uint64_t)ldexpl(frexpl(fabsl(f), &e), 64);                      // |f| = m 2^(e - 64)
+  if (e <= -64) return 0;                                                             // (less than half a unit)
+  const u128 product = (u128)m * HIGH + ((u128)m * LOW >> 64);                        // of m 2^64 / 2 pi
+  const uint64_t turns = (uint64_t)((product + ((u128)1 << (63 - e))) >> (64 - e));
+  return f < 0 ? 0 - turns : turns;
+}
+
+}  // namespace
+
 extern "C" {
 
 int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host, rf2_rope_plan** out) {
@@ -27,8 +45,7 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
   if (dims > c.head_dim) return RF2_ERR_INVALID_ARG;
   if (c.axes > 0 && !inv_freq_host && !(c.theta > 0.0 && std::isfinite(c.theta))) return RF2_ERR_INVALID_ARG;
 
-  // turns per position of each pair, in the 64 bits of a long double; pairs behind the last axis do not turn
-  constexpr long double TWO_PI = 6.283185307179586476925286766559L;
+  // turns per position of each pair; pairs behind the last axis do not turn
   rf2_rope_table tables[2] = {};
   int i = 0;
   for (int a = 0; a < c.axes; ++a)
@@ -36,12 +53,10 @@ int rf2_rope_plan_create(const rf2_rope_config* cfg, const double* inv_freq_host
       const long double f = inv_freq_host ? (long double)inv_freq_host[i] : powl((long double)c.theta, -2.0L * j / c.axis_dim[a]);
       if (!(fabsl(f) <= 65536.0L)) return RF2_ERR_INVALID_ARG;
       for (int way = 0; way < 2; ++way) {
-        const long double turns = (way == 0 ? f : -f) / TWO_PI, part = (turns - rintl(turns)) * 0x1p32L, whole = rintl(part);     // |part| <= 2^31
-        const int64_t rest = llrintl((part - whole) * 0x1p32L);                                                                  // |rest| <= 2^31
-        // (2^31 units are as good as -2^31, but so many of the rest are one more or less of the others)
-        const int64_t carry = rest > INT32_MAX ? 1 : 0;
-        tables[way].turns[i] = (int32_t)(uint32_t)(uint64_t)((int64_t)whole + carry);
-        tables[way].rest[i] = (int32_t)(rest - (carry << 32));
+        const uint64_t turns = fraction_of_turns(way == 0 ? f : -f);
+        const int32_t rest = (int32_t)(uint32_t)turns;                 // with a sign: what is left is a multiple of 2^32 again
+        tables[way].turns[i] = (int32_t)(uint32_t)((turns - (uint64_t)(int64_t)rest) >> 32);
+        tables[way].rest[i] = rest;
       }
       tables[0].axis[i] = tables[1].axis[i] = (uint8_t)a;
     }
