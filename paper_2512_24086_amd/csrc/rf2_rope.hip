@@ -229,6 +229,8 @@ int check_rows(const rf2_rope_plan* plan, int32_t batch, int32_t n_tokens, rf2_r
       if (heads == 1) rows[i][j]->head = 0;
       if ((rows[i][j]->at == nullptr) != (rows[i][n - 1]->at == nullptr)) return RF2_ERR_INVALID_ARG;
       if (rows[i][j]->at && (!readable(*rows[i][j]) || !in_range(*rows[i][j], batch, n_tokens, heads))) return RF2_ERR_INVALID_ARG;
+      // (the only token has its heads side by side, whatever its stride is)
+      if (rows[i][j]->at && batch == 1 && n_tokens == 1) rows[i][j]->token = rows[i][j]->head * heads;
     }
     const rf2_rows& out = *rows[i][n - 1];
     if (out.at && !writable(out, batch, n_tokens, heads, plan->cfg.head_dim)) return RF2_ERR_INVALID_ARG;

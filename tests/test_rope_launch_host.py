@@ -89,3 +89,33 @@ def test_turns_of_a_base(library, theta):
         pairs = [(j, 60) for j in range(30)] + [(j, 68) for j in range(34)]
         for (j, dim), units in zip(pairs, way):
             assert off(units, exact_turns(sign * exact_frequency(theta, j, dim))) <= 1.0, (theta, j, dim)
+
+
+def grids(library, backward, batch, tokens, layout, **over):
+    """Workgroups of each launch of a call on dense rows; `layout` is the order of tokens and heads, or the strides of both."""
+    cfg = config(**over)
+    rows = []
+    for _ in range(3 if backward else 2):
+        for heads in (cfg.heads, cfg.kv_heads):
+            token, head = {"bnhd": (heads * cfg.head_dim, cfg.head_dim), "bhnd": (cfg.head_dim, tokens * cfg.head_dim)}.get(layout, layout)
+            rows += [1 << 20, tokens * heads * cfg.head_dim, token, head]
+    out = (C.c_uint32 * 16)()
+    n = library.rope_grids(C.byref(cfg), int(backward), batch, tokens, (C.c_int64 * len(rows))(*rows), out)
+    assert n >= 0, n
+    return list(out[:n])
+
+
+@pytest.mark.parametrize("layout", ["bnhd", "bhnd", (0, 128), (8, 4096), (1 << 40, 128)], ids=str)
+@pytest.mark.parametrize("heads, kv, d, workgroups", [(8, 2, 64, 2), (40, 40, 128, 20), (7, 1, 128, 8), (32, 8, 128, 10), (16, 16, 64, 4)])
+def test_one_token_is_rows_of_heads_side_by_side(library, heads, kv, d, workgroups, layout):
+    # a wavefront's 64 / (d / 8) rows are heads, as many as divide all, whatever the stride of the only token is
+    sizes = dict(heads=heads, kv_heads=kv, head_dim=d, dims=(d,))
+    assert grids(library, False, 1, 1, layout, **sizes) == [workgroups]
+    # the gradients' sums of one workgroup need no launch of their own
+    alone = heads <= 512 // d and kv <= 512 // d
+    assert grids(library, True, 1, 1, layout, **sizes) == ([workgroups] if alone else [workgroups, d // 4])
+
+
+def test_few_tokens_keep_their_layout(library):
+    assert grids(library, False, 1, 4, "bhnd", heads=8, kv_heads=8) == [16] and grids(library, False, 1, 4, "bnhd", heads=8, kv_heads=8) == [4]
+    assert grids(library, False, 4, 1, "bnhd", heads=8, kv_heads=8) == [4]
