@@ -401,7 +401,8 @@ int rf2_paged_attn(const rf2_paged_plan* plan, int32_t n_seqs, int32_t n_tokens,
  * theta^(-2j / axis_dim[a]), or the pairs' frequencies come from a table.  Pairs behind the last axis do not turn.
  *
  * All in 32 bits (angles in 64, so that far positions keep theirs), rounded to dtype once.  Rows of any finite numbers are
- * normalised; what is not finite makes its pair not a number, or with a norm its row (an infinity: its pair, and the rest of the row 0).
+ * normalised.  What is not finite stays in its pair without a norm: not a number makes both channels so, an infinity makes both infinite or not a
+ * number.  With a norm not a number makes its whole row so, an infinity its pair, and the rest of the row 0.
  * Positions are int32 in device memory, any value, [n_tokens][axes].  Conventions as above.
  */
 enum { RF2_NORM_NONE = 0, RF2_NORM_RMS = 1 };

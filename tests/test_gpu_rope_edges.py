@@ -1,9 +1,10 @@
-"""Norms and rotations: calls of C that the binding does not make."""
+"""Norms and rotations: calls of C that the binding does not make, numbers that are not finite without a norm."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2512_24086_amd import rf2
-from tests.test_gpu_rope import Case
+from tests.test_gpu_rope import NONE, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +32,22 @@ def test_gradients_of_weights_whose_side_is_left_out_are_sums_over_no_rows(case,
     assert code == rf2.RF2_OK
     assert torch.equal(dx, back[at]) and torch.equal(dw[at], back[2 + at])
     assert (dw[1 - at] == 0).all()
+
+
+@pytest.mark.parametrize("halves", [False, True])
+def test_rotations_alone_of_rows_that_are_not_finite(halves):
+    # the last pair does not turn, and token 0 is where no pair does
+    c = Case(tokens=9, heads=2, kv=2, norm=NONE, halves=halves, dims=(44, 42, 40))
+    c.pos[0] = 0
+    c.rot = type(c.rot)(c.pos.cpu().numpy()[None], 128, (44, 42, 40), 10000.0, halves)
+    want, _ = c.forward()
+    partner = [(i + 64) % 128 if halves else i ^ 1 for i in range(128)]
+    for n, i, value in [(n, i, value) for n in (0, 4) for i in (0, 5, 62, 63, 64, 127) for value in (float("inf"), float("-inf"), float("nan"))]:
+        q, out = c.q.clone(), c.like(c.q)
+        q[0, n, 1, i] = value
+        c.plan.rf2_rope_apply(q, None, c.pos, out, None)
+        pair = [i, partner[i]]
+        got = out[0, n, 1, pair]
+        assert not got.isfinite().any() and (not np.isnan(value) or got.isnan().all()), (n, i, value)
+        out[0, n, 1, pair] = want[0, n, 1, pair]
+        assert torch.equal(out, want), (n, i, value)
