@@ -1,10 +1,10 @@
-"""Norms and rotations: calls of C that the binding does not make, numbers that are not finite without a norm."""
+"""Norms and rotations: calls of C that the binding does not make, gradients that lie over the inputs, numbers that are not finite without a norm."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2512_24086_amd import rf2
-from tests.test_gpu_rope import NONE, Case
+from tests.test_gpu_rope import BHND, NONE, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,20 @@ def test_rotations_alone_of_rows_that_are_not_finite(halves):
         assert not got.isfinite().any() and (not np.isnan(value) or got.isnan().all()), (n, i, value)
         out[0, n, 1, pair] = want[0, n, 1, pair]
         assert torch.equal(out, want), (n, i, value)
+
+
+@pytest.mark.parametrize("case", [dict(), dict(layout=BHND), dict(joint=True, tokens=300, heads=16, kv=4), dict(joint=True, layout=BHND, batch=2, tokens=65),
+                                  dict(halves=True, d=64, dims=(64,)), dict(tokens=3001, heads=40, kv=8, d=64, dims=(16, 24, 24))], ids=str)
+def test_gradients_over_the_inputs(case):
+    # dq over q and dk over k; with a joint projection its other columns stay
+    c = Case(**case)
+    want = c.backward()
+    joint = case.get("joint")
+    q, k = (c.q, c.k) if joint else (c.q.clone(), c.k.clone())
+    v = (q.transpose(1, 2) if c.layout == BHND else q)._base if joint else None
+    before = v.clone() if joint else None
+    dw = [torch.full((c.d,), float("nan"), device="cuda") for _ in range(2)]
+    c.plan.rf2_rope_backward(q, k, c.pos, c.dq_out, c.dk_out, q, k, c.wq, c.wk, *dw, c.plan.alloc_workspace())
+    assert all(torch.equal(a, b) for a, b in zip(want, (q, k, *dw)))
+    if joint:
+        assert torch.equal(v[:, :, c.heads + c.kv:], before[:, :, c.heads + c.kv:])
