@@ -261,6 +261,8 @@ class Plan:
     def layer_fused(self, q, k, v, buf, stream=None, rope=None, pos=None, weights=()):
         """The whole layer with the inverse permutation fused into the attention epilogue; returns buf['o'].  With a RopePlan, and pos and
         weights (wq, wk, wq_text, wk_text: as many as there are) as rf2_permute_rope takes them, q and k are raw projections."""
+        if rope is None and (pos is not None or any(w is not None for w in weights or ())):
+            raise ValueError("pos, weights: expected with rope, the RopePlan that they are for")
         stream = torch.cuda.current_stream() if stream is None else stream
         if rope is None:
             self.rf2_permute(q, k, v, buf["qp"], buf["kp"], buf["vp"], buf["qbar"], buf["kbar"], stream)
