@@ -178,6 +178,7 @@ class Plan:
         _check(lib().rf2_plan_create(C.byref(self.cfg), C.byref(self._h)), "rf2_plan_create")
         self.info = rf2_info()
         _check(lib().rf2_plan_info(self._h, C.byref(self.info)), "rf2_plan_info")
+        self._shape = (batch, self.info.N, heads, head_dim) if qkv_layout == RF2_LAYOUT_BNHD else (batch, heads, self.info.N, head_dim)
 
     def close(self):
         if self._h:
@@ -228,10 +229,14 @@ class Plan:
                                  _ptr(kbar), _stream(stream)), "rf2_permute")
 
     def rf2_permute_rope(self, rope, q, k, v, pos, qp, kp, vp, qbar=None, kbar=None, wq=None, wk=None, wq_text=None, wk_text=None, stream=None):
-        """rf2_permute of q and k normalised and rotated by a RopePlan; pos is [N, axes] or [batch, N, axes], text tokens behind the grid's."""
+        """rf2_permute of q and k normalised and rotated by a RopePlan; pos is [N, axes] or [batch, N, axes], text tokens behind the grid's.  q, k and v
+        are laid out as this plan's qkv_layout says, whatever the RopePlan's own layout is."""
         c, i, dev, bf, f32 = self.cfg, self.info, rope.device, torch.bfloat16, torch.float32
         at, step = rope._pos(pos, c.batch, i.N)
         row = c.batch * c.heads * c.head_dim
+        if not q.shape == k.shape == v.shape == self._shape:
+            for x, what in ((q, "q"), (k, "k"), (v, "v")):
+                _not_the_other_layout(x, what, self._shape)
         _check(lib().rf2_permute_rope(
             self._h, rope._h, _arg(q, "q", bf, row * i.N, dev), _arg(k, "k", bf, row * i.N, dev), _arg(v, "v", bf, row * i.N, dev), at, step,
             rope._weight(wq, "wq"), rope._weight(wk, "wk"), None if wq_text is None else rope._weight(wq_text, "wq_text"),
@@ -296,6 +301,13 @@ def _arg(t, what, dtype, numel, device):
         raise ValueError(f"{what}: expected {numel} contiguous elements of {dtype} on device {device}, got "
                          f"{tuple(t.shape)} of {t.dtype} on {t.device}, strides {t.stride()}")
     return t.data_ptr()
+
+
+def _not_the_other_layout(t, what, shape):
+    """Refuses a tensor whose tokens and heads stand in each other's place of `shape`, [batch, tokens, heads, head_dim] or [batch, heads, tokens, head_dim]."""
+    last = tuple(t.shape[-3:])
+    if last != shape[1:] and last == (shape[2], shape[1], shape[3]):
+        raise ValueError(f"{what}: expected {shape}, got {tuple(t.shape)}: tokens and heads the other way round")
 
 
 def _rows(t, what, dtype, shape, device):
@@ -450,7 +462,7 @@ class RopePlan:
     `layout` says how the tensors handed over are indexed: [batch, tokens, heads, head_dim] (RF2_LAYOUT_BNHD) or
     [batch, heads, tokens, head_dim] (RF2_LAYOUT_BHND), with or without the batch; their rows may lie anywhere (parts of a joint
     projection, views), channels side by side.  pos is [tokens, axes] or [batch, tokens, axes], int32.  A plan's rotation may also ride on
-    `Plan.rf2_permute_rope` and `PagedPlan.rf2_paged_store_rope`.
+    `Plan.rf2_permute_rope` and `PagedPlan.rf2_paged_store_rope`, which go by the layout of the plan that they belong to.
     """
 
     def __init__(self, *, heads, kv_heads, head_dim, axis_dims, theta=10000.0, inv_freq=None, pairing=RF2_ROPE_PAIRS, norm=RF2_NORM_RMS,
