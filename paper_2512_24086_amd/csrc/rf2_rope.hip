@@ -3,7 +3,7 @@
 // HBM bound: each row is read once and written once.  d / 8 neighbouring lanes hold a row, 16 bytes each.  Cosines and sines belong to a
 // token, not to a head: a wavefront takes a few tokens, works their angles out once and goes through the heads, 64 / (d / 8) rows at a
 // time.  Those are consecutive tokens of a head where tokens lie side by side, consecutive heads of a token where heads do.  75,600 tokens of
-// 40 + 40 heads: 3.1 GB in 494 us, 6.3 TB/s (a large copy reaches 6.2); the vector unit is 77 % busy beside it.  48 tokens: 3.0 us in a graph, 8.2 with
+// 40 + 40 heads: 3.1 GB in 497 us, 6.2 TB/s (a large copy reaches 6.2); the vector unit is 77 % busy beside it.  48 tokens: 2.8 us in a graph, 8.0 with
 // the host's part of a call.
 #include "rf2_rope.h"
 
@@ -38,12 +38,13 @@ struct BackArgs {
 };
 
 // With g = R(-phi) dz and x^ = x r:  dx = r (g w - x^ mean(g w x^)),  dw = sum over rows of g x^.  Sums of dw: a token's heads in 32 bits, a
-// lane's tokens in 64, then the rows of the workgroup in order.
+// lane's tokens in 64, then the rows of the workgroup in order, in 64 too.  A lane's sum and a workgroup's are handed on in 32 bits
+// (2^-24 of each, no more than a sum of a token's heads may be off).
 //
 // HBM bound: x and dz are read once, dx is written once.  Loads of a token's next two heads are asked for before those in hand are worked on.  Large
 // calls take 8,192 workgroups for each of Q and K, many more than are resident, which reads faster than few that go round (32,760 tokens of
-// 40 + 40 heads: 1,024 354 us, 4,096 336, 8,192 323, and 10 for their sums; sums by elements, read and written alike, take 312).  Smaller ones are
-// better off with 512, whose sums one launch adds up.
+// 40 + 40 heads: 1,024 354 us, 4,096 336, 8,192 323, and 10 for their sums; sums by elements, read and written alike, take 312).  Smaller ones,
+// up to 2,048 units, take 512 at most, whose sums one launch adds up.
 template <class T, int D, bool HALVES, bool KEEP>
 __global__ void __launch_bounds__(256, 4) backward_kernel(BackArgs a) {
   constexpr int CH = D / 8, R = 64 / CH, U = 2;
